@@ -64,7 +64,9 @@ typedef enum {
   NNC_F32 = 0,
   NNC_BF16 = 1,
   NNC_F16 = 2, /* IEEE binary16, the paper's F16 (Section 4, setup) */
-  NNC_W8 = 3   /* blob_dtype only: bytes with one scale per output row in the layers, bf16 elsewhere */
+  NNC_W8 = 3,  /* blob_dtype only: bytes with one scale per output row in the layers, bf16 elsewhere */
+  NNC_I8 = 4,  /* paged KV cache only: signed bytes -127 .. 127 with one fp32 scale per row and kv head */
+  NNC_E4M3 = 5 /* paged KV cache only: OCP 8-bit floats (4 exponent bits, largest 448), scales likewise */
 } nnc_dtype;
 
 typedef struct {
@@ -377,6 +379,185 @@ nnc_status nnc_plan_prefill_gemm_query(uint32_t rows, uint32_t k, uint32_t n_tok
 nnc_status nnc_plan_skinny_gemm_query(uint32_t rows, uint32_t k, uint32_t n_seq, uint32_t pieces,
                                       uint32_t epilogue, uint32_t max_k_slices, uint32_t n_cus,
                                       nnc_gemm_plan *out);
+
+/* =============================================================================================
+ * Paged KV cache, and the search that shares its pages.  (The paper's runs are one sequence in one
+ * cache; nothing of this section is in it, all of it is defined here.)
+ *
+ * Operators of their own, without a model: nnc_page_append, nnc_page_read, nnc_page_attention,
+ * nnc_page_reorder, nnc_beam_select.  They enqueue on `stream` (hipStream_t, NULL = default stream) of
+ * the current device, which must be the one that holds every buffer named in the call; they allocate
+ * nothing, keep nothing and may be captured into a graph.  Buffers belong to the caller and must live
+ * until the work has run; a workspace may serve any number of calls that follow each other in one
+ * stream, not calls (or replays of graphs that captured it) that may run side by side.
+ * What the host can see is checked (NNC_E_ARG); page numbers, positions and lengths lie in device
+ * memory and are checked on the device: what each call does about a wrong one is said there.
+ *
+ * nnc_pages: one pool for all layers, memory of the caller:
+ *   k, v              [n_layers][n_pages][n_kv_heads][page_tokens][head_dim] of dtype, on a multiple of 16 bytes
+ *   k_scale, v_scale  [n_layers][n_pages][n_kv_heads][page_tokens] fp32 for NNC_I8 and NNC_E4M3, else NULL
+ * dtype: NNC_F32, NNC_BF16, NNC_F16, NNC_I8 or NNC_E4M3.  head_dim: 64 or 128.  page_tokens: 1 .. 4096,
+ * n_kv_heads and n_layers: up to 1024.  Pages need no initial contents.
+ * nnc_page_table: entries [n_seqs][max_pages], device: position p of sequence i is row p % page_tokens of
+ * page entries[i][p / page_tokens].  Sequences may name the same page (a shared prompt) as long as nobody writes to it.
+ */
+typedef struct {
+  uint32_t struct_bytes; /* = sizeof(nnc_pages) */
+  uint32_t dtype, n_layers, n_pages, page_tokens, n_kv_heads, head_dim;
+  void *k, *v;
+  float *k_scale, *v_scale;
+} nnc_pages;
+
+typedef struct {
+  const int32_t *entries;
+  uint32_t n_seqs, max_pages;
+} nnc_page_table;
+
+/* Rows of K and V: row i, kv head h, element e at k[i * k_row_stride + h * k_head_stride + e] (elements of dtype:
+ * NNC_F32, NNC_BF16 or NNC_F16; any strides), likewise v.  Row i is position pos[i] of sequence seq[i] (device
+ * arrays of n; NULL: every row is of sequence seq0; row i is position pos0 + i). */
+typedef struct {
+  void *k, *v;
+  uint32_t dtype;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  uint32_t n;
+  const int32_t *seq, *pos;
+  int32_t seq0, pos0;
+} nnc_page_rows;
+
+/*
+ * Write rows into the pages of one layer.  16- and 32-bit pools round to nearest even.  8-bit pools take, for each row
+ * and kv head, scale = max(max |x| / T, 2^-80) in fp32 (T = 127 for NNC_I8, 448 for NNC_E4M3) and store x / scale, rounded
+ * to the nearest value of the format (ties to even): off by at most scale / 2, or by 2^-4 of the value (2^-10 scale at the
+ * least).  A row of which one value is not finite becomes NaN as a whole (its scale does).
+ * A row with a negative position is padding and is not written; nor is one whose sequence, position or page
+ * does not exist.  Rows of one call must be different positions.  The rows are only read.
+ */
+nnc_status nnc_page_append(const nnc_pages *pages, uint32_t layer, const nnc_page_table *table,
+                           const nnc_page_rows *rows, void *stream);
+
+/*
+ * The way back: read the named positions of one layer into rows (k or v may be NULL).  Values are value * scale in
+ * fp32, rounded once to the rows' type.  A row whose sequence, position or page does not exist becomes NaN.
+ */
+nnc_status nnc_page_read(const nnc_pages *pages, uint32_t layer, const nnc_page_table *table,
+                         const nnc_page_rows *rows, void *stream);
+
+/* One query row per sequence of the table: q head a of row i at q[i * q_row_stride + a * q_head_stride], reading kv
+ * head a / (n_q_heads / n_kv_heads); out in the same type, with strides of its own (it may be q itself). */
+typedef struct {
+  const void *q;
+  void *out;
+  uint32_t dtype, n_q_heads;
+  int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+  const int32_t *lens; /* device [n_seqs]: cached positions of each sequence */
+  uint32_t max_len;    /* none of them is larger (it sizes the launch); 0: what the table holds */
+  uint32_t window;     /* only the last `window` positions are attended to; 0: all */
+  float scale;         /* of the scores, e.g. 1 / sqrt(head_dim) */
+} nnc_page_query;
+
+/*
+ * Attention of one new token per sequence over one layer: softmax(scale * q K^T) V over positions 0 .. lens[i] - 1
+ * (the last `window` of them).  Sums, softmax statistics and scores are fp32-grade whatever the types; out is
+ * rounded once.  A sequence of length 0 gives zeros; a negative length, one above max_len and a missing page
+ * give NaN.  What pages hold beyond a sequence's length is not looked at.
+ * Long sequences are split over several workgroups and their results joined in a fixed order: the same call gives the same
+ * bits.  How they are split depends on max_len, n_seqs and the heads, so results for another max_len
+ * differ in rounding.  workspace: nnc_page_attention_workspace bytes (which may be 0), on a multiple of 16.
+ */
+nnc_status nnc_page_attention_workspace(const nnc_pages *pages, const nnc_page_table *table,
+                                        const nnc_page_query *query, size_t *bytes);
+nnc_status nnc_page_attention(const nnc_pages *pages, uint32_t layer, const nnc_page_table *table,
+                              const nnc_page_query *query, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Beams take over the cache of the beams that they continue.  Sequences g * width .. + width - 1 of the table are
+ * the beams of group g, all of one length lens[g * width] (device [n_seqs]); parents: device [n_seqs], each
+ * 0 .. width - 1 (another value: the beam continues itself).  With f full pages and r more rows:
+ *   after[b][i] = before[parent of b][i]  for i < f;
+ *   if r > 0, rows 0 .. r - 1 of page before[parent][f] are copied to page after[b][f], in every layer;
+ *   the other entries of after stay: from f on they name pages of the beam's own, which no other beam of `after` has.
+ * after: device [n_seqs][max_pages], may be before->entries itself (then a beam's page may be another's
+ * source, in any permutation).  Full pages are shared, nothing of them is copied.  A length that is negative or does not fit
+ * the table changes nothing; a missing page is not copied.  width: up to 32.
+ */
+nnc_status nnc_page_reorder(const nnc_pages *pages, const nnc_page_table *before, int32_t *after,
+                            const int32_t *lens, const int32_t *parents, uint32_t width, void *stream);
+
+/* One step of a beam search over n_groups groups of `width` beams (row r = group * width + beam). */
+typedef struct {
+  const void *logits;      /* device, row r at logits + r * row_stride, vocab elements of dtype */
+  uint32_t dtype;          /* NNC_F32, NNC_BF16 or NNC_F16 */
+  int64_t row_stride;
+  uint32_t n_groups, width, vocab;
+  const float *scores;     /* device [rows]: log-probability so far; -infinity: the beam is not in use */
+  const uint8_t *finished; /* device [rows]: not 0 where the beam has ended; NULL: none has */
+  int32_t eos;             /* token that ends a beam, -1: none (then finished must be NULL) */
+  int32_t *tokens_out, *parents_out; /* device [rows] */
+  float *scores_out;       /* device [rows], may be scores */
+  uint8_t *finished_out;   /* device [rows] or NULL, may be finished */
+} nnc_beam;
+
+/*
+ * The `width` best continuations of every group, best first.  Beam w continued by token v has the score
+ * scores[w] + logit[v] - log sum_u exp(logit[u]); an ended beam has one continuation, eos with its score unchanged; the
+ * logits of ended and unused beams are not looked at (every continuation of an unused one is -infinity).
+ * Ties go to the lower beam, then to the lower token.  Sums in fp32 and wider; scores of different beams are
+ * compared in 64 bits.  A logit of -infinity forbids its token (score -infinity: chosen only when
+ * nothing else is left).  A beam with a NaN or a +infinity among its logits has NaN scores, and NaN ranks first, so that
+ * such a failure shows; its tokens rank by logit.  width: up to 32.
+ * workspace: nnc_beam_select_workspace bytes, on a multiple of 16.
+ */
+nnc_status nnc_beam_select_workspace(const nnc_beam *beam, size_t *bytes);
+nnc_status nnc_beam_select(const nnc_beam *beam, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A model on pages.  The three calls below run on the model's stream like every other call on it; pages must have the
+ * model's layers, kv heads and head_dim, any dtype.  They do not touch the lengths of the model's slots.
+ *
+ * Copy positions pos0 .. pos0 + n - 1 of a slot's cache, all layers, to the same positions of sequence `seq` of the
+ * table: a prompt goes through nnc_prefill into a slot and from there into pages, and the slot is free again.
+ */
+nnc_status nnc_pages_store(nnc_model *m, const nnc_pages *pages, const nnc_page_table *table, uint32_t seq,
+                           uint32_t slot, uint32_t pos0, uint32_t n);
+
+/*
+ * One decode step of the table's sequences (up to 21): token tokens[i] (device) becomes position lens[i] (device) of
+ * sequence i, in pages that must be there already, and lens[i] grows by one.  max_len: no lens[i] is larger before
+ * the call (0: only the table and max_seq bound them); NNC_E_KV_FULL if max_len + 1 positions fit neither the table
+ * nor the rotary table (max_seq).  logits_out: device [n_seqs, vocab] floats or NULL, next_out: device [n_seqs] greedy
+ * tokens or NULL.  A sequence whose token is outside the vocabulary, or whose length is outside 0 .. max_len, gets
+ * NaN logits, caches nothing and keeps its length.
+ * The arithmetic is that of nnc_decode_step, but for what the cache's type loses and the order of sums.
+ */
+nnc_status nnc_decode_step_paged(nnc_model *m, const nnc_pages *pages, const nnc_page_table *table, int32_t *lens,
+                                 uint32_t max_len, const int32_t *tokens, float *logits_out, int32_t *next_out);
+
+/*
+ * Beam search on the device: n_steps times a decode step of every beam, nnc_beam_select and nnc_page_reorder, without
+ * host synchronisation.  tables: device [n_groups * width][max_pages], updated; the entries behind the full pages are
+ * the beam's own.  With first_logits (device [n_groups][vocab], e.g. of nnc_prefill) the search begins: all beams of a
+ * group stand at the same prompt, whose full pages every one of them names and whose last, not full page lies in beam
+ * 0's own; scores and finished are set by the call, and its first step only selects and reorders.  Without, it
+ * goes on from `tokens`, scores and finished as the call before left them (tokens: the last row of its tokens_out).
+ * lens: device [n_groups * width], updated (a first step adds nothing); max_len as for nnc_decode_step_paged, before the call.
+ * tokens_out, parents_out: device [n_steps][n_groups * width]; scores, finished: device [n_groups * width].
+ * Beams that have ended keep their score and repeat eos.  n_groups * width: up to 21.
+ */
+typedef struct {
+  int32_t *tables;
+  uint32_t max_pages, n_groups, width;
+  int32_t *lens;
+  uint32_t max_len;
+  const float *first_logits; /* or NULL */
+  const int32_t *tokens;     /* device [n_groups * width]; not read with first_logits */
+  int32_t eos;               /* -1: none */
+  uint32_t n_steps;
+  int32_t *tokens_out, *parents_out;
+  float *scores;
+  uint8_t *finished;
+} nnc_beam_run;
+nnc_status nnc_decode_beam(nnc_model *m, const nnc_pages *pages, const nnc_beam_run *run);
 
 /* Bytes of the canonical blob for a config (0 if the config is invalid).  (Paper silent: the blob
  * is this library's input format, the stand-in for the paper's pre-laid-out constants,

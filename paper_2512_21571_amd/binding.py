@@ -15,6 +15,7 @@ from . import _build
 OK, E_ARG, E_CONFIG, E_BLOB, E_NOMEM, E_KV_FULL, E_DEVICE, E_STATE = range(8)
 F32, BF16, F16 = 0, 1, 2
 W8 = 3   # blob dtype only (weight-only 8 bits); computes in BF16
+I8, E4M3 = 4, 5   # paged KV cache only
 OPT_GRAPH, OPT_PREFILL_EXACT, OPT_PERSISTENT, OPT_STAGE_TRACE, OPT_PREFILL_TILE, OPT_SPIN_LIMIT = 0, 1, 2, 3, 4, 5
 OPT_PREFILL_ATTN = 6
 OPT_FUSE_QK = 7
@@ -33,6 +34,8 @@ EXPORTS = [
     "nnc_kv_reset", "nnc_synchronize", "nnc_slot_len", "nnc_prefill_hidden", "nnc_decode_step_hidden", "nnc_kv_read",
     "nnc_set_option", "nnc_profile_begin", "nnc_profile_end", "nnc_stage_trace", "nnc_blob_bytes",
     "nnc_last_error", "nnc_plan_prefill_gemm_query", "nnc_plan_skinny_gemm_query",
+    "nnc_page_append", "nnc_page_read", "nnc_page_attention_workspace", "nnc_page_attention", "nnc_page_reorder",
+    "nnc_beam_select_workspace", "nnc_beam_select", "nnc_pages_store", "nnc_decode_step_paged", "nnc_decode_beam",
 ]
 
 
@@ -61,6 +64,41 @@ class NncGemmPlan(ctypes.Structure):
                 ("k_slices", ctypes.c_uint32), ("workgroups", ctypes.c_uint32), ("t_comp_us", ctypes.c_double),
                 ("t_mem_us", ctypes.c_double), ("t_us", ctypes.c_double), ("candidates", ctypes.c_uint32),
                 ("rejected_by_capacity", ctypes.c_uint32)]
+
+
+class NncPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint32) for n in ("struct_bytes", "dtype", "n_layers", "n_pages", "page_tokens", "n_kv_heads", "head_dim")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class NncPageTable(ctypes.Structure):
+    _fields_ = [("entries", ctypes.c_void_p), ("n_seqs", ctypes.c_uint32), ("max_pages", ctypes.c_uint32)]
+
+
+class NncPageRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_uint32)] + [
+        (n, ctypes.c_int64) for n in ("k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride")] + [
+        ("n", ctypes.c_uint32), ("seq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("seq0", ctypes.c_int32), ("pos0", ctypes.c_int32)]
+
+
+class NncPageQuery(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("dtype", ctypes.c_uint32), ("n_q_heads", ctypes.c_uint32)] + [
+        (n, ctypes.c_int64) for n in ("q_row_stride", "q_head_stride", "out_row_stride", "out_head_stride")] + [
+        ("lens", ctypes.c_void_p), ("max_len", ctypes.c_uint32), ("window", ctypes.c_uint32), ("scale", ctypes.c_float)]
+
+
+class NncBeam(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_uint32), ("row_stride", ctypes.c_int64), ("n_groups", ctypes.c_uint32),
+                ("width", ctypes.c_uint32), ("vocab", ctypes.c_uint32), ("scores", ctypes.c_void_p), ("finished", ctypes.c_void_p),
+                ("eos", ctypes.c_int32), ("tokens_out", ctypes.c_void_p), ("parents_out", ctypes.c_void_p),
+                ("scores_out", ctypes.c_void_p), ("finished_out", ctypes.c_void_p)]
+
+
+class NncBeamRun(ctypes.Structure):
+    _fields_ = [("tables", ctypes.c_void_p), ("max_pages", ctypes.c_uint32), ("n_groups", ctypes.c_uint32), ("width", ctypes.c_uint32),
+                ("lens", ctypes.c_void_p), ("max_len", ctypes.c_uint32), ("first_logits", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+                ("eos", ctypes.c_int32), ("n_steps", ctypes.c_uint32), ("tokens_out", ctypes.c_void_p), ("parents_out", ctypes.c_void_p),
+                ("scores", ctypes.c_void_p), ("finished", ctypes.c_void_p)]
 
 
 class NncError(RuntimeError):
@@ -106,6 +144,16 @@ def lib():
             "nnc_last_error": (ctypes.c_char_p, []),
             "nnc_plan_prefill_gemm_query": (i32, [u32, u32, u32, u32, u32, u32, u32, P(NncGemmPlan)]),
             "nnc_plan_skinny_gemm_query": (i32, [u32, u32, u32, u32, u32, u32, u32, P(NncGemmPlan)]),
+            "nnc_page_append": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageRows), vp]),
+            "nnc_page_read": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageRows), vp]),
+            "nnc_page_attention_workspace": (i32, [P(NncPages), P(NncPageTable), P(NncPageQuery), P(ctypes.c_size_t)]),
+            "nnc_page_attention": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageQuery), vp, ctypes.c_size_t, vp]),
+            "nnc_page_reorder": (i32, [P(NncPages), P(NncPageTable), vp, vp, vp, u32, vp]),
+            "nnc_beam_select_workspace": (i32, [P(NncBeam), P(ctypes.c_size_t)]),
+            "nnc_beam_select": (i32, [P(NncBeam), vp, ctypes.c_size_t, vp]),
+            "nnc_pages_store": (i32, [vp, P(NncPages), P(NncPageTable), u32, u32, u32, u32]),
+            "nnc_decode_step_paged": (i32, [vp, P(NncPages), P(NncPageTable), vp, u32, vp, vp, vp]),
+            "nnc_decode_beam": (i32, [vp, P(NncPages), P(NncBeamRun)]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -154,6 +202,219 @@ def _i32(a):
 
 def _u32(a):
     return np.ascontiguousarray(a, dtype=np.uint32)
+
+
+# ---- paged KV cache and beam selection -------------------------------------------------------
+
+def _bad(message: str):
+    raise NncError(E_ARG, message)
+
+
+def _dtype_of(t):
+    import torch
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    return _bad(f"{t.dtype} is not one of float32, bfloat16, float16") if code is None else code
+
+
+def _on(device, dtype, shape, **tensors):
+    """Tensors of one device, type and shape, contiguous (None is skipped)."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            _bad(f"{name}: contiguous {dtype} {list(shape)} on {device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _Here:
+    """The device of a call made current for its time; `.stream` is the caller's current stream of that device."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = torch.cuda.device(device)
+        self.cuda, self.device = torch.cuda, device
+
+    def __enter__(self):
+        self.guard.__enter__()
+        self.stream = self.cuda.current_stream(self.device).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+class Pages:
+    """A paged KV cache: the tensors of a pool and the operators on it.
+
+    k, v: [layers, pages, kv heads, positions of a page, head_dim] of float32, bfloat16, float16, int8 or float8_e4m3fn;
+    k_scale, v_scale: float32 [layers, pages, kv heads, positions of a page] for the last two.  The tensors are kept, not
+    copied.  A table is an int32 tensor [sequences, pages of a sequence].  Calls run on the caller's current stream of the
+    pool's device; outputs and workspaces are allocated for that stream."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        self.torch = torch
+        code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int8: I8, torch.float8_e4m3fn: E4M3}.get(k.dtype)
+        if code is None or k.dim() != 5:
+            _bad(f"k: a pool of five dimensions in float32, bfloat16, float16, int8 or float8_e4m3fn expected, not {k.dtype} {list(k.shape)}")
+        if k.device.type != "cuda":
+            _bad("k: device memory expected")
+        _on(k.device, k.dtype, k.shape, k=k, v=v)
+        _on(k.device, torch.float32, k.shape[:-1], k_scale=k_scale, v_scale=v_scale)
+        if (code in (I8, E4M3)) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            _bad("k_scale and v_scale go with int8 and float8_e4m3fn, and only with those")
+        self.k, self.v, self.k_scale, self.v_scale, self.dtype, self.device = k, v, k_scale, v_scale, code, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.desc = NncPages(ctypes.sizeof(NncPages), code, self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim,
+                             k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale))
+
+    @classmethod
+    def empty(cls, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, dtype, device: str = "cuda:0"):
+        """A pool of its own memory; dtype: a torch type of those above."""
+        import torch
+        shape = (n_layers, n_pages, n_kv_heads, page_tokens, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        scales = [torch.empty(shape[:-1], dtype=torch.float32, device=device) if dtype in (torch.int8, torch.float8_e4m3fn) else None for _ in range(2)]
+        return cls(k, v, *scales)
+
+    def _table(self, tables, name="tables"):
+        if tables.dim() != 2:
+            _bad(f"{name}: [sequences, pages] expected")
+        _on(self.device, self.torch.int32, tables.shape, **{name: tables})
+        return NncPageTable(tables.data_ptr() if tables.numel() else None, tables.shape[0], tables.shape[1])
+
+    def _rows(self, k, v, seq, pos):
+        rows = NncPageRows()
+        some = k if k is not None else v
+        if some is None:
+            _bad("k and v are both None")
+        for t in (k, v):
+            if t is None:
+                continue
+            if t.dim() != 3 or tuple(t.shape) != (some.shape[0], self.n_kv_heads, self.head_dim) or t.dtype != some.dtype or t.device != self.device:
+                _bad(f"rows: [rows, {self.n_kv_heads}, {self.head_dim}] of one type on {self.device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
+            if t.shape[0] and t.stride(2) != 1:
+                _bad("rows: the elements of a head must lie next to each other")
+        rows.n, rows.dtype = some.shape[0], _dtype_of(some)
+        if k is not None:
+            rows.k, rows.k_row_stride, rows.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
+        if v is not None:
+            rows.v, rows.v_row_stride, rows.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
+        for name, x in (("seq", seq), ("pos", pos)):
+            if isinstance(x, self.torch.Tensor):
+                _on(self.device, self.torch.int32, (rows.n,), **{name: x})
+                setattr(rows, name, x.data_ptr())
+            else:
+                setattr(rows, name + "0", int(x))
+        return rows
+
+    def append(self, layer: int, k, v, tables, seq, pos):
+        """Write rows [n, kv heads, head_dim] (any strides between rows and heads) as positions `pos` of sequences `seq`: int32
+        tensors [n], or one number: the sequence of all rows, the position of the first.  Negative positions are padding."""
+        if k is None or v is None:
+            _bad("rows: k or v is None")
+        rows, table = self._rows(k, v, seq, pos), self._table(tables)
+        with _Here(self.device) as here:
+            _check(lib().nnc_page_append(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(rows), here.stream))
+
+    def read(self, layer: int, tables, seq, pos, dtype=None, n: int | None = None, k=None, v=None):
+        """Rows (k, v) [n, kv heads, head_dim] of the named positions, in `dtype` (float32).  n: with two numbers for seq and
+        pos, how many.  k, v: tensors to write into instead of new ones (one of them: only that is read)."""
+        if k is None and v is None:
+            if n is None:
+                n = next((x.shape[0] for x in (seq, pos) if isinstance(x, self.torch.Tensor)), None)
+                if n is None:
+                    _bad("read: n is missing")
+            k, v = (self.torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype or self.torch.float32, device=self.device) for _ in range(2))
+        rows, table = self._rows(k, v, seq, pos), self._table(tables)
+        with _Here(self.device) as here:
+            _check(lib().nnc_page_read(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(rows), here.stream))
+        return k, v
+
+    def _query(self, q, tables, lens, max_len, scale, window, out):
+        if q.dim() != 3 or q.shape[0] != tables.shape[0] or q.shape[2] != self.head_dim or q.device != self.device:
+            _bad(f"q: [{tables.shape[0]}, query heads, {self.head_dim}] on {self.device} expected, not {list(q.shape)} on {q.device}")
+        if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
+            _bad("out: shape and type of q expected")
+        for t in (q, out):
+            if t is not None and t.numel() and t.stride(2) != 1:
+                _bad("q, out: the elements of a head must lie next to each other")
+        _on(self.device, self.torch.int32, (q.shape[0],), lens=lens)
+        return NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), q.shape[1], q.stride(0), q.stride(1), out.stride(0) if out is not None else 0,
+                            out.stride(1) if out is not None else 0, lens.data_ptr(), max_len, window,
+                            self.head_dim ** -0.5 if scale is None else scale)
+
+    def attention_workspace(self, q, tables, lens, max_len: int = 0, window: int = 0) -> int:
+        """Bytes of workspace of the same call of `attention`."""
+        n = ctypes.c_size_t()
+        query, table = self._query(q, tables, lens, max_len, None, window, None), self._table(tables)
+        _check(lib().nnc_page_attention_workspace(ctypes.byref(self.desc), ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
+        return n.value
+
+    def attention(self, layer: int, q, tables, lens, max_len: int = 0, scale: float | None = None, window: int = 0, out=None, workspace=None):
+        """One query row per sequence, q [sequences, query heads, head_dim], against the first lens[i] (int32) cached positions
+        of each; max_len: an upper bound of lens (0: what the table holds); scale: 1 / sqrt(head_dim) unless given; window: only
+        that many last positions (0: all).  workspace: a tensor of attention_workspace bytes instead of a new one."""
+        if out is None:
+            out = self.torch.empty_like(q, memory_format=self.torch.contiguous_format)
+        query, table = self._query(q, tables, lens, max_len, scale, window, out), self._table(tables)
+        with _Here(self.device) as here:
+            if workspace is None:
+                n = ctypes.c_size_t()
+                _check(lib().nnc_page_attention_workspace(ctypes.byref(self.desc), ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
+                workspace = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device) if n.value else None
+            elif workspace.device != self.device or not workspace.is_contiguous():
+                _bad("workspace: contiguous memory of the pool's device expected")
+            size = workspace.numel() * workspace.element_size() if workspace is not None else 0
+            _check(lib().nnc_page_attention(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size, here.stream))
+        return out
+
+    def reorder(self, before, after, lens, parents):
+        """Beams take over the cache of their parents: tables before and after [groups * width, pages] (may be one tensor), lens
+        [groups * width], parents [groups, width], all int32."""
+        if parents.dim() != 2:
+            _bad("parents: [groups, width] expected")
+        table = self._table(before, "before")
+        _on(self.device, self.torch.int32, before.shape, after=after)
+        _on(self.device, self.torch.int32, (before.shape[0],), lens=lens)
+        _on(self.device, self.torch.int32, parents.shape, parents=parents)
+        if parents.numel() != before.shape[0]:
+            _bad(f"parents: {before.shape[0]} beams expected, not {list(parents.shape)}")
+        with _Here(self.device) as here:
+            _check(lib().nnc_page_reorder(ctypes.byref(self.desc), ctypes.byref(table), after.data_ptr(), lens.data_ptr(), parents.data_ptr(),
+                                          parents.shape[1], here.stream))
+
+
+def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
+    """The best continuations of every group of beams (nnc_beam_select): logits [groups, width, vocab] (float32, bfloat16,
+    float16), scores [groups, width] float32, finished [groups, width] bool or None, eos: the token that ends a beam (-1: none).
+    Returns tokens, parents (int32), scores, finished, each [groups, width], best first."""
+    import torch
+    if logits.dim() != 3 or logits.device.type != "cuda":
+        _bad("logits: [groups, width, vocab] in device memory expected")
+    g, w, v = logits.shape
+    if logits.numel() and (logits.stride(2) != 1 or (g > 1 and logits.stride(0) != w * logits.stride(1))):
+        _bad("logits: rows of adjacent elements, one distance between all rows, expected")
+    _on(logits.device, torch.float32, (g, w), scores=scores)
+    if finished is not None and finished.dtype != torch.bool:
+        _bad("finished: bool expected")
+    _on(logits.device, torch.bool, (g, w), finished=finished)
+    with _Here(logits.device) as here:
+        tokens, parents = (torch.empty((g, w), dtype=torch.int32, device=logits.device) for _ in range(2))
+        out, ended = torch.empty_like(scores), torch.empty((g, w), dtype=torch.bool, device=logits.device)
+        beam = NncBeam(logits.data_ptr(), _dtype_of(logits), logits.stride(1), g, w, v, scores.data_ptr(), _ptr(finished), eos, tokens.data_ptr(),
+                       parents.data_ptr(), out.data_ptr(), ended.data_ptr())
+        if workspace is None:
+            n = ctypes.c_size_t()
+            _check(lib().nnc_beam_select_workspace(ctypes.byref(beam), ctypes.byref(n)))
+            workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+        elif workspace.device != logits.device or not workspace.is_contiguous():
+            _bad("workspace: contiguous memory of the logits' device expected")
+        _check(lib().nnc_beam_select(ctypes.byref(beam), _ptr(workspace), workspace.numel() * workspace.element_size(), here.stream))
+    return tokens, parents, out, ended
 
 
 class Model:
@@ -315,6 +576,63 @@ class Model:
         if x.dim() == 1:
             x = x[None]
         return x
+
+    # -- pages --------------------------------------------------------------------------
+    def pages_store(self, pages: Pages, tables, seq: int, slot: int, pos0: int = 0, n: int | None = None):
+        """Positions pos0 .. pos0 + n - 1 (to the slot's end) of a slot's cache to the same positions of a sequence in pages."""
+        n = self.slot_len(slot) - pos0 if n is None else n
+        table = pages._table(tables)
+        self._before()
+        try:
+            _check(lib().nnc_pages_store(self.h, ctypes.byref(pages.desc), ctypes.byref(table), seq, slot, pos0, n))
+        finally:
+            self._after()
+
+    def decode_step_paged(self, pages: Pages, tables, lens, tokens, max_len: int = 0, want_logits: bool = True):
+        """nnc_decode_step_paged: lens and tokens are int32 tensors [sequences]; lens grow by one."""
+        table = pages._table(tables)
+        b = tables.shape[0]
+        _on(pages.device, self.torch.int32, (b,), lens=lens, tokens=tokens)
+        logits = self._empty((b, self.V), self.torch.float32) if want_logits else None
+        nxt = self._empty((b,), self.torch.int32)
+        self._before()
+        try:
+            _check(lib().nnc_decode_step_paged(self.h, ctypes.byref(pages.desc), ctypes.byref(table), lens.data_ptr(), max_len, tokens.data_ptr(),
+                                               _ptr(logits), nxt.data_ptr()))
+        finally:
+            self._after()
+        return logits, nxt
+
+    def decode_beam(self, pages: Pages, tables, lens, n_steps: int, first_logits=None, tokens=None, scores=None, finished=None, width: int | None = None,
+                    eos: int = -1, max_len: int = 0):
+        """nnc_decode_beam.  Begin: first_logits [groups, vocab] and width.  Go on: tokens, scores, finished [groups, width] of the
+        call before.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
+        torch, beams = self.torch, tables.shape[0]
+        table = pages._table(tables)
+        if first_logits is not None:
+            groups = first_logits.shape[0]
+            if width is None or groups * width != beams:
+                _bad(f"{beams} sequences are not {groups} groups of {width} beams")
+            _on(pages.device, torch.float32, (groups, self.V), first_logits=first_logits)
+            scores, finished = self._empty((groups, width), torch.float32), self._empty((groups, width), torch.bool)
+        else:
+            if tokens is None or scores is None or finished is None or scores.dim() != 2 or scores.numel() != beams:
+                _bad("first_logits, or tokens, scores and finished [groups, width] expected")
+            groups, width = scores.shape
+            _on(pages.device, torch.int32, scores.shape, tokens=tokens)
+            _on(pages.device, torch.float32, scores.shape, scores=scores)
+            _on(pages.device, torch.bool, scores.shape, finished=finished)
+            scores, finished = scores.clone(), finished.clone()
+        _on(pages.device, torch.int32, (beams,), lens=lens)
+        out, parents = (self._empty((n_steps, groups, width), torch.int32) for _ in range(2))
+        run = NncBeamRun(tables.data_ptr(), table.max_pages, groups, width, lens.data_ptr(), max_len, _ptr(first_logits), _ptr(tokens), eos, n_steps,
+                         out.data_ptr(), parents.data_ptr(), scores.data_ptr(), finished.data_ptr())
+        self._before()
+        try:
+            _check(lib().nnc_decode_beam(self.h, ctypes.byref(pages.desc), ctypes.byref(run)))
+        finally:
+            self._after()
+        return out, parents, scores, finished
 
     # -- state ------------------------------------------------------------------------
     def kv_reset(self, slot: int = -1):

@@ -21,21 +21,26 @@
 
 #include "../../include/nnc.h"
 #include "nnc_internal.h"
+#include "nnc_ops.h"
 #include "nnc_plan.h"
 
 using namespace nnc;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-nnc_status fail(nnc_status st, const char* fmt, ...) {
+nnc_status nnc::fail(nnc_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof g_err, fmt, ap);
   va_end(ap);
   return st;
 }
+
+nnc_status nnc::dev_fail(hipError_t e, const char* what) {
+  return fail(e == hipErrorOutOfMemory ? NNC_E_NOMEM : NNC_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+namespace {
 
 struct LayerW {
   float *g_in = nullptr, *g_q = nullptr, *g_k = nullptr, *g_post = nullptr;
@@ -54,11 +59,13 @@ struct ProfRec {
 // One family per kernel; the skinny GEMM is split by the matrix it streams (same kernel, very
 // different sizes), the reader adds what it wants.
 enum Family { FAM_GEMM = 0, FAM_NORM, FAM_QKROPE, FAM_ATTN, FAM_COMBINE, FAM_EMBED, FAM_ARGMAX, FAM_MISC, FAM_PGEMM, FAM_PATTN,
-              FAM_GEMM_O, FAM_GEMM_GU, FAM_GEMM_D, FAM_GEMM_HEAD, FAM_PGEMM_O, FAM_PGEMM_GU, FAM_PGEMM_D, FAM_COUNT };
+              FAM_GEMM_O, FAM_GEMM_GU, FAM_GEMM_D, FAM_GEMM_HEAD, FAM_PGEMM_O, FAM_PGEMM_GU, FAM_PGEMM_D, FAM_PAGE_ATTN, FAM_PAGE_ROWS,
+              FAM_BEAM, FAM_COUNT };
 const char* const kFamName[FAM_COUNT] = {"gemm_skinny.qkv", "rmsnorm_pack", "qknorm_rope_append", "attn_partial",
                                          "attn_combine", "embed", "argmax", "misc", "gemm_prefill.qkv", "attn_prefill",
                                          "gemm_skinny.o", "gemm_skinny.gate_up", "gemm_skinny.down", "gemm_skinny.lm_head",
-                                         "gemm_prefill.o", "gemm_prefill.gate_up", "gemm_prefill.down"};
+                                         "gemm_prefill.o", "gemm_prefill.gate_up", "gemm_prefill.down", "page_attention",
+                                         "page_rows", "beam"};
 
 }  // namespace
 
@@ -212,10 +219,6 @@ uint64_t blob_bytes_of(const nnc_config* c) {
     if (!c->tied_lm_head) total += w * V * H;
   }
   return total;
-}
-
-nnc_status dev_fail(hipError_t e, const char* what) {
-  return fail(e == hipErrorOutOfMemory ? NNC_E_NOMEM : NNC_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
 #define HIP_TRY(call)                                      \
@@ -425,6 +428,9 @@ struct Pass {
   bool one_slot = false;    // the columns are consecutive positions of one slot (prompt chunk)
   bool begun = false;       // hidden-state steps: x, the columns' state and the first layer's operand are there already
   int* pending_out = nullptr;  // hidden-state models: leave the last projection's partials unadded and say how many
+  const nnc_pages* pages = nullptr;  // the cache is these pages (table, max_len) instead of the slots
+  PageTable table{};
+  uint32_t max_len = 0;     // cached positions of the longest sequence, the new one among them
   bool decode = false;      // every column is a different slot: QK-norm, RoPE and the cache append may run inside the attention kernel
 };
 
@@ -470,7 +476,7 @@ nnc_status run_pass(nnc_model* m, const Pass& p) {
       RUN(FAM_NORM, n * H * 8.0, 0,
           launch_rmsnorm_pack(s, dt, m->x, H, m->rpart, pending, pstride, L.g_in, H, c.rms_eps, n, m->Xp, nc, ns));
     normed = false;
-    const bool fuse = p.decode && m->opt_fuse_qk && attn_partial_can_fuse(dt, nq, nkv);
+    const bool fuse = p.decode && !p.pages && m->opt_fuse_qk && attn_partial_can_fuse(dt, nq, nkv);
     int qkv_slices = 1;
     {
       GemmArgs a{};
@@ -482,19 +488,33 @@ nnc_status run_pass(nnc_model* m, const Pass& p) {
       qkv_slices = (KTH + a.kts_per_split - 1) / a.kts_per_split;
       RUN(FAM_GEMM, (double)Nqkv * H * w, 2.0 * Nqkv * H * n, launch_gemm(s, dt, EPI_STORE, a));
     }
-    const AttnFuseArgs fz{L.g_q, L.g_k, c.rms_eps, m->rope, qkv_slices, (long)n * Nqkv};
-    if (!fuse)
-      RUN(FAM_QKROPE, n * Nqkv * 4.0, 0,
-          launch_qknorm_rope_append(s, dt, m->qkv, nq, nkv, L.g_q, L.g_k, c.rms_eps, m->rope, cm, n,
-                                    L.kc, L.vc, c.max_batch, c.max_seq, m->qsplit));
-    // (fp32 attention over one chunk writes the operand of the output projection itself)
-    const bool direct = m->f32 && p.grid_chunks == 1;
-    RUN(FAM_ATTN, p.kv_rows * 2.0 * Dkv * hw, p.kv_rows * 4.0 * Dq,
-        launch_attn_partial(s, dt, m->qkv, m->qsplit, nq, nkv, L.kc, L.vc, c.max_batch, c.max_seq, cm, n,
-                            p.grid_chunks, m->partial, m->max_chunks, fuse ? &fz : nullptr, p.one_slot,
-                            direct ? m->Ap : nullptr, nc, ns));
-    if (!direct) RUN(FAM_COMBINE, 0, 0,
-        launch_attn_combine(s, dt, m->partial, m->max_chunks, nq, cm, n, m->Ap, nc, ns));
+    if (p.pages) {
+      const PagePool pool = pool_layer(p.pages, li);
+      RUN(FAM_QKROPE, n * Nqkv * 4.0, 0, launch_qknorm_rope_page(s, m->qkv, nq, nkv, L.g_q, L.g_k, c.rms_eps, m->rope, m->st, n, pool, p.table));
+      PageAttn a{};
+      a.q = m->qkv; a.q_dtype = DT_F32; a.q_row = Nqkv; a.q_head = 128; a.n_q_heads = nq;
+      a.lens = reinterpret_cast<const int32_t*>(m->st->pos); a.len_add = 1; a.max_len = p.max_len;
+      a.scale = 0.08838834764831845f;
+      a.packed = m->Ap; a.pk_dt = dt; a.NC = nc; a.nsplit = ns;
+      // (the workspace holds max_chunks records of 132 words for each of MAX_COLS columns and query head)
+      const PageAttnPlan plan = plan_page_attention(pool, (uint32_t)n, a, (uint32_t)(MAX_COLS * m->max_chunks / n));
+      RUN(FAM_PAGE_ATTN, p.kv_rows * 2.0 * Dkv * page_elem_bytes(pool.store), p.kv_rows * 4.0 * Dq,
+          launch_page_attention(s, pool, p.table, a, plan, m->partial));
+    } else {
+      const AttnFuseArgs fz{L.g_q, L.g_k, c.rms_eps, m->rope, qkv_slices, (long)n * Nqkv};
+      if (!fuse)
+        RUN(FAM_QKROPE, n * Nqkv * 4.0, 0,
+            launch_qknorm_rope_append(s, dt, m->qkv, nq, nkv, L.g_q, L.g_k, c.rms_eps, m->rope, cm, n,
+                                      L.kc, L.vc, c.max_batch, c.max_seq, m->qsplit));
+      // (fp32 attention over one chunk writes the operand of the output projection itself)
+      const bool direct = m->f32 && p.grid_chunks == 1;
+      RUN(FAM_ATTN, p.kv_rows * 2.0 * Dkv * hw, p.kv_rows * 4.0 * Dq,
+          launch_attn_partial(s, dt, m->qkv, m->qsplit, nq, nkv, L.kc, L.vc, c.max_batch, c.max_seq, cm, n,
+                              p.grid_chunks, m->partial, m->max_chunks, fuse ? &fz : nullptr, p.one_slot,
+                              direct ? m->Ap : nullptr, nc, ns));
+      if (!direct) RUN(FAM_COMBINE, 0, 0,
+          launch_attn_combine(s, dt, m->partial, m->max_chunks, nq, cm, n, m->Ap, nc, ns));
+    }
     {
       GemmArgs a{};
       a.Wp = L.wo; a.wscale = L.so; a.n_tiles = H / 16; a.KT = KTQ; a.kts_per_split = pick_kts(a.n_tiles, KTQ);
@@ -1919,6 +1939,143 @@ nnc_status nnc_decode_step_hidden(nnc_model* m, const uint32_t* slots, const flo
   }
   HIP_TRY(launch_fold_residual(m->stream, m->x, m->rpart, pending, (long)batch * m->H(), y, (size_t)batch * m->H()));
   for (uint32_t i = 0; i < batch; ++i) m->len[slots[i]] += 1;
+  return fetch_tail_flag(m);
+}
+
+// ---- a model on pages --------------------------------------------------------------
+
+namespace {
+
+nnc_status check_model_pages(const nnc_model* m, const nnc_pages* pages) {
+  if (nnc_status st = check_pages(pages)) return st;
+  if (pages->n_layers != m->c.n_layers || pages->n_kv_heads != m->c.n_kv_heads || pages->head_dim != m->c.head_dim)
+    return fail(NNC_E_ARG, "pages of %u layers x %u kv heads x %u; the model has %u x %u x %u", pages->n_layers, pages->n_kv_heads,
+                pages->head_dim, m->c.n_layers, m->c.n_kv_heads, m->c.head_dim);
+  return NNC_OK;
+}
+
+// Positions a sequence may have: what its table and the rotary table hold.  NNC_E_KV_FULL if that is less than max_len + more.
+nnc_status paged_room(const nnc_model* m, const nnc_pages* pages, uint32_t max_pages, uint32_t max_len, uint32_t more, uint32_t* room) {
+  *room = (uint32_t)std::min<uint64_t>((uint64_t)max_pages * pages->page_tokens, m->c.max_seq);
+  if ((uint64_t)max_len + more > *room)
+    return fail(NNC_E_KV_FULL, "%u + %u positions exceed %u (%u pages of %u, max_seq %u)", max_len, more, *room, max_pages,
+                pages->page_tokens, m->c.max_seq);
+  return NNC_OK;
+}
+
+nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& table, int32_t* lens, uint32_t max_len, const int32_t* tokens,
+                      float* logits, int32_t* next) {
+  const uint32_t n = table.n_seqs;
+  HIP_TRY(launch_paged_state(m->stream, m->st, (int)n, tokens, lens, m->V(), max_len));
+  Pass p;
+  p.decode = true;
+  p.pages = pages;
+  p.table = table;
+  p.max_len = max_len + 1;
+  p.kv_rows = (double)n * p.max_len;
+  p.ncols = (int)n;
+  p.nsplit = decode_nsplit(m, n);
+  p.head_ncols = (int)n;
+  p.logits = logits;
+  p.logits_ld = m->V();
+  p.next = next;
+  return run_pass(m, p);
+}
+
+}  // namespace
+
+nnc_status nnc_pages_store(nnc_model* m, const nnc_pages* pages, const nnc_page_table* table, uint32_t seq, uint32_t slot,
+                           uint32_t pos0, uint32_t n) {
+  if (!m) return fail(NNC_E_ARG, "model is NULL");
+  if (nnc_status st = check_model_pages(m, pages)) return st;
+  if (nnc_status st = check_table(pages, table)) return st;
+  if (seq >= table->n_seqs) return fail(NNC_E_ARG, "sequence %u of %u", seq, table->n_seqs);
+  if (slot >= m->c.max_batch || (uint64_t)pos0 + n > m->len[slot]) return fail(NNC_E_ARG, "slot %u has no positions %u .. + %u", slot, pos0, n);
+  if ((uint64_t)pos0 + n > (uint64_t)table->max_pages * pages->page_tokens)
+    return fail(NNC_E_KV_FULL, "%u positions exceed the table's %u pages of %u", pos0 + n, table->max_pages, pages->page_tokens);
+  if (n == 0) return NNC_OK;
+  const size_t slot_at = ((size_t)slot * m->c.n_kv_heads * m->c.max_seq + pos0) * 128 * m->esz();
+  for (uint32_t li = 0; li < m->c.n_layers; ++li) {
+    PageRows r{};
+    r.k = static_cast<char*>(m->L[li].kc) + slot_at;
+    r.v = static_cast<char*>(m->L[li].vc) + slot_at;
+    r.dtype = m->dt;
+    r.k_row = r.v_row = 128;
+    r.k_head = r.v_head = (int64_t)m->c.max_seq * 128;
+    r.n = n;
+    r.seq0 = (int32_t)seq;
+    r.pos0 = (int32_t)pos0;
+    RUN(FAM_PAGE_ROWS, (double)n * 2 * m->Dkv() * (m->esz() + page_elem_bytes((int)pages->dtype)), 0,
+        launch_page_append(m->stream, pool_layer(pages, li), PageTable{table->entries, table->n_seqs, table->max_pages}, r));
+  }
+  return NNC_OK;
+}
+
+nnc_status nnc_decode_step_paged(nnc_model* m, const nnc_pages* pages, const nnc_page_table* table, int32_t* lens, uint32_t max_len,
+                                 const int32_t* tokens, float* logits_out, int32_t* next_out) {
+  if (!m || !lens || !tokens) return fail(NNC_E_ARG, "NULL argument");
+  if (!m->c.has_embed_and_head) return fail(NNC_E_STATE, "model has no embedding");
+  if (resident_failed(m, false))
+    return fail(NNC_E_DEVICE, "an earlier decode launch gave up waiting for its other workgroups; recreate the model");
+  if (nnc_status st = check_model_pages(m, pages)) return st;
+  if (nnc_status st = check_table(pages, table)) return st;
+  if (table->n_seqs == 0 || table->n_seqs > MAX_DECODE_BATCH)
+    return fail(NNC_E_ARG, "%u sequences (1 .. %u)", table->n_seqs, MAX_DECODE_BATCH);
+  uint32_t room = 0;
+  if (nnc_status st = paged_room(m, pages, table->max_pages, max_len, 1, &room)) return st;
+  const uint32_t most = max_len ? max_len : room - 1;
+  if (nnc_status st = paged_step(m, pages, PageTable{table->entries, table->n_seqs, table->max_pages}, lens, most, tokens,
+                                 logits_out ? logits_out : m->logits, next_out ? m->next : nullptr))
+    return st;
+  if (next_out) HIP_TRY(hipMemcpyAsync(next_out, m->next, table->n_seqs * 4, hipMemcpyDeviceToDevice, m->stream));
+  return fetch_tail_flag(m);
+}
+
+nnc_status nnc_decode_beam(nnc_model* m, const nnc_pages* pages, const nnc_beam_run* run) {
+  if (!m || !run) return fail(NNC_E_ARG, "NULL argument");
+  if (!m->c.has_embed_and_head) return fail(NNC_E_STATE, "model has no embedding");
+  if (resident_failed(m, false))
+    return fail(NNC_E_DEVICE, "an earlier decode launch gave up waiting for its other workgroups; recreate the model");
+  if (nnc_status st = check_model_pages(m, pages)) return st;
+  if (nnc_status st = check_beams(run->n_groups, run->width)) return st;
+  const uint32_t n = run->n_groups * run->width;
+  if (n == 0 || n > MAX_DECODE_BATCH) return fail(NNC_E_ARG, "%u beams in all (1 .. %u)", n, MAX_DECODE_BATCH);
+  const nnc_page_table table{run->tables, n, run->max_pages};
+  if (nnc_status st = check_table(pages, &table)) return st;
+  if (!run->lens || !run->tokens_out || !run->parents_out || !run->scores || !run->finished || (!run->first_logits && !run->tokens))
+    return fail(NNC_E_ARG, "NULL buffer");
+  if (run->eos < -1 || (run->eos >= 0 && (uint32_t)run->eos >= m->c.vocab)) return fail(NNC_E_ARG, "end token %d", run->eos);
+  if (run->n_steps == 0) return fail(NNC_E_ARG, "n_steps is 0");
+  const bool begin = run->first_logits != nullptr;
+  const uint32_t passes = run->n_steps - (begin ? 1 : 0);
+  uint32_t room = 0;
+  if (nnc_status st = paged_room(m, pages, run->max_pages, run->max_len, passes, &room)) return st;
+  if (beam_select_bytes(n, run->width, m->V()) > (size_t)MAX_COLS * m->c.n_q_heads * m->max_chunks * 132 * 4)
+    return fail(NNC_E_ARG, "the selection of %u beams out of %u tokens does not fit the workspace", n, m->V());
+  hipStream_t s = m->stream;
+  if (begin) RUN(FAM_BEAM, 0, 0, launch_beam_start(s, run->scores, run->finished, run->n_groups, run->width));
+  BeamSelect b{};
+  b.dtype = DT_F32; b.n_groups = run->n_groups; b.width = run->width; b.vocab = m->V();
+  b.scores = run->scores; b.scores_out = run->scores;
+  b.finished = run->eos >= 0 ? run->finished : nullptr; b.finished_out = run->finished; b.eos = run->eos;
+  for (uint32_t step = 0; step < run->n_steps; ++step) {
+    const bool first = begin && step == 0;
+    if (!first) {
+      const uint32_t done = step - (begin ? 1 : 0);  // passes so far
+      const int32_t* tok = step ? run->tokens_out + (size_t)(step - 1) * n : run->tokens;
+      // (a bound on the lengths that is not known stays the table's)
+      const uint32_t most = run->max_len ? run->max_len + done : room - 1;
+      if (nnc_status st = paged_step(m, pages, PageTable{table.entries, n, table.max_pages}, run->lens, most, tok, m->logits, nullptr)) return st;
+    }
+    // (at the start only beam 0 of a group is in use, the rows of the others are not looked at)
+    b.logits = first ? run->first_logits : m->logits;
+    b.row = first ? 0 : (int64_t)m->V();
+    b.group = first ? (int64_t)m->V() : (int64_t)m->V() * run->width;
+    b.tokens = run->tokens_out + (size_t)step * n;
+    b.parents = run->parents_out + (size_t)step * n;
+    RUN(FAM_BEAM, (double)n * m->V() * 4, 0, launch_beam_select(s, b, m->partial));
+    RUN(FAM_BEAM, 0, 0, launch_page_reorder(s, reorder_of(pages, &table, run->tables, run->lens, b.parents, run->width)));
+  }
   return fetch_tail_flag(m);
 }
 

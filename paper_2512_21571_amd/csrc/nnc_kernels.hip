@@ -8,6 +8,7 @@
 // decoder arithmetic in fp32.
 #include "nnc_half.h"
 #include "nnc_internal.h"
+#include "nnc_pages.h"
 #include "nnc_lanes.h"
 
 namespace nnc {
@@ -182,6 +183,25 @@ hipError_t launch_set_state(hipStream_t s, ColState* st, int ncols, const int32_
   if (!rows) n = 0;
   const unsigned grid = (unsigned)((n + 255) / 256 < 256 ? (n + 255) / 256 : 256);
   k_set_state<<<grid ? grid : 1, n ? 256 : MAX_COLS, 0, s>>>(st, init, ncols, step, rows, x, n);
+  return hipGetLastError();
+}
+
+// The state of a step over pages, from device memory: column i is row i of the page table.
+__global__ __launch_bounds__(MAX_COLS) void k_paged_state(ColState* st, int ncols, const int32_t* __restrict__ tok,
+                                                          int32_t* __restrict__ lens, uint32_t vocab, uint32_t max_pos) {
+  const int i = threadIdx.x;
+  if (i >= ncols) return;
+  const int32_t t = tok[i], n = lens[i];
+  const bool ok = (uint32_t)t < vocab && (uint32_t)n <= max_pos;
+  st->tok[i] = ok ? t : 0;
+  st->slot[i] = (uint32_t)i;
+  st->pos[i] = ok ? (uint32_t)n : (uint32_t)-2;
+  if (ok) lens[i] = n + 1;
+  if (i == 0) st->step = 0;
+}
+
+hipError_t launch_paged_state(hipStream_t s, ColState* st, int ncols, const int32_t* tok, int32_t* lens, uint32_t vocab, uint32_t max_pos) {
+  k_paged_state<<<1, MAX_COLS, 0, s>>>(st, ncols, tok, lens, vocab, max_pos);
   return hipGetLastError();
 }
 
@@ -919,6 +939,61 @@ hipError_t launch_qknorm_rope_append(hipStream_t s, int dt, float* qkv, int nq, 
   if (dt == DT_F32) qs = nullptr;
   NNC_FOR_DTYPE(dt, k_qknorm_rope_append<F32, HF><<<grid, 64, 0, s>>>(qkv, nq, nkv, gq, gk, eps, rope, cm, kc, vc, max_seq, qs,
                                                                        nullptr, 0));
+  return hipGetLastError();
+}
+
+// The same with the K and V rows going into the pages of a paged cache (nnc_pages.h), of whatever stored format.  A column
+// at position -2 (a token or a position that does not exist) is not cached.
+__global__ __launch_bounds__(64) void k_qknorm_rope_page(float* __restrict__ qkv, int nq, const float* __restrict__ gq,
+                                                         const float* __restrict__ gk, float eps, const float2* __restrict__ rope,
+                                                         const ColState* __restrict__ st, PagePool pool, PageTable table) {
+  const int nkv = (int)pool.n_kv_heads, col = blockIdx.y, hh = blockIdx.x, lane = threadIdx.x;
+  float* p = qkv + (size_t)col * (nq + 2 * nkv) * 128 + (size_t)hh * 128;
+  const int32_t pos = (int32_t)st->pos[col];
+  float a = p[lane], b = p[lane + 64];
+  const bool is_v = hh >= nq + nkv;
+  if (!is_v) {
+    const float* gg = hh < nq ? gq : gk;
+    qk_norm_rope(a, b, eps, gg[lane], gg[lane + 64], rope[(size_t)max(pos, 0) * 64 + lane]);
+  }
+  if (hh < nq) {
+    p[lane] = a;
+    p[lane + 64] = b;
+    return;
+  }
+  const uint32_t head = (uint32_t)(is_v ? hh - nq - nkv : hh - nq);
+  const int64_t row = page_row(pool, table, (int32_t)st->slot[col], pos, head);
+  if (row < 0) return;
+  void* dst = is_v ? pool.v : pool.k;
+  if (page_scaled(pool.store)) {
+    uint32_t top = max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    const float scale = page_scale_of(top, pool.store), inv = 1.f / scale;
+    uint32_t w = 0;
+    if (scale == scale) {
+      const float qa = page_quotient(a, scale, inv), qb = page_quotient(b, scale, inv);
+      w = pool.store == PS_I8 ? page_bytes4<PS_I8>(qa, qb, 0.f, 0.f) : page_bytes4<PS_E4M3>(qa, qb, 0.f, 0.f);
+    }
+    uint8_t* d = static_cast<uint8_t*>(dst) + row * 128;
+    d[lane] = (uint8_t)w;
+    d[lane + 64] = (uint8_t)(w >> 8);
+    if (lane == 0) (is_v ? pool.v_scale : pool.k_scale)[row] = scale;
+  } else if (pool.store == PS_F32) {
+    float* d = static_cast<float*>(dst) + row * 128;
+    d[lane] = a;
+    d[lane + 64] = b;
+  } else {
+    uint16_t* d = static_cast<uint16_t*>(dst) + row * 128;
+    d[lane] = (uint16_t)(pool.store == PS_BF16 ? Bf16::bits(a) : Fp16::bits(a));
+    d[lane + 64] = (uint16_t)(pool.store == PS_BF16 ? Bf16::bits(b) : Fp16::bits(b));
+  }
+}
+
+hipError_t launch_qknorm_rope_page(hipStream_t s, float* qkv, int nq, int nkv, const float* gq, const float* gk, float eps,
+                                   const float2* rope, const ColState* st, int ncols, const PagePool& p, const PageTable& t) {
+  if (p.head_dim != 128 || (int)p.n_kv_heads != nkv) return hipErrorInvalidValue;
+  k_qknorm_rope_page<<<dim3(nq + 2 * nkv, ncols), 64, 0, s>>>(qkv, nq, gq, gk, eps, rope, st, p, t);
   return hipGetLastError();
 }
 

@@ -1,0 +1,202 @@
+// Rows into a paged KV cache and out of it, and the pages of beams that follow other beams.  Bound: memory traffic; the
+// arithmetic per value is a conversion.
+#include <type_traits>
+
+#include "nnc_internal.h"
+#include "nnc_pages.h"
+
+namespace nnc {
+
+#define NNC_FOR_STORE(st, ...)                                       \
+  do {                                                               \
+    switch (st) {                                                    \
+      case PS_F32: { constexpr int STORE = PS_F32; __VA_ARGS__; break; }   \
+      case PS_BF16: { constexpr int STORE = PS_BF16; __VA_ARGS__; break; } \
+      case PS_F16: { constexpr int STORE = PS_F16; __VA_ARGS__; break; }   \
+      case PS_I8: { constexpr int STORE = PS_I8; __VA_ARGS__; break; }     \
+      case PS_E4M3: { constexpr int STORE = PS_E4M3; __VA_ARGS__; break; } \
+      default: return hipErrorInvalidValue;                          \
+    }                                                                \
+  } while (0)
+#define NNC_FOR_ROWS(dt, ...)                                        \
+  do {                                                               \
+    switch (dt) {                                                    \
+      case DT_F32: { constexpr int DT = DT_F32; __VA_ARGS__; break; }      \
+      case DT_BF16: { constexpr int DT = DT_BF16; __VA_ARGS__; break; }    \
+      case DT_F16: { constexpr int DT = DT_F16; __VA_ARGS__; break; }      \
+      default: return hipErrorInvalidValue;                          \
+    }                                                                \
+  } while (0)
+
+// Largest of LPR (8 or 16) neighbouring lanes, in all of them.
+template <int LPR>
+__device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
+  auto get = [](uint32_t x, auto ctrl) __attribute__((always_inline)) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR1>{}));
+  v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR2>{}));
+  v = max(v, get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{}));
+  if constexpr (LPR == 16) v = max(v, get(v, std::integral_constant<int, DPP_ROW_MIRROR>{}));
+  return v;
+}
+
+// Eight values per thread, head_dim / 8 neighbouring threads per (row, kv head), K in blockIdx.y 0 and V in 1.
+template <int STORE, int DT, int LPR>
+__global__ __launch_bounds__(256) void k_page_append(PagePool p, PageTable t, PageRows r, bool wide) {
+  const uint32_t id = (blockIdx.x * 256u + threadIdx.x) / LPR;
+  const int lane = threadIdx.x % LPR;
+  const uint32_t row = id / p.n_kv_heads, head = id - row * p.n_kv_heads;
+  if (row >= r.n) return;
+  const bool is_v = blockIdx.y;
+  const int64_t at = page_row(p, t, r.seq ? r.seq[row] : r.seq0, r.pos ? r.pos[row] : r.pos0 + (int32_t)row, head);
+  if (at < 0) return;
+  float x[8];
+  load8<DT>(is_v ? r.v : r.k, (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8, wide, x);
+  void* pool = is_v ? p.v : p.k;
+  const int64_t e = at * (LPR * 8) + lane * 8;
+  if constexpr (page_scaled(STORE)) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    const float scale = page_scale_of(lanes_umax<LPR>(top), STORE);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + e) = page_bytes8<STORE>(x, scale);
+    if (lane == 0) (is_v ? p.v_scale : p.k_scale)[at] = scale;
+  } else {
+    store8<STORE>(pool, e, true, x);
+  }
+}
+
+template <int STORE, int DT, int LPR>
+__global__ __launch_bounds__(256) void k_page_read(PagePool p, PageTable t, PageRows r, bool wide) {
+  const uint32_t id = (blockIdx.x * 256u + threadIdx.x) / LPR;
+  const int lane = threadIdx.x % LPR;
+  const uint32_t row = id / p.n_kv_heads, head = id - row * p.n_kv_heads;
+  if (row >= r.n) return;
+  const bool is_v = blockIdx.y;
+  void* out = is_v ? r.v : r.k;
+  if (!out) return;
+  const int64_t at = page_row(p, t, r.seq ? r.seq[row] : r.seq0, r.pos ? r.pos[row] : r.pos0 + (int32_t)row, head);
+  float x[8];
+  if (at < 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7fc00000u);
+  } else {
+    const void* pool = is_v ? p.v : p.k;
+    const int64_t e = at * (LPR * 8) + lane * 8;
+    if constexpr (page_scaled(STORE)) {
+      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + e);
+      const float scale = (is_v ? p.v_scale : p.k_scale)[at];
+      page_widen4<STORE>(w.x, x);
+      page_widen4<STORE>(w.y, x + 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= scale;
+    } else {
+      load8<STORE>(pool, e, true, x);
+    }
+  }
+  store8<DT>(out, (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8, wide, x);
+}
+
+// Whether eight elements of every row can be moved sixteen bytes at a time.
+static bool rows_wide(const PageRows& r) {
+  const int64_t per16 = r.dtype == DT_F32 ? 4 : 8;
+  auto ok = [&](const void* p, int64_t a, int64_t b) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && a % per16 == 0 && b % per16 == 0); };
+  return ok(r.k, r.k_row, r.k_head) && ok(r.v, r.v_row, r.v_head);
+}
+
+#define NNC_PAGE_ROWS_LAUNCH(kernel)                                                                                   \
+  const uint64_t threads = (uint64_t)r.n * p.n_kv_heads * (p.head_dim / 8);                                            \
+  if (threads == 0) return hipSuccess;                                                                                 \
+  if (threads > 0xffffff00ull || (p.head_dim != 64 && p.head_dim != 128)) return hipErrorInvalidValue;                 \
+  const dim3 grid((unsigned)((threads + 255) / 256), 2);                                                               \
+  const bool wide = rows_wide(r);                                                                                      \
+  NNC_FOR_STORE(p.store, NNC_FOR_ROWS(r.dtype, if (p.head_dim == 128) kernel<STORE, DT, 16><<<grid, 256, 0, s>>>(p, t, r, wide); \
+                                      else kernel<STORE, DT, 8><<<grid, 256, 0, s>>>(p, t, r, wide)));                 \
+  return hipGetLastError()
+
+hipError_t launch_page_append(hipStream_t s, const PagePool& p, const PageTable& t, const PageRows& r) { NNC_PAGE_ROWS_LAUNCH(k_page_append); }
+hipError_t launch_page_read(hipStream_t s, const PagePool& p, const PageTable& t, const PageRows& r) { NNC_PAGE_ROWS_LAUNCH(k_page_read); }
+
+// ---- beams -------------------------------------------------------------------------------------------------
+// Workgroups 0 .. nt - 1 of a group turn 256 table columns each, the others copy.  `before` and `after` may be the same
+// table and a beam's own page may be another beam's source: every thread loads what all beams need of its column (its 16
+// bytes) before it stores any of it, and no other thread touches that column.
+template <int W>
+__global__ __launch_bounds__(256) void k_page_reorder(PageReorder r, uint32_t nt, uint32_t nchunks) {
+  __shared__ int32_t parent[W], src[W], dst[W];
+  const uint32_t g = blockIdx.y, tid = threadIdx.x;
+  const int32_t* before = r.before + (size_t)g * r.width * r.max_pages;
+  int32_t* after = r.after + (size_t)g * r.width * r.max_pages;
+  const int32_t len = r.lens[(size_t)g * r.width];
+  if (len < 0 || (uint64_t)len > (uint64_t)r.max_pages * r.page_tokens) return;
+  const uint32_t full = fdiv((uint32_t)len, r.by_page), part = (uint32_t)len - full * r.page_tokens;
+  if (tid < r.width) {
+    int32_t p = r.parents[(size_t)g * r.width + tid];
+    if ((uint32_t)p >= r.width) p = (int32_t)tid;  // (a beam without a parent stays as it is)
+    parent[tid] = p;
+    if (part) {
+      src[tid] = before[(size_t)p * r.max_pages + full];
+      dst[tid] = after[(size_t)tid * r.max_pages + full];
+    }
+  }
+  __syncthreads();
+  if (blockIdx.x < nt) {
+    const uint32_t i = blockIdx.x * 256 + tid;
+    if (i >= full) return;
+    int32_t e[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < (int)r.width) e[j] = before[(size_t)parent[j] * r.max_pages + i];
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < (int)r.width) after[(size_t)j * r.max_pages + i] = e[j];
+    return;
+  }
+  if (!part) return;
+  const uint32_t b = blockIdx.x - nt;
+  const uint32_t chunk = b % nchunks, which = b / nchunks % 2, lh = b / nchunks / 2;
+  const uint32_t layer = lh / r.n_kv_heads, head = lh - layer * r.n_kv_heads;
+  auto at = [&](int32_t page) { return (((size_t)layer * r.n_pages + page) * r.n_kv_heads + head) * r.page_tokens; };
+  auto moves = [&](int j) {
+    return j < (int)r.width && src[j] != dst[j] && (uint32_t)src[j] < r.n_pages && (uint32_t)dst[j] < r.n_pages;
+  };
+  const uint32_t bytes = part * r.row_bytes, o = chunk * 4096 + tid * 16;
+  if (o < bytes) {
+    char* base = static_cast<char*>(which ? r.v : r.k);
+    u32x4_v x[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (moves(j)) x[j] = *reinterpret_cast<const u32x4_v*>(base + at(src[j]) * r.row_bytes + o);
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (moves(j)) *reinterpret_cast<u32x4_v*>(base + at(dst[j]) * r.row_bytes + o) = x[j];
+  }
+  if (chunk == 0 && r.k_scale) {
+    float* base = which ? r.v_scale : r.k_scale;
+    for (uint32_t i = tid; i < part; i += 256) {
+      float x[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        if (moves(j)) x[j] = base[at(src[j]) + i];
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        if (moves(j)) base[at(dst[j]) + i] = x[j];
+    }
+  }
+}
+
+hipError_t launch_page_reorder(hipStream_t s, const PageReorder& r) {
+  const uint32_t nt = (r.max_pages + 255) / 256;
+  const uint32_t nchunks = (uint32_t)(((uint64_t)r.page_tokens * r.row_bytes + 4095) / 4096);
+  const uint64_t blocks = nt + (uint64_t)r.n_layers * r.n_kv_heads * 2 * nchunks;
+  if (r.width == 0 || r.width > BEAM_MAX_WIDTH || blocks > 0x7fffffffull || r.n_groups > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks, r.n_groups);
+  if (r.width <= 4) k_page_reorder<4><<<grid, 256, 0, s>>>(r, nt, nchunks);
+  else if (r.width <= 8) k_page_reorder<8><<<grid, 256, 0, s>>>(r, nt, nchunks);
+  else if (r.width <= 16) k_page_reorder<16><<<grid, 256, 0, s>>>(r, nt, nchunks);
+  else k_page_reorder<32><<<grid, 256, 0, s>>>(r, nt, nchunks);
+  return hipGetLastError();
+}
+
+}  // namespace nnc

@@ -1,0 +1,469 @@
+"""The paged KV cache on the GPU against plain 64-bit definitions: append, read, decode attention, beam selection and reordering,
+one by one and as a search uses them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import page_util as pu
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def nnc():
+    from paper_2512_21571_amd import binding
+    binding.lib()
+    return binding
+
+
+def make_pool(nnc, store, layers=1, pages=12, tokens=16, heads=3, dim=128):
+    """Every value a NaN (int8: -128, which is never stored; its scale is one): what is read without having been written shows."""
+    p = nnc.Pages.empty(layers, pages, tokens, heads, dim, pu.STORES[store], DEV)
+    for x in (p.k, p.v):
+        x.view(torch.uint8).fill_(0x80 if store == "i8" else 0xff)
+    for x in (p.k_scale, p.v_scale):
+        if x is not None:
+            x.fill_(math.nan)
+    return p
+
+
+def scattered(rng, n_seqs, per, pages):
+    return torch.from_numpy(rng.permutation(pages)[:n_seqs * per].reshape(n_seqs, per).astype(np.int32)).to(DEV)
+
+
+def raw(p):
+    return [x.view(torch.uint8).clone() if x.element_size() == 1 else x.clone() for x in (p.k, p.v, p.k_scale, p.v_scale) if x is not None]
+
+
+def same_bits(a, b):
+    v = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[a.element_size()]
+    return torch.equal(a.view(v), b.view(v))
+
+
+# ---- append and read -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("store", list(pu.STORES))
+@pytest.mark.parametrize("heads,dim,tokens", [(3, 128, 16), (1, 64, 1), (5, 64, 24), (2, 128, 7)])
+def test_append_and_read_back(nnc, store, rows, heads, dim, tokens):
+    rng = np.random.default_rng(7)
+    n_seqs, per, n = 3, 4 if tokens > 1 else 9, 8
+    p = make_pool(nnc, store, 2, 3 * per + 2, tokens, heads, dim)
+    tables = scattered(rng, n_seqs, per, p.n_pages)
+    cap = per * tokens
+    seq = torch.tensor([0, 0, 1, 2, 2, 1, 0, 2], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([0, cap - 1, min(5, cap - 1), 1, 0, 0, -1, cap], dtype=torch.int32, device=DEV)   # the last two: padding, beyond the table
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    wide = torch.randn((n, heads + 2, dim + 1), generator=gen, device=DEV) * torch.exp(torch.randn((n, heads + 2, 1), generator=gen, device=DEV) * 3)
+    k = wide[:, 1:1 + heads, 1:].to(pu.ROWS[rows])                       # contiguous
+    v = wide.to(pu.ROWS[rows])[:, 2:2 + heads, :dim]                     # rows and heads apart, no alignment but the element's
+    before = raw(p)
+    p.append(1, k, v, tables, seq, pos)
+    values = pu.pool_values(p, 1)
+    kept = np.zeros((p.n_pages, tokens), bool)
+    tb = tables.cpu().numpy()
+    for i in range(6):
+        page, row = tb[int(seq[i]), int(pos[i]) // tokens], int(pos[i]) % tokens
+        kept[page, row] = True
+        for x, pool, scales, val in ((k, p.k, p.k_scale, values[0]), (v, p.v, p.v_scale, values[1])):
+            want = pu.f64(x[i])
+            got = pu.f64(pool.view(torch.uint8)[1, page, :, row].view(pool.dtype)) if store == "e4m3" else pu.f64(pool[1, page, :, row])
+            if store in pu.TOP:
+                q, s = pu.quantise(want, store)
+                assert np.array_equal(got, q)
+                assert np.array_equal(scales[1, page, :, row].cpu().numpy(), s)
+            else:
+                assert torch.equal(pool[1, page, :, row], x[i].to(pool.dtype))
+    # nothing else of the pool has changed
+    untouched = torch.from_numpy(~kept).to(DEV)
+    for a, b in zip(before, raw(p)):
+        assert same_bits(a[0], b[0])
+        assert same_bits(a[1].transpose(1, 2)[untouched].contiguous(), b[1].transpose(1, 2)[untouched].contiguous())
+    # back again: value * scale in fp32, rounded once; missing rows are NaN
+    for t in pu.ROWS.values():
+        rk, rv = p.read(1, tables, seq, pos, dtype=t)
+        for got, pool, scales in ((rk, p.k, p.k_scale), (rv, p.v, p.v_scale)):
+            for i in range(6):
+                page, row = tb[int(seq[i]), int(pos[i]) // tokens], int(pos[i]) % tokens
+                x = (pool.view(torch.uint8)[1, page, :, row].view(pool.dtype) if store == "e4m3" else pool[1, page, :, row]).float()
+                x = x if scales is None else x * scales[1, page, :, row, None]
+                assert torch.equal(got[i], x.to(t))
+            assert got[6:].isnan().all()
+    only = torch.empty((n, heads, dim), device=DEV)
+    a, b = p.read(1, tables, seq, pos, v=only)
+    assert a is None and torch.equal(only[:6], p.read(1, tables, seq, pos)[1][:6])
+
+
+@pytest.mark.parametrize("store", ["i8", "e4m3"])
+def test_quantised_rows_at_the_borders(nnc, store):
+    """Values exactly between two stored ones and one unit of the last place to either side; rows of zeros, of tiny and huge
+    values, of one magnitude; rows with an infinity or a NaN."""
+    top = pu.TOP[store]
+    levels = np.arange(0.5, 127, 1.0) if store == "i8" else (pu.E4M3[1:] + pu.E4M3[:-1]) / 2
+    rows = []
+    for size in (1.0, 0.37, 3.1e-9, 7.7e12, 1.9e-20):
+        s = np.float32(np.float32(size * top) / np.float32(top))
+        for nudge in (-1, 0, 1):
+            x = (levels[:126].astype(np.float64) * float(s)).astype(np.float32)
+            x = np.nextafter(x, np.float32(np.inf if nudge > 0 else -np.inf)) if nudge else x
+            r = np.zeros(128, np.float32)
+            r[:len(x)], r[127] = x, np.float32(size * top)
+            rows += [r, -r]
+    rows += [np.zeros(128), np.full(128, 1e-38), np.full(128, -3e38), np.full(128, 1.4e-45), np.full(128, 0.25), np.full(128, 0.25), np.full(128, 5.0)]
+    x = np.stack(rows).astype(np.float32)
+    x[-3][5], x[-2][77] = np.inf, np.nan
+    n = len(x)
+    p = make_pool(nnc, store, 1, n, 1, 1, 128)
+    tables = torch.arange(n, dtype=torch.int32, device=DEV)[None]
+    t = torch.from_numpy(x).to(DEV)[:, None]
+    p.append(0, t, t, tables, 0, 0)
+    want, scale = pu.quantise(x.astype(np.float64), store)
+    got = pu.f64(p.k.view(torch.uint8).view(p.k.dtype)[0, :, 0, 0] if store == "e4m3" else p.k[0, :, 0, 0])
+    assert np.array_equal(p.k_scale[0, :, 0, 0].cpu().numpy(), scale, equal_nan=True)
+    assert np.array_equal(got, want)
+    rk, rv = p.read(0, tables, 0, 0, n=n)
+    assert rk[-3:-1].isnan().all() and not rk[:-3].isnan().any() and torch.equal(rk[:-3], rv[:-3])
+    assert (rk[-1] == 5.0).all() or store == "i8"
+
+
+def test_pages_and_sequences_that_do_not_exist(nnc):
+    p = make_pool(nnc, "bf16", 1, 4, 16, 2, 64)
+    tables = torch.tensor([[0, 4, -1], [2, 3, 1 << 30]], dtype=torch.int32, device=DEV)
+    x = torch.ones((6, 2, 64), device=DEV)
+    seq = torch.tensor([0, 0, 1, 2, -1, 1], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([16, 40, 47, 0, 0, -(1 << 31)], dtype=torch.int32, device=DEV)
+    before = raw(p)
+    p.append(0, x, x, tables, seq, pos)
+    assert all(same_bits(a, b) for a, b in zip(before, raw(p)))
+    assert p.read(0, tables, seq, pos)[0].isnan().all()
+    p.append(0, x[:0], x[:0], tables, seq[:0], pos[:0])       # no rows
+    assert p.read(0, tables, seq[:0], pos[:0])[0].shape == (0, 2, 64)
+
+
+# ---- attention ------------------------------------------------------------------------------------------------
+
+def fill(nnc, p, tables, lens, seed=1, loud=1.0):
+    """Random rows at positions 0 .. lens[i] - 1 of every sequence, everything else stays what make_pool left."""
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    for i, n in enumerate(lens):
+        if n:
+            k, v = (torch.randn((n, p.n_kv_heads, p.head_dim), generator=gen, device=DEV) * loud for _ in range(2))
+            p.append(p.n_layers - 1, k, v, tables, i, 0)
+
+
+def check_attention(p, q, out, tables, lens, window=0, scale=None):
+    """Against the definition in 64 bits on the cache as stored.  What may differ: an fp32 score of dim products is off by
+    (dim + 8) 2^-24 of the sum of their magnitudes (twice: the weight and the normaliser), a weight carries 2^-17 where the
+    output has 16 bits (its two bf16 pieces) and 2^-23 else, sums of n weights n 2^-24, exponentials 2^-22; then the output is rounded."""
+    rows = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}[q.dtype]
+    k, v = pu.pool_values(p, p.n_layers - 1)
+    t, g = p.page_tokens, q.shape[1] // p.n_kv_heads
+    scale = p.head_dim ** -0.5 if scale is None else scale
+    got, qq = pu.f64(out), pu.f64(q)
+    for i, n in enumerate(lens):
+        lo = max(0, n - window) if window else 0
+        pos = np.arange(lo, n)
+        page = tables[i].cpu().numpy()[pos // t]
+        for h in range(p.n_kv_heads):
+            kk, vv = k[page, h, pos % t], v[page, h, pos % t]
+            want, size = pu.attention(qq[i, h * g:(h + 1) * g], kk, vv, scale)
+            top = np.abs(vv).max() if len(vv) else 0.0
+            rel = 2 * (p.head_dim + 8) * 2.0 ** -24 * size + (2.0 ** -17 if rows != "f32" else 2.0 ** -23) + (len(pos) + 64) * 2.0 ** -24 + 2.0 ** -22
+            err = np.abs(got[i, h * g:(h + 1) * g] - want)
+            tol = 2 * top * rel + pu.HALF_ULP[rows] * (np.abs(want) + 2 * top * rel) + (2.0 ** -25 if rows == "f16" else 0)
+            assert (err <= tol).all(), (i, h, n, float((err - tol).max()), float(err.max()))
+
+
+@pytest.mark.parametrize("store", list(pu.STORES))
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("heads,group,dim,tokens", [(2, 4, 128, 16), (3, 1, 64, 7), (1, 16, 128, 1), (2, 5, 64, 24), (1, 20, 128, 64)])
+def test_attention_of_ragged_lengths(nnc, store, rows, heads, group, dim, tokens):
+    rng = np.random.default_rng(2)
+    lens = [0, 1, tokens, tokens + 1, 33, 100, 2 * tokens + 3]
+    per = -(-max(lens) // tokens)
+    p = make_pool(nnc, store, 1, len(lens) * per + 1, tokens, heads, dim)
+    tables = scattered(rng, len(lens), per, p.n_pages)
+    fill(nnc, p, tables, lens)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    q = (torch.randn((len(lens), heads * group, dim), generator=gen, device=DEV) * 1.5).to(pu.ROWS[rows])
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out = p.attention(0, q, tables, ln)
+    assert (out[0] == 0).all()
+    check_attention(p, q, out, tables, lens)
+    assert torch.equal(out, p.attention(0, q, tables, ln))             # the same call, the same bits
+    check_attention(p, q, p.attention(0, q, tables, ln, max_len=max(lens), window=17), tables, lens, 17)
+    check_attention(p, q, p.attention(0, q, tables, ln, scale=0.03), tables, lens, 0, 0.03)
+
+
+@pytest.mark.parametrize("store,rows", [("bf16", "f32"), ("i8", "bf16"), ("e4m3", "f16"), ("f32", "f32"), ("f16", "f16"), ("i8", "f32")])
+@pytest.mark.parametrize("heads,group,lens", [(1, 4, [5000]), (8, 2, [1, 3000, 700]), (2, 8, [2049, 0, 1, 64, 4095])])
+def test_attention_split_over_long_sequences(nnc, store, rows, heads, group, lens):
+    rng = np.random.default_rng(4)
+    per = -(-max(lens) // 32)
+    p = make_pool(nnc, store, 1, len(lens) * per, 32, heads, 128)
+    tables = scattered(rng, len(lens), per, p.n_pages)
+    fill(nnc, p, tables, lens, loud=2.0)
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    q = (torch.randn((len(lens), heads * group, 128), generator=gen, device=DEV) * 2).to(pu.ROWS[rows])
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    assert p.attention_workspace(q, tables, ln) > 0
+    for window in (0, 1, 1000):
+        check_attention(p, q, p.attention(0, q, tables, ln, window=window), tables, lens, window)
+
+
+def test_attention_one_loud_position_and_infinities(nnc):
+    """A weight of 1 beside weights that vanish; an infinite score (NaN by the definition); -infinity scores (left out, and zeros
+    where nothing is left)."""
+    p = make_pool(nnc, "f32", 1, 4, 64, 1, 128)
+    tables = torch.arange(4, dtype=torch.int32, device=DEV).reshape(4, 1)
+    k = torch.zeros((60, 1, 128), device=DEV)
+    v = torch.randn((60, 1, 128), device=DEV)
+    loud = k.clone()
+    loud[41, 0, 0] = 1e4
+    inf, low, none = k.clone(), k.clone(), k.clone()
+    inf[3, 0, 0], low[:59, 0, 0], none[:, 0, 0] = math.inf, -math.inf, -math.inf
+    for i, x in enumerate((loud, inf, low, none)):
+        p.append(0, x, v, tables, i, 0)
+    q = torch.zeros((4, 1, 128), device=DEV)
+    q[:, :, 0] = 3.0
+    out = p.attention(0, q, tables, torch.full((4,), 60, dtype=torch.int32, device=DEV))
+    assert torch.equal(out[0, 0], v[41, 0])
+    assert out[1].isnan().all()
+    assert torch.equal(out[2, 0], v[59, 0])
+    assert (out[3] == 0).all()
+
+
+@pytest.mark.parametrize("store", ["bf16", "i8"])
+def test_attention_wrong_lengths_and_missing_pages_are_nan(nnc, store):
+    p = make_pool(nnc, store, 1, 40, 16, 2, 128)
+    tables = torch.arange(40, dtype=torch.int32, device=DEV).reshape(5, 8)
+    fill(nnc, p, tables, [128] * 5)
+    tables[3, 2] = 40
+    tables[4, 7] = -1
+    q = torch.randn((5, 4, 128), device=DEV)
+    out = p.attention(0, q, tables, torch.tensor([-1, 129, 128, 100, 112], dtype=torch.int32, device=DEV))
+    assert [bool(x.isnan().all()) for x in out] == [True, True, False, True, False]
+    assert not out[2].isnan().any() and not out[4].isnan().any()
+    out = p.attention(0, q, tables, torch.tensor([100, 101, 0, 30, 1], dtype=torch.int32, device=DEV), max_len=100)
+    assert [bool(x.isnan().any()) for x in out] == [False, True, False, False, False]
+
+
+def test_attention_strides_in_place_and_offsets_past_32_bits(nnc):
+    """Queries inside a fused projection, the output over the queries; a pool whose last page starts beyond 2^32 bytes and
+    beyond 2^31 elements."""
+    rng = np.random.default_rng(0)
+    pages = 17000
+    p = nnc.Pages.empty(1, pages, 128, 16, 64, torch.float16, DEV)       # 4.5 GB for K, as much for V, 2.2e9 elements each
+    assert p.k.numel() > 2 ** 31
+    tables = torch.from_numpy((pages - 1 - rng.permutation(4)).reshape(2, 2).astype(np.int32)).to(DEV)
+    lens = [200, 256]
+    fill(nnc, p, tables, lens)
+    wide = torch.randn((2, 48 * 64 + 3), device=DEV).to(torch.float16)
+    q = wide[:, 3:].view(2, 48, 64)[:, ::3]                               # 16 heads, three apart, odd alignment
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    # (the definition on the four pages alone)
+    small = nnc.Pages(p.k[:, -4:].clone(), p.v[:, -4:].clone())
+    out = p.attention(0, q, tables, ln)
+    check_attention(small, q, out, tables - (pages - 4), lens)
+    kept = wide.clone()
+    assert p.attention(0, q, tables, ln, out=q) is q and torch.equal(q, out)
+    mask = torch.zeros(48, dtype=torch.bool)
+    mask[::3] = True
+    assert torch.equal(wide[:, 3:].view(2, 48, 64)[:, ~mask], kept[:, 3:].view(2, 48, 64)[:, ~mask]) and torch.equal(wide[:, :3], kept[:, :3])
+
+
+# ---- selection ------------------------------------------------------------------------------------------------
+
+def check_select(nnc, logits, scores, finished=None, eos=-1):
+    got = nnc.beam_select(logits, scores, finished, eos)
+    want = pu.select(pu.f64(logits), pu.f64(scores), None if finished is None else finished.cpu().numpy(), eos)
+    assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+    assert np.array_equal(got[3].cpu().numpy(), want[3])
+    s = pu.f64(got[2])
+    # the log-sum in fp32 sums of at most 16 x 64 terms: 2^-14 relative of a sum at the very worst, 2^-20 in practice; then one rounding
+    fin = np.isfinite(want[2])
+    assert np.array_equal(s[~fin], want[2][~fin], equal_nan=True)
+    assert (np.abs(s[fin] - want[2][fin]) <= 2.0 ** -20 + 2.0 ** -23 * np.abs(want[2][fin])).all()
+
+
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("g,w,v", [(1, 1, 1), (2, 3, 2), (1, 4, 17), (3, 5, 4096), (2, 8, 4097), (1, 32, 10001), (2, 4, 151936), (1, 2, 300001)])
+def test_select(nnc, rows, g, w, v):
+    gen = torch.Generator(device=DEV).manual_seed(v)
+    wide = (torch.randn((g * w, v + 3), generator=gen, device=DEV) * 3).to(pu.ROWS[rows])
+    logits = wide[:, 3:].unflatten(0, (g, w))                               # rows of every alignment
+    scores = -torch.rand((g, w), generator=gen, device=DEV) * 3 - 20
+    check_select(nnc, logits, scores)
+    finished = torch.rand((g, w), generator=gen, device=DEV) < 0.4
+    eos = v // 2
+    check_select(nnc, logits, scores, finished, eos)
+    check_select(nnc, logits.masked_fill(torch.rand((g, w, v), generator=gen, device=DEV) < 0.7, -math.inf), scores, finished, eos)
+    scores[:, w // 2:] = -math.inf
+    scores[:, 0] = -1.0
+    check_select(nnc, logits, scores, torch.zeros_like(finished), eos)
+
+
+def test_select_ties_go_to_the_lower_beam_and_token(nnc):
+    """Equal rows at different alignments have equal sums; equal logits, zeros of both signs, everything forbidden."""
+    for v in (5, 777, 9001):
+        gen = torch.Generator(device=DEV).manual_seed(v)
+        row = torch.randn(v, generator=gen, device=DEV).round(decimals=1)
+        logits = torch.empty((4, v + 1), device=DEV)
+        logits[:, :v] = row
+        logits = logits[:, :v][None]
+        got = nnc.beam_select(logits, torch.full((1, 4), -2.5, device=DEV))
+        best = (row == row.max()).nonzero().flatten()[:4].tolist()
+        want = [(b, t) for b in range(4) for t in best][:4]
+        assert list(zip(got[1][0].tolist(), got[0][0].tolist()))[:len(want)] == want
+        assert len(set(got[2][0].tolist()[:len(best) if len(best) < 4 else 4])) == 1
+        zeros = torch.zeros((1, 3, v), device=DEV)
+        zeros[:, :, ::2] = -0.0
+        check_select(nnc, zeros, torch.zeros((1, 3), device=DEV))
+        none = torch.full((2, 3, v), -math.inf, device=DEV)
+        check_select(nnc, none, torch.zeros((2, 3), device=DEV))
+        low = torch.full((1, 3, v), torch.finfo(torch.float32).min, device=DEV)   # the type's lowest value is a number
+        check_select(nnc, low, torch.zeros((1, 3), device=DEV))
+
+
+def test_select_shows_a_failed_beam(nnc):
+    logits = torch.randn((2, 3, 5000), device=DEV)
+    scores = torch.full((2, 3), -1.0, device=DEV)
+    logits[0, 1, 4321] = math.nan
+    logits[1, 2, 17] = math.inf
+    tokens, parents, out, _ = nnc.beam_select(logits, scores)
+    assert out.isnan().all() and parents[0].tolist() == [1] * 3 and parents[1].tolist() == [2] * 3
+    assert tokens[0, 0] == 4321 and tokens[1, 0] == 17
+    logits[0, 1] = math.nan                                                # all of it; and where the beam is not in use
+    assert nnc.beam_select(logits, scores)[0][0].tolist() == [0, 1, 2]
+    scores[0, 1] = scores[1, 2] = -math.inf
+    out = nnc.beam_select(logits, scores)
+    assert torch.isfinite(out[2]).all() and 1 not in out[1][0].tolist()
+
+
+# ---- reordering -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("store", list(pu.STORES))
+@pytest.mark.parametrize("g,w,tokens,dim,length,in_place", [(1, 4, 16, 128, 37, True), (2, 3, 24, 64, 24, True), (2, 8, 7, 64, 6, False), (1, 13, 1, 128, 5, True),
+                                                            (3, 32, 16, 64, 15, True), (1, 2, 300, 64, 299, False), (2, 5, 16, 128, 33, False), (1, 1, 16, 128, 0, True)])
+def test_reorder(nnc, store, g, w, tokens, dim, length, in_place):
+    rng = np.random.default_rng(length)
+    full, part = divmod(length, tokens)
+    cols, heads, layers = full + 2, 2, 3
+    p = nnc.Pages.empty(layers, g * (full + 4 * w), tokens, heads, dim, pu.STORES[store], DEV)
+    for x in (p.k, p.v):
+        x.view(torch.uint8).copy_(torch.from_numpy(rng.integers(0, 120, x.view(torch.uint8).shape, dtype=np.uint8)))
+    for x in (p.k_scale, p.v_scale):
+        if x is not None:
+            x.copy_(torch.from_numpy(rng.random(x.shape).astype(np.float32)))
+    pages = rng.permutation(p.n_pages).astype(np.int32).reshape(g, -1)
+    before = np.zeros((g, w, cols), np.int32)
+    before[:, :, :full] = pages[:, None, :full]
+    before[:, :, full], before[:, :, full + 1] = pages[:, full:full + w], pages[:, full + w:full + 2 * w]
+    if full:  # the beams differ in a page that is full, too
+        before[:, :, full - 1] = pages[:, full + 2 * w:full + 3 * w]
+    after = before.copy()
+    if not in_place:
+        after[:, :, :full], after[:, :, full] = -7, pages[:, full + 3 * w:]
+    parents = rng.integers(0, w, (g, w)).astype(np.int32)
+    parents[0, w - 1] = w                                                   # no such beam: it goes on by itself
+    want_t, old = after.copy(), raw(p)
+    want = [x.clone() for x in old]
+    for b in range(g):
+        for j in range(w):
+            par = parents[b, j] if parents[b, j] < w else j
+            want_t[b, j, :full] = before[b, par, :full]
+            for x, y in zip(want, old):
+                x[:, int(after[b, j, full]), :, :part] = y[:, int(before[b, par, full]), :, :part]
+    tb = torch.from_numpy(before.reshape(g * w, cols)).to(DEV)
+    ta = tb if in_place else torch.from_numpy(after.reshape(g * w, cols)).to(DEV)
+    p.reorder(tb, ta, torch.full((g * w,), length, dtype=torch.int32, device=DEV), torch.from_numpy(parents).to(DEV))
+    assert np.array_equal(ta.cpu().numpy().reshape(g, w, cols), want_t)
+    assert all(same_bits(a, b) for a, b in zip(raw(p), want))
+    if not in_place:
+        assert np.array_equal(tb.cpu().numpy().reshape(g, w, cols), before)
+    # a length that does not fit changes nothing
+    for bad in (-1, cols * tokens + 1):
+        ta0, old = ta.clone(), raw(p)
+        p.reorder(ta, ta, torch.full((g * w,), bad, dtype=torch.int32, device=DEV), torch.from_numpy(parents).to(DEV))
+        assert torch.equal(ta, ta0) and all(same_bits(a, b) for a, b in zip(raw(p), old))
+
+
+# ---- together -------------------------------------------------------------------------------------------------
+
+def _search_step(nnc, p, s, ws):
+    p.append(0, s["k"], s["v"], s["tables"], s["seq"], s["lens"] - 1)
+    s["out"].copy_(p.attention(0, s["q"], s["tables"], s["lens"], max_len=40, workspace=ws[0]))
+    got = nnc.beam_select(s["logits"], s["scores"], s["finished"], 3, workspace=ws[1])
+    p.reorder(s["tables"], s["tables"], s["lens"], got[1])
+    return got
+
+
+@pytest.mark.parametrize("store", ["bf16", "i8"])
+def test_a_search_step_captured_and_replayed(nnc, store):
+    """append, attention, selection and reordering in one graph, replayed with other inputs in between, against the same calls
+    made one by one on a second pool."""
+    g, w, heads, v = 2, 3, 2, 6000
+    rng = np.random.default_rng(0)
+    tables = torch.from_numpy(rng.permutation(g * w * 3).reshape(g * w, 3).astype(np.int32)).to(DEV)
+    pools = [make_pool(nnc, store, 1, g * w * 3, 16, heads, 64) for _ in range(2)]
+    lens = [20] * (g * w)
+    for p in pools:
+        fill(nnc, p, tables, lens)
+
+    def inputs(seed):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        r = lambda *shape: torch.randn(shape, generator=gen, device=DEV)
+        return dict(k=r(g * w, heads, 64), v=r(g * w, heads, 64), q=r(g * w, heads * 2, 64), logits=r(g, w, v), scores=-r(g, w).abs())
+
+    def state(p):
+        return dict(inputs(0), tables=tables.clone(), lens=torch.tensor(lens, dtype=torch.int32, device=DEV) + 1,
+                    seq=torch.arange(g * w, dtype=torch.int32, device=DEV), out=torch.zeros((g * w, heads * 2, 64), device=DEV),
+                    finished=torch.zeros((g, w), dtype=torch.bool, device=DEV))
+
+    a, b = state(pools[0]), state(pools[1])
+    need = pools[0].attention_workspace(a["q"], a["tables"], a["lens"], max_len=40)
+    ws = [torch.empty(max(need, 16), dtype=torch.uint8, device=DEV), torch.empty(1 << 16, dtype=torch.uint8, device=DEV)]
+    tables0, raw0 = a["tables"].clone(), raw(pools[0])
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        got = _search_step(nnc, pools[0], a, ws)
+    assert torch.equal(a["tables"], tables0) and all(same_bits(x, y) for x, y in zip(raw(pools[0]), raw0))  # (captured, not run)
+    for step in range(6):
+        new = inputs(step + 1)
+        for s in (a, b):
+            for name, x in new.items():
+                s[name].copy_(x)
+            s["lens"].fill_(21 + step)
+        graph.replay()
+        want = _search_step(nnc, pools[1], b, [None, None])
+        torch.cuda.synchronize()
+        assert torch.equal(a["out"], b["out"]) and torch.equal(a["tables"], b["tables"])
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        for x, y in zip(raw(pools[0]), raw(pools[1])):
+            assert same_bits(x, y)
+
+
+def test_calls_on_two_streams(nnc):
+    """Two pools on two streams at once, each against its own result alone."""
+    runs = []
+    for seed in (1, 2):
+        p = make_pool(nnc, "e4m3", 1, 64, 64, 4, 128)
+        tables = torch.arange(64, dtype=torch.int32, device=DEV).reshape(2, 32)
+        fill(nnc, p, tables, [2000, 1500], seed)
+        q = torch.randn((2, 16, 128), device=DEV)
+        ln = torch.tensor([2000, 1500], dtype=torch.int32, device=DEV)
+        runs.append((p, q, tables, ln, p.attention(0, q, tables, ln)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    outs = [[], []]
+    for _ in range(8):
+        for i, (p, q, tables, ln, _) in enumerate(runs):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(p.attention(0, q, tables, ln))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, runs[i][4]) for o in outs[i])
