@@ -3,6 +3,7 @@
 // Each workgroup walks `chunk` positions of one sequence with a running maximum m, sum l and weighted sum; where a
 // sequence has several workgroups, k_page_attn_join merges their (m, l, sum) records.  Bound: the cache's bytes.
 #include <type_traits>
+#include <algorithm>
 
 #include "nnc_internal.h"
 #include "nnc_pages.h"
@@ -17,6 +18,7 @@ struct AttnArgs {
   PageAttn a;
   PageAttnPlan plan;
   float* part;  // [seq][head][split][head_dim] weighted sums, then [seq][head][split][2] maxima and sums
+  bool q_wide;  // query rows can be read sixteen bytes at a time
 };
 
 // Positions of a sequence that are attended to: lo .. hi - 1; bad: the length is no length of this cache.
@@ -50,85 +52,232 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, uint32_t seq, uint3
   else static_cast<uint16_t*>(a.a.out)[o] = (uint16_t)(a.a.q_dtype == DT_BF16 ? Bf16::bits(v) : Fp16::bits(v));
 }
 
-// One query head per workgroup: head_dim / 8 neighbouring lanes per position, sixteen (thirty-two) positions at a time.
-template <int STORE, int D>
-__global__ __launch_bounds__(256) void k_page_attn(AttnArgs a) {
-  constexpr int LPR = D / 8, NG = 256 / LPR;
-  __shared__ float sm[NG], sl[NG], sacc[NG][D];
-  const uint32_t split = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
-  const uint32_t kvh = head / (a.a.n_q_heads / a.p.n_kv_heads);
-  const Reach r = reach(a, seq);
-  const uint32_t begin = r.lo + split * a.plan.chunk, end = min(r.hi, begin + a.plan.chunk);
-  if (split && begin >= end) return;  // (the first workgroup answers for an empty row)
-  const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
-  const float c = a.a.scale * 1.44269504088896341f;
-  float q[8];
-  const int64_t qo = (int64_t)seq * a.a.q_row + (int64_t)head * a.a.q_head + lane * 8;
-  if (a.a.q_dtype == DT_F32) load8<DT_F32>(a.a.q, qo, false, q);
-  else if (a.a.q_dtype == DT_BF16) load8<DT_BF16>(a.a.q, qo, false, q);
-  else load8<DT_F16>(a.a.q, qo, false, q);
-  float m = -INFINITY, l = r.bad ? NAN : 0.f, acc[8] = {};
-  for (uint32_t pos = begin + grp; pos < end; pos += NG) {
-    const int64_t at = page_row(a.p, a.t, (int32_t)seq, (int32_t)pos, kvh);
-    float k[8], v[8], ks = 1.f, vs = 1.f;
-    const int64_t e = (at < 0 ? 0 : at) * D + lane * 8;
-    if constexpr (page_scaled(STORE)) {
-      const uint2 kw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.p.k) + e);
-      const uint2 vw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.p.v) + e);
-      ks = a.p.k_scale[at < 0 ? 0 : at];
-      vs = a.p.v_scale[at < 0 ? 0 : at];
-      page_widen4<STORE>(kw.x, k);
-      page_widen4<STORE>(kw.y, k + 4);
-      page_widen4<STORE>(vw.x, v);
-      page_widen4<STORE>(vw.y, v + 4);
-    } else {
-      load8<STORE>(a.p.k, e, true, k);
-      load8<STORE>(a.p.v, e, true, v);
+// Where a workgroup is: heads head0 .. + nh - 1 of one kv head, positions begin .. end - 1 of a sequence.
+struct Part {
+  uint32_t split, seq, kvh, nh, head0, begin, end;
+  bool bad, idle;
+};
+__device__ __forceinline__ Part part_of(const AttnArgs& a, uint32_t head_tiles) {
+  Part w;
+  w.split = blockIdx.z;
+  w.seq = blockIdx.y;
+  w.kvh = blockIdx.x / head_tiles;
+  const uint32_t G = a.a.n_q_heads / a.p.n_kv_heads, h0 = (blockIdx.x - w.kvh * head_tiles) * 16;
+  w.nh = min(16u, G - h0);
+  w.head0 = w.kvh * G + h0;
+  const Reach r = reach(a, w.seq);
+  w.begin = r.lo + w.split * a.plan.chunk;
+  w.end = min(r.hi, w.begin + a.plan.chunk);
+  w.bad = r.bad;
+  w.idle = w.split && w.begin >= w.end;  // (the first workgroup answers for an empty row)
+  return w;
+}
+
+// The pages of a tile's rows, from the table.
+struct Finder {
+  const int32_t* entries;
+  FastDiv by_page;
+  uint32_t n_pages, page_tokens, page_rows, first_row, last;
+  __device__ __forceinline__ Finder(const AttnArgs& a, uint32_t seq, uint32_t kvh)
+      : entries(a.t.entries + (size_t)seq * a.t.max_pages), by_page(a.p.by_page), n_pages(a.p.n_pages), page_tokens(a.p.page_tokens),
+        page_rows(a.p.n_kv_heads * a.p.page_tokens), first_row(kvh * a.p.page_tokens), last(a.a.max_len ? a.a.max_len - 1 : 0) {}
+  // The entry of a position, and its row within that page's rows.  A position behind the sequence's end may be asked for too (up to
+  // max_len, which the table holds): its entry is a number that nothing is known about.
+  __device__ __forceinline__ void look(uint32_t pos, int32_t& page, uint32_t& row) const {
+    pos = min(pos, last);
+    const uint32_t e = fdiv(pos, by_page);
+    page = entries[e];
+    row = first_row + (pos - e * page_tokens);
+  }
+  // The row in the pool; `in`: the position is one of the sequence's, whose page has to exist.
+  __device__ __forceinline__ uint64_t at(int32_t page, uint32_t row, bool in, bool& missing) const {
+    const bool ok = (uint32_t)page < n_pages;
+    missing |= in && !ok;
+    return (uint64_t)(ok ? (uint32_t)page : 0u) * page_rows + row;
+  }
+};
+__device__ __forceinline__ uint64_t first_lane(uint64_t v) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) |
+         ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32);
+}
+
+// Eight query values at element o.
+__device__ __forceinline__ void load_query8(const AttnArgs& a, int64_t o, bool wide, float (&x)[8]) {
+  if (a.a.q_dtype == DT_F32) load8<DT_F32>(a.a.q, o, wide, x);
+  else if (a.a.q_dtype == DT_BF16) load8<DT_BF16>(a.a.q, o, wide, x);
+  else load8<DT_F16>(a.a.q, o, wide, x);
+}
+
+// The four waves' maxima and sums (smax, ssum [wave][head]) and weighted sums (out[wave * stride + head * pitch + dim], already
+// brought to the common maximum) -> output, or the workgroup's record.
+template <int D>
+__device__ __forceinline__ void finish(const AttnArgs& a, const Part& w, const float (&smax)[4][16], const float (&ssum)[4][16],
+                                       const float* out, int stride, int pitch) {
+  for (uint32_t e = threadIdx.x; e < w.nh * D; e += 256) {
+    const uint32_t h = e / D, d = e % D;
+    float L = 0.f, v = 0.f, M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, smax[i][h]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float l = ssum[i][h];
+      L += l != l ? l : smax[i][h] == -INFINITY ? 0.f : l * __builtin_amdgcn_exp2f(smax[i][h] - M);
+      v += out[i * stride + h * pitch + d];
     }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(q[i], k[i], s);
-    s += dpp_get<DPP_QUAD_XOR1>(s);
-    s += dpp_get<DPP_QUAD_XOR2>(s);
-    s += dpp_get<DPP_ROW_HALF_MIRROR>(s);
-    if constexpr (LPR == 16) s += dpp_get<DPP_ROW_MIRROR>(s);
-    s = at < 0 ? NAN : s * ks * c;
-    const float mn = fmaxf(m, s), ms = mn == -INFINITY ? 0.f : mn;
-    const float f = exp2f(m - ms), w = exp2f(s - ms);
-    l = l * f + w;
-    const float wv = w * vs;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(wv, v[i], acc[i] * f);
-    m = mn;
+    if (a.plan.splits == 1) {
+      store_out(a, w.seq, w.head0 + h, (int)d, L == 0.f ? 0.f : v / L);
+    } else {
+      const size_t rec = ((size_t)w.seq * a.a.n_q_heads + w.head0 + h) * a.plan.splits + w.split;
+      a.part[rec * D + d] = v;
+      if (d == 0) {
+        float* ml = a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D + rec * 2;
+        ml[0] = M;
+        ml[1] = L;
+      }
+    }
   }
-  if (lane == 0) {
-    sm[grp] = m;
-    sl[grp] = l;
-  }
+}
+
+// fp32 pages, on the fp32 matrix instruction (16 x 16 x 4), tiles of 16 positions.  Its operands are one value per lane, so
+// nothing has to be turned: for S^T = K Q^T lane (c, g) loads dims 16 i + 4 g .. + 3 of row c and product j takes element j
+// (the sum over dims may run in any order that both operands share); for O^T = V^T P^T product (i, b, j) takes dim 64 b + 4 c + j of row
+// 4 g + i, whose weight the lane holds.
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_tiles) {
+  constexpr int LD = D / 16, NB = D / 64, OPITCH = D + 4;
+  __shared__ __attribute__((aligned(16))) float out[4][16 * OPITCH];
+  __shared__ float smax[4][16], ssum[4][16];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const float fac = a.a.scale * 1.44269504088896341f;
+  struct Tile {
+    f32x4_t k[LD], v[4][NB];
+  };
+  struct Where {
+    int32_t page[5];
+    uint32_t row[5];
+  };
+  const Finder find(a, blockIdx.y, blockIdx.x / head_tiles);
+  bool missing = false;
+  auto look = [&](Where& t, uint32_t p0) __attribute__((always_inline)) {
+    find.look(p0 + c, t.page[4], t.row[4]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sacc[grp][lane * 8 + i] = acc[i];
+    for (int i = 0; i < 4; ++i) find.look(p0 + g * 4 + i, t.page[i], t.row[i]);
+  };
+  // (the table is asked before the sequence's length is known, unless a window moves the first position)
+  Where p;
+  if (!a.a.window) look(p, blockIdx.z * a.plan.chunk + wave * 16);
+  const Part w = part_of(a, head_tiles);
+  if (w.idle) return;
+  uint32_t p0 = w.begin + wave * 16;
+  if (a.a.window) look(p, p0);
+  // (rows behind the end are the tile's first row again)
+  auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
+    uint64_t at = find.at(p.page[4], p.row[4], p0 + c < w.end, missing);
+    const uint64_t first = first_lane(at);
+    const float* k = static_cast<const float*>(a.p.k) + (p0 + c < w.end ? at : first) * D + g * 4;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) t.k[i] = *reinterpret_cast<const f32x4_t*>(k + i * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in = p0 + g * 4 + i < w.end;
+      at = find.at(p.page[i], p.row[i], in, missing);
+      const float* v = static_cast<const float*>(a.p.v) + (in ? at : first) * D + c * 4;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) t.v[i][b] = *reinterpret_cast<const f32x4_t*>(v + b * 64);
+    }
+  };
+  float q[LD][4];
+  {
+    const int64_t qo = (int64_t)w.seq * a.a.q_row + (int64_t)(w.head0 + min((uint32_t)c, w.nh - 1)) * a.a.q_head;
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t o = qo + i * 16 + g * 4 + j;
+        q[i][j] = a.a.q_dtype == DT_F32 ? static_cast<const float*>(a.a.q)[o]
+                  : a.a.q_dtype == DT_BF16 ? Bf16::widen(static_cast<const uint16_t*>(a.a.q)[o]) : Fp16::widen(static_cast<const uint16_t*>(a.a.q)[o]);
+      }
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x4_t acc[NB][4];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  auto step = [&](Tile& t, uint32_t p0) __attribute__((always_inline)) {
+    f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[i][j], q[i][j], s, 0, 0, 0);
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool past = p0 + g * 4 + i >= w.end;  // (weighs nothing, and nothing times an infinity would not be nothing)
+      x[i] = past ? -INFINITY : s[i] * fac;
+      if (past) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) t.v[i][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+    const float top = col4_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+    if (__any(top > m)) {
+      const float mn = fmaxf(m, top), r = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= r;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[b][j] *= r;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = __builtin_amdgcn_exp2f(x[i] - base);
+      l += p;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[i][b][j], p, acc[b][j], 0, 0, 0);
+    }
+  };
+  if (p0 < w.end) {
+    Tile t0, t1;
+    load(t0, p, p0);
+    look(p, p0 + 64);
+    while (true) {
+      load(t1, p, p0 + 64);
+      look(p, p0 + 128);
+      step(t0, p0);
+      p0 += 64;
+      if (p0 >= w.end) break;
+      load(t0, p, p0 + 64);
+      look(p, p0 + 128);
+      step(t1, p0);
+      p0 += 64;
+      if (p0 >= w.end) break;
+    }
+  }
+  l = col4_sum(l);
+  if (__any(missing) || w.bad) l = NAN;
+  if (g == 0) {
+    smax[wave][c] = m;
+    ssum[wave][c] = l;
+  }
   __syncthreads();
-  if (tid >= D) return;
-  float M = -INFINITY;
-  for (int i = 0; i < NG; ++i) M = fmaxf(M, sm[i]);
-  const float Ms = M == -INFINITY ? 0.f : M;
-  float L = 0.f, o = 0.f;
-  for (int i = 0; i < NG; ++i) {
-    const float f = exp2f(sm[i] - Ms);
-    L += sl[i] * (sl[i] == sl[i] ? f : 1.f);
-    o += sacc[i][tid] * f;
+  const float M = fmaxf(fmaxf(smax[0][c], smax[1][c]), fmaxf(smax[2][c], smax[3][c]));
+  const float r = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  // element e of lane (c, g) in product (b, j): head c, dim 64 b + 4 (4 g + e) + j
+  if (c < (int)w.nh) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4_t*>(&out[wave][c * OPITCH + b * 64 + (g * 4 + e) * 4]) =
+            f32x4_t{acc[b][0][e], acc[b][1][e], acc[b][2][e], acc[b][3][e]} * r;
   }
-  if (a.plan.splits == 1) {
-    store_out(a, seq, head, tid, L == 0.f ? 0.f : o / L);
-    return;
-  }
-  const size_t rec = ((size_t)seq * a.a.n_q_heads + head) * a.plan.splits + split;
-  a.part[rec * D + tid] = o;
-  if (tid == 0) {
-    float* ml = a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D + rec * 2;
-    ml[0] = M;
-    ml[1] = L;
-  }
+  __syncthreads();
+  finish<D>(a, w, smax, ssum, out[0], 16 * OPITCH, OPITCH);
 }
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -140,10 +289,12 @@ __device__ __forceinline__ u32x4_v widen8_bf16(uint32_t lo, uint32_t hi) {
   if constexpr (STORE == PS_I8) {
     return Bf16W8::widen8(lo, hi);
   } else {
-    float x[8];
-    page_widen4<STORE>(lo, x);
-    page_widen4<STORE>(hi, x + 4);
-    return u32x4_v{Bf16::pack2(x[0], x[1]), Bf16::pack2(x[2], x[3]), Bf16::pack2(x[4], x[5]), Bf16::pack2(x[6], x[7])};
+    auto two = [](uint32_t w, auto high) __attribute__((always_inline)) {
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, decltype(high)::value));
+    };
+    const std::false_type l{};
+    const std::true_type h{};
+    return u32x4_v{two(lo, l), two(lo, h), two(hi, l), two(hi, h)};
   }
 }
 
@@ -154,7 +305,7 @@ __device__ __forceinline__ u32x2_v lds_column4(const char* p) {
   return __builtin_bit_cast(u32x2_v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)p));
 }
 
-// The same on the matrix cores, up to sixteen query heads of one kv head per workgroup, a wave walking tiles of 32 positions.
+// Up to sixteen query heads of one kv head per workgroup, a wave walking tiles of 32 positions, both products on the matrix cores.
 //   S^T = K Q^T: A = 16 cached rows as they lie in the page, B = the queries; lane (c, g) gets head c, positions 4 g .. + 3.
 //   O^T = V^T P^T: B is what the lane holds already (its 4 + 4 weights); A, 8 positions of one dim per lane, comes from LDS,
 //   where a wave lays its 32 rows of V down and reads them back by columns.
@@ -173,28 +324,58 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
   __shared__ __attribute__((aligned(16))) float sc[4][64];
   __shared__ float smax[4][16], ssum[4][16];
   static_assert(16 * OPITCH * 4 <= 32 * PITCH, "the waves' results fit where V was");
-  const uint32_t split = blockIdx.x, seq = blockIdx.z;
-  const uint32_t kvh = blockIdx.y / head_tiles, G = a.a.n_q_heads / a.p.n_kv_heads;
-  const uint32_t h0 = (blockIdx.y - kvh * head_tiles) * 16, nh = min(16u, G - h0), head0 = kvh * G + h0;
-  const Reach r = reach(a, seq);
-  const uint32_t begin = r.lo + split * a.plan.chunk, end = min(r.hi, begin + a.plan.chunk);
-  if (split && begin >= end) return;  // (the first workgroup answers for an empty row)
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
   char* vb = vbuf[wave];
 
+  struct Tile {
+    u32x4_v k[2][LD], v[2][LD];
+    float scale;
+  };
+  // A tile's rows of this lane are its positions c and 16 + c (behind the end: the tile's first row again).  The table is read a
+  // tile ahead of the rows, which would otherwise wait for it in front of the work on the tile before.
+  struct Where {
+    int32_t page[2];
+    uint32_t row[2];
+  };
+  const Finder find(a, blockIdx.y, blockIdx.x / head_tiles);
+  bool missing = false;
+  auto look = [&](Where& p, uint32_t p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) find.look(p0 + h * 16 + c, p.page[h], p.row[h]);
+  };
+  // (the table is asked before the sequence's length is known, unless a window moves the first position)
+  Where p;
+  if (!a.a.window) look(p, blockIdx.z * a.plan.chunk + wave * 32);
+  const Part w = part_of(a, head_tiles);
+  if (w.idle) return;
+  const uint32_t end = w.end;
+  uint32_t p0 = w.begin + wave * 32;
+  if (a.a.window) look(p, p0);
+  auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
+    uint64_t at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) at[h] = find.at(p.page[h], p.row[h], p0 + h * 16 + c < end, missing);
+    const uint64_t first = first_lane(at[0]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (p0 + h * 16 + c >= end) at[h] = first;
+      const uint64_t o = at[h] * (D * (B8 ? 1 : 2)) + g * 16;
+#pragma unroll
+      for (int i = 0; i < LD; ++i) t.k[h][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.k) + o + i * 64);
+#pragma unroll
+      for (int i = 0; i < LD; ++i) t.v[h][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.v) + o + i * 64);
+    }
+    // lanes 0 .. 31: the K scales of the tile's positions, 32 .. 63: those of V
+    if constexpr (B8) t.scale = (g < 2 ? a.p.k_scale : a.p.v_scale)[(g & 1) ? at[1] : at[0]];
+  };
   // queries: head c (columns past the last head repeat it and are not used), eight dims per k tile
   u32x4_v qf[KT][NQ];
   float fac = a.a.scale * 1.44269504088896341f;
   {
-    const int64_t qo = (int64_t)seq * a.a.q_row + (int64_t)(head0 + min((uint32_t)c, nh - 1)) * a.a.q_head;
+    const int64_t qo = (int64_t)w.seq * a.a.q_row + (int64_t)(w.head0 + min((uint32_t)c, w.nh - 1)) * a.a.q_head;
     float x[KT][8];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const int64_t o = qo + (B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8);
-      if (a.a.q_dtype == DT_F32) load8<DT_F32>(a.a.q, o, false, x[kt]);
-      else if (a.a.q_dtype == DT_BF16) load8<DT_BF16>(a.a.q, o, false, x[kt]);
-      else load8<DT_F16>(a.a.q, o, false, x[kt]);
-    }
+    for (int kt = 0; kt < KT; ++kt) load_query8(a, qo + (B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8), a.q_wide, x[kt]);
     if constexpr (FULL && HF::kNarrowRange) {
       float top = 0.f;
 #pragma unroll
@@ -225,30 +406,6 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
         }
       }
   }
-
-  struct Tile {
-    u32x4_v k[2][LD], v[2][LD];
-    float scale;
-  };
-  bool missing = false;
-  auto load = [&](Tile& t, uint32_t p0) __attribute__((always_inline)) {
-    int64_t row[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      row[h] = page_row(a.p, a.t, (int32_t)seq, (int32_t)min(p0 + h * 16 + c, end - 1), kvh);
-      if (row[h] < 0) {
-        missing = true;
-        row[h] = 0;
-      }
-      const int64_t o = row[h] * (D * (B8 ? 1 : 2)) + g * 16;
-#pragma unroll
-      for (int i = 0; i < LD; ++i) t.k[h][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.k) + o + i * 64);
-#pragma unroll
-      for (int i = 0; i < LD; ++i) t.v[h][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.v) + o + i * 64);
-    }
-    // lanes 0 .. 31: the K scales of the tile's positions, 32 .. 63: those of V
-    if constexpr (B8) t.scale = (g < 2 ? a.p.k_scale : a.p.v_scale)[row[g & 1]];
-  };
 
   constexpr float LIFT = HF::kNarrowRange ? 10.f : 0.f;
   float m = -INFINITY, l = 0.f;
@@ -359,23 +516,25 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
   };
 
   // two tiles in registers: the next one is on its way while this one is worked on
-  uint32_t p0 = begin + wave * 32;
   if (p0 < end) {
     Tile t0, t1;
-    load(t0, p0);
+    load(t0, p, p0);
+    look(p, p0 + 128);
     while (true) {
-      if (p0 + 128 < end) load(t1, p0 + 128);
+      load(t1, p, p0 + 128);
+      look(p, p0 + 256);
       step(t0, p0);
       p0 += 128;
       if (p0 >= end) break;
-      if (p0 + 128 < end) load(t0, p0 + 128);
+      load(t0, p, p0 + 128);
+      look(p, p0 + 256);
       step(t1, p0);
       p0 += 128;
       if (p0 >= end) break;
     }
   }
   l = col4_sum(l);
-  if (__any(missing) || r.bad) l = NAN;
+  if (__any(missing) || w.bad) l = NAN;
 
   // the four waves' results
   if (g == 0) {
@@ -383,75 +542,89 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
     ssum[wave][c] = l;
   }
   __syncthreads();
-  float M = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) M = fmaxf(M, smax[w][c]);
+  const float M = fmaxf(fmaxf(smax[0][c], smax[1][c]), fmaxf(smax[2][c], smax[3][c]));
   const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
   float* o = reinterpret_cast<float*>(vb);
-  if (c < (int)nh) {
+  if (c < (int)w.nh) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o + c * OPITCH + dt * 16 + g * 4) = acc[dt] * f;
   }
   __syncthreads();
-  for (uint32_t e = tid; e < nh * D; e += 256) {
-    const uint32_t h = e / D, d = e % D;
-    float L = 0.f, v = 0.f, Mh = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) Mh = fmaxf(Mh, smax[w][h]);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float lw = ssum[w][h];
-      L += lw != lw ? lw : smax[w][h] == -INFINITY ? 0.f : lw * __builtin_amdgcn_exp2f(smax[w][h] - Mh);
-      v += reinterpret_cast<const float*>(vbuf[w])[h * OPITCH + d];
-    }
-    if (a.plan.splits == 1) {
-      store_out(a, seq, head0 + h, (int)d, L == 0.f ? 0.f : v / L);
-    } else {
-      const size_t rec = ((size_t)seq * a.a.n_q_heads + head0 + h) * a.plan.splits + split;
-      a.part[rec * D + d] = v;
-      if (d == 0) {
-        float* ml = a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D + rec * 2;
-        ml[0] = Mh;
-        ml[1] = L;
-      }
-    }
-  }
+  finish<D>(a, w, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
 }
 
+// Grid: heads, sequences, splits, so that the workgroups of one split go to all XCDs in turn (with the splits innermost, four of them
+// and eight heads, a split stays on two of the eight XCDs, and where most sequences have no fourth one those two idle: 48 sequences
+// of 1 .. 6000 positions as 2 splits 81 -> 68 us), and the splits that few sequences reach come last.
+//
+// Merge of a sequence's records for one query head: eight groups of threads take the splits in turn, four dims a thread.
 template <int D>
-__global__ __launch_bounds__(D) void k_page_attn_join(AttnArgs a) {
+__global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
+  constexpr int NT = 2 * D, LANES = D / 4;
+  __shared__ float top[NT / 64];
+  __shared__ __attribute__((aligned(16))) float sum[8][D];
+  __shared__ float total[8];
   const uint32_t head = blockIdx.x, seq = blockIdx.y;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, grp = tid / LANES, lane = tid % LANES;
   const Reach r = reach(a, seq);
   const uint32_t used = r.hi == r.lo ? 1u : (r.hi - r.lo + a.plan.chunk - 1) / a.plan.chunk;
   const size_t rec0 = ((size_t)seq * a.a.n_q_heads + head) * a.plan.splits;
-  const float* ml = a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D + rec0 * 2;
-  const float* acc = a.part + rec0 * D + tid;
-  float M = -INFINITY;
-  for (uint32_t i = 0; i < used; ++i) M = fmaxf(M, ml[2 * i]);
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D) + rec0;
+  const float4* acc = reinterpret_cast<const float4*>(a.part + rec0 * D) + lane;
+  float m = -INFINITY;
+  for (uint32_t i = tid; i < used; i += NT) m = fmaxf(m, ml[i].x);
+  m = wave_max(m);
+  if ((tid & 63) == 0) top[tid >> 6] = m;
+  __syncthreads();
+  float M = top[0];
+#pragma unroll
+  for (int i = 1; i < NT / 64; ++i) M = fmaxf(M, top[i]);
   const float Ms = M == -INFINITY ? 0.f : M;
-  float L = 0.f, o = 0.f;
-  for (uint32_t i = 0; i < used; ++i) {
-    const float f = exp2f(ml[2 * i] - Ms), l = ml[2 * i + 1];
-    L += l == l ? l * f : l;
-    o += acc[(size_t)i * D] * f;
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (uint32_t i = grp; i < used; i += 8) {
+    const float2 v = ml[i];
+    const float4 x = acc[(size_t)i * LANES];
+    const float f = __builtin_amdgcn_exp2f(v.x - Ms);
+    L += v.y == v.y ? v.y * f : v.y;
+    o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
   }
-  store_out(a, seq, head, tid, L == 0.f ? 0.f : o / L);
+  *reinterpret_cast<float4*>(&sum[grp][lane * 4]) = o;
+  if (lane == 0) total[grp] = L;
+  __syncthreads();
+  if (tid >= D) return;
+  L = 0.f;
+  float v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    L += total[i];
+    v += sum[i][tid];
+  }
+  store_out(a, seq, head, tid, L == 0.f ? 0.f : v / L);
 }
 
 }  // namespace
 
+// Workgroups along a sequence.  Two workgroups fit a CU, so 512 of them fill the chip; more only add starts, records and joining
+// (16384 positions of one sequence, 8 kv heads, bf16, us with the join: 64 splits 20.5, 128 25.0), while a split of 128 positions,
+// a tile for each of the four waves, is worth its join from 512 positions on (512 positions: 4 splits 10.6, none 12.7; 256: 11.0 and 9.1).
+// The lengths are not known here, only their bound: where sequences are several, as many workgroups again, of 1024 positions at
+// least, let the long ones be shared when the short ones are done (32 sequences of 0 .. 4096, 2 / 4 splits: 79 / 70; where all are
+// equally long it costs the join: 64 of 2048, 1 / 2 splits 98.6 / 102.7).
 PageAttnPlan plan_page_attention(const PagePool& p, uint32_t n_seqs, const PageAttn& a, uint32_t max_splits) {
   const uint32_t span = a.window ? (a.window < a.max_len ? a.window : a.max_len) : a.max_len;
   const uint64_t rows = (uint64_t)n_seqs * a.n_q_heads;
-  const uint64_t wgs = p.store == PS_F32 ? rows : (uint64_t)n_seqs * p.n_kv_heads * ((a.n_q_heads / p.n_kv_heads + 15) / 16);
-  uint64_t splits = (1024 + wgs - 1) / (wgs ? wgs : 1);
-  const uint64_t most = (span + 127) / 128;
+  const uint64_t wgs = (uint64_t)n_seqs * p.n_kv_heads * ((a.n_q_heads / p.n_kv_heads + 15) / 16);
+  const uint64_t one = wgs ? wgs : 1, most = span <= 256 ? 1 : (span + 127) / 128;
+  uint64_t splits = (512 + one - 1) / one;
+  const uint64_t uneven = std::min<uint64_t>((1024 + one - 1) / one, span / 1024);
+  if (n_seqs > 1 && splits < uneven) splits = uneven;
   if (splits > most) splits = most;
   if (splits > max_splits) splits = max_splits;
   if (splits < 1) splits = 1;
   PageAttnPlan pl;
-  pl.chunk = (uint32_t)(((span + splits - 1) / splits + 31) / 32 * 32);
+  pl.chunk = (uint32_t)(((span + splits - 1) / splits + 127) / 128 * 128);
   if (pl.chunk == 0) pl.chunk = 1;
   pl.splits = span ? (span + pl.chunk - 1) / pl.chunk : 1;
   pl.floats = pl.splits > 1 ? rows * pl.splits * (p.head_dim + 2) : 0;
@@ -462,12 +635,12 @@ hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTab
                                  float* workspace) {
   if (t.n_seqs == 0) return hipSuccess;
   if (t.n_seqs > 65535 || a.n_q_heads > 65535 || (p.head_dim != 64 && p.head_dim != 128) || (plan.splits > 1 && !workspace)) return hipErrorInvalidValue;
-  const AttnArgs g{p, t, a, plan, workspace};
-  const dim3 grid(plan.splits, a.n_q_heads, t.n_seqs);
+  const int64_t per16 = a.q_dtype == DT_F32 ? 4 : 8;
+  const AttnArgs g{p, t, a, plan, workspace, reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_row % per16 == 0 && a.q_head % per16 == 0};
   // queries that enter the product as they are (and an output whose rounding hides two-piece weights)
   const bool lite = !a.packed && a.q_dtype != DT_F32 && a.q_dtype == (p.store == PS_F16 ? DT_F16 : DT_BF16);
   const int ht = (a.n_q_heads / (int)p.n_kv_heads + 15) / 16;
-  const dim3 mc(plan.splits, p.n_kv_heads * ht, t.n_seqs);
+  const dim3 mc(p.n_kv_heads * ht, t.n_seqs, plan.splits);
 #define NNC_ATTN_CASE(ST)                                                                  \
   case ST:                                                                                 \
     if (p.head_dim == 128) {                                                               \
@@ -480,8 +653,8 @@ hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTab
     break
   switch (p.store) {
     case PS_F32:
-      if (p.head_dim == 128) k_page_attn<PS_F32, 128><<<grid, 256, 0, s>>>(g);
-      else k_page_attn<PS_F32, 64><<<grid, 256, 0, s>>>(g);
+      if (p.head_dim == 128) k_page_attn_f32<128><<<mc, 256, 0, s>>>(g, ht);
+      else k_page_attn_f32<64><<<mc, 256, 0, s>>>(g, ht);
       break;
     NNC_ATTN_CASE(PS_BF16);
     NNC_ATTN_CASE(PS_F16);
@@ -491,8 +664,8 @@ hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTab
   }
   if (plan.splits > 1) {
     const dim3 jg(a.n_q_heads, t.n_seqs);
-    if (p.head_dim == 128) k_page_attn_join<128><<<jg, 128, 0, s>>>(g);
-    else k_page_attn_join<64><<<jg, 64, 0, s>>>(g);
+    if (p.head_dim == 128) k_page_attn_join<128><<<jg, 256, 0, s>>>(g);
+    else k_page_attn_join<64><<<jg, 128, 0, s>>>(g);
   }
   return hipGetLastError();
 }

@@ -30,7 +30,7 @@ inline FastDiv fast_div(uint32_t d) {
   f.m = (uint32_t)((1ull << (31 + f.s)) / d + 1);
   return f;
 }
-__host__ __device__ __forceinline__ uint32_t fdiv(uint32_t n, const FastDiv& f) { return (uint32_t)(((uint64_t)n * f.m) >> (31 + f.s)); }
+__host__ __device__ __forceinline__ uint32_t fdiv(uint32_t n, const FastDiv& f) { return (uint32_t)(((uint64_t)(2 * n) * f.m) >> 32) >> f.s; }
 
 // One layer of a pool.
 struct PagePool {
