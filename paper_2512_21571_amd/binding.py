@@ -210,18 +210,26 @@ def _bad(message: str):
     raise NncError(E_ARG, message)
 
 
-def _dtype_of(t):
+def _row_types():
     import torch
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+_ROW_TYPES = None
+
+
+def _dtype_of(t):
+    global _ROW_TYPES
+    if _ROW_TYPES is None:
+        _ROW_TYPES = _row_types()
+    code = _ROW_TYPES.get(t.dtype)
     return _bad(f"{t.dtype} is not one of float32, bfloat16, float16") if code is None else code
 
 
 def _on(device, dtype, shape, **tensors):
     """Tensors of one device, type and shape, contiguous (None is skipped)."""
     for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        if t is not None and (t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
             _bad(f"{name}: contiguous {dtype} {list(shape)} on {device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
 
 
@@ -229,21 +237,18 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-class _Here:
-    """The device of a call made current for its time; `.stream` is the caller's current stream of that device."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = torch.cuda.device(device)
-        self.cuda, self.device = torch.cuda, device
-
-    def __enter__(self):
-        self.guard.__enter__()
-        self.stream = self.cuda.current_stream(self.device).cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+def _enqueue(device, f, *args):
+    """f(*args, stream) on the caller's current stream of a device, which is made current for the call if it is not.  (The stream's
+    handle as torch's own launchers get it: a Stream object costs 2 us, device guard and ctypes call 5.)"""
+    import torch
+    i = device.index
+    if torch.cuda.current_device() == i:
+        st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    if st != OK:
+        raise NncError(st, last_error())
 
 
 class Pages:
@@ -270,6 +275,7 @@ class Pages:
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
         self.desc = NncPages(ctypes.sizeof(NncPages), code, self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim,
                              k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale))
+        self._desc, self._i32 = ctypes.byref(self.desc), torch.int32
 
     @classmethod
     def empty(cls, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, dtype, device: str = "cuda:0"):
@@ -281,35 +287,43 @@ class Pages:
         return cls(k, v, *scales)
 
     def _table(self, tables, name="tables"):
-        if tables.dim() != 2:
-            _bad(f"{name}: [sequences, pages] expected")
-        _on(self.device, self.torch.int32, tables.shape, **{name: tables})
-        return NncPageTable(tables.data_ptr() if tables.numel() else None, tables.shape[0], tables.shape[1])
+        if tables.dtype != self._i32 or tables.dim() != 2 or tables.device != self.device or not tables.is_contiguous():
+            _bad(f"{name}: contiguous int32 [sequences, pages] on {self.device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
+        n, m = tables.shape
+        return NncPageTable(tables.data_ptr() or None, n, m)
+
+    def _index(self, x, n, name):
+        """seq or pos of n rows: (pointer, 0) of a tensor, (None, value) of a number."""
+        if not isinstance(x, self.torch.Tensor):
+            return None, int(x)
+        if x.dtype != self._i32 or x.shape != (n,) or x.device != self.device or not x.is_contiguous():
+            _bad(f"{name}: contiguous int32 [{n}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")
+        return x.data_ptr(), 0
+
+    def _strides(self, x, n, dtype, what):
+        """(row stride, head stride) of rows [n, heads, head_dim] whose elements lie next to each other."""
+        if x.dtype != dtype or x.device != self.device or x.dim() != 3 or x.shape[0] != n or x.shape[2] != self.head_dim:
+            _bad(f"{what}: {dtype} [{n}, heads, {self.head_dim}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")
+        row, head, one = x.stride()
+        if one != 1 and n:
+            _bad(f"{what}: the elements of a head must lie next to each other")
+        return row, head
 
     def _rows(self, k, v, seq, pos):
-        rows = NncPageRows()
-        some = k if k is not None else v
+        some = v if k is None else k
         if some is None:
-            _bad("k and v are both None")
-        for t in (k, v):
-            if t is None:
-                continue
-            if t.dim() != 3 or tuple(t.shape) != (some.shape[0], self.n_kv_heads, self.head_dim) or t.dtype != some.dtype or t.device != self.device:
-                _bad(f"rows: [rows, {self.n_kv_heads}, {self.head_dim}] of one type on {self.device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
-            if t.shape[0] and t.stride(2) != 1:
-                _bad("rows: the elements of a head must lie next to each other")
-        rows.n, rows.dtype = some.shape[0], _dtype_of(some)
+            _bad("rows: k and v are both None")
+        n, dtype = some.shape[0], some.dtype
+        kr = kh = vr = vh = 0
         if k is not None:
-            rows.k, rows.k_row_stride, rows.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
+            kr, kh = self._strides(k, n, dtype, "k")
         if v is not None:
-            rows.v, rows.v_row_stride, rows.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
-        for name, x in (("seq", seq), ("pos", pos)):
-            if isinstance(x, self.torch.Tensor):
-                _on(self.device, self.torch.int32, (rows.n,), **{name: x})
-                setattr(rows, name, x.data_ptr())
-            else:
-                setattr(rows, name + "0", int(x))
-        return rows
+            vr, vh = self._strides(v, n, dtype, "v")
+        if some.shape[1] != self.n_kv_heads or (k is not None and v is not None and v.shape[1] != self.n_kv_heads):
+            _bad(f"rows: {self.n_kv_heads} kv heads expected, not {some.shape[1]}")
+        sp, s0 = self._index(seq, n, "seq")
+        pp, p0 = self._index(pos, n, "pos")
+        return NncPageRows(_ptr(k), _ptr(v), _dtype_of(some), kr, kh, vr, vh, n, sp, pp, s0, p0)
 
     def append(self, layer: int, k, v, tables, seq, pos):
         """Write rows [n, kv heads, head_dim] (any strides between rows and heads) as positions `pos` of sequences `seq`: int32
@@ -317,8 +331,7 @@ class Pages:
         if k is None or v is None:
             _bad("rows: k or v is None")
         rows, table = self._rows(k, v, seq, pos), self._table(tables)
-        with _Here(self.device) as here:
-            _check(lib().nnc_page_append(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(rows), here.stream))
+        _enqueue(self.device, lib().nnc_page_append, self._desc, layer, ctypes.byref(table), ctypes.byref(rows))
 
     def read(self, layer: int, tables, seq, pos, dtype=None, n: int | None = None, k=None, v=None):
         """Rows (k, v) [n, kv heads, head_dim] of the named positions, in `dtype` (float32).  n: with two numbers for seq and
@@ -328,31 +341,33 @@ class Pages:
                 n = next((x.shape[0] for x in (seq, pos) if isinstance(x, self.torch.Tensor)), None)
                 if n is None:
                     _bad("read: n is missing")
-            k, v = (self.torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype or self.torch.float32, device=self.device) for _ in range(2))
+            k = self.torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype or self.torch.float32, device=self.device)
+            v = self.torch.empty_like(k)
         rows, table = self._rows(k, v, seq, pos), self._table(tables)
-        with _Here(self.device) as here:
-            _check(lib().nnc_page_read(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(rows), here.stream))
+        _enqueue(self.device, lib().nnc_page_read, self._desc, layer, ctypes.byref(table), ctypes.byref(rows))
         return k, v
 
-    def _query(self, q, tables, lens, max_len, scale, window, out):
-        if q.dim() != 3 or q.shape[0] != tables.shape[0] or q.shape[2] != self.head_dim or q.device != self.device:
-            _bad(f"q: [{tables.shape[0]}, query heads, {self.head_dim}] on {self.device} expected, not {list(q.shape)} on {q.device}")
-        if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
-            _bad("out: shape and type of q expected")
-        for t in (q, out):
-            if t is not None and t.numel() and t.stride(2) != 1:
-                _bad("q, out: the elements of a head must lie next to each other")
-        _on(self.device, self.torch.int32, (q.shape[0],), lens=lens)
-        return NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), q.shape[1], q.stride(0), q.stride(1), out.stride(0) if out is not None else 0,
-                            out.stride(1) if out is not None else 0, lens.data_ptr(), max_len, window,
+    def _query(self, q, n, lens, max_len, scale, window, out):
+        row, head = self._strides(q, n, q.dtype, "q")
+        o_row = o_head = 0
+        if out is not None:
+            o_row, o_head = self._strides(out, n, q.dtype, "out")
+            if out.shape != q.shape:
+                _bad("out: shape of q expected")
+        if lens.dtype != self._i32 or lens.shape != (n,) or lens.device != self.device or not lens.is_contiguous():
+            _bad(f"lens: contiguous int32 [{n}] on {self.device} expected, not {lens.dtype} {list(lens.shape)} on {lens.device}")
+        return NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), q.shape[1], row, head, o_row, o_head, lens.data_ptr(), max_len, window,
                             self.head_dim ** -0.5 if scale is None else scale)
+
+    def _attention_bytes(self, table, query):
+        n = ctypes.c_size_t()
+        _check(lib().nnc_page_attention_workspace(self._desc, ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
+        return n.value
 
     def attention_workspace(self, q, tables, lens, max_len: int = 0, window: int = 0) -> int:
         """Bytes of workspace of the same call of `attention`."""
-        n = ctypes.c_size_t()
-        query, table = self._query(q, tables, lens, max_len, None, window, None), self._table(tables)
-        _check(lib().nnc_page_attention_workspace(ctypes.byref(self.desc), ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
-        return n.value
+        table = self._table(tables)
+        return self._attention_bytes(table, self._query(q, table.n_seqs, lens, max_len, None, window, None))
 
     def attention(self, layer: int, q, tables, lens, max_len: int = 0, scale: float | None = None, window: int = 0, out=None, workspace=None):
         """One query row per sequence, q [sequences, query heads, head_dim], against the first lens[i] (int32) cached positions
@@ -360,16 +375,16 @@ class Pages:
         that many last positions (0: all).  workspace: a tensor of attention_workspace bytes instead of a new one."""
         if out is None:
             out = self.torch.empty_like(q, memory_format=self.torch.contiguous_format)
-        query, table = self._query(q, tables, lens, max_len, scale, window, out), self._table(tables)
-        with _Here(self.device) as here:
-            if workspace is None:
-                n = ctypes.c_size_t()
-                _check(lib().nnc_page_attention_workspace(ctypes.byref(self.desc), ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
-                workspace = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device) if n.value else None
-            elif workspace.device != self.device or not workspace.is_contiguous():
-                _bad("workspace: contiguous memory of the pool's device expected")
-            size = workspace.numel() * workspace.element_size() if workspace is not None else 0
-            _check(lib().nnc_page_attention(ctypes.byref(self.desc), layer, ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size, here.stream))
+        table = self._table(tables)
+        query = self._query(q, table.n_seqs, lens, max_len, scale, window, out)
+        if workspace is None:
+            size = self._attention_bytes(table, query)
+            workspace = self.torch.empty(size, dtype=self.torch.uint8, device=self.device) if size else None
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            _bad("workspace: contiguous memory of the pool's device expected")
+        else:
+            size = workspace.numel() * workspace.element_size()
+        _enqueue(self.device, lib().nnc_page_attention, self._desc, layer, ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size)
         return out
 
     def reorder(self, before, after, lens, parents):
@@ -378,14 +393,13 @@ class Pages:
         if parents.dim() != 2:
             _bad("parents: [groups, width] expected")
         table = self._table(before, "before")
-        _on(self.device, self.torch.int32, before.shape, after=after)
-        _on(self.device, self.torch.int32, (before.shape[0],), lens=lens)
-        _on(self.device, self.torch.int32, parents.shape, parents=parents)
-        if parents.numel() != before.shape[0]:
-            _bad(f"parents: {before.shape[0]} beams expected, not {list(parents.shape)}")
-        with _Here(self.device) as here:
-            _check(lib().nnc_page_reorder(ctypes.byref(self.desc), ctypes.byref(table), after.data_ptr(), lens.data_ptr(), parents.data_ptr(),
-                                          parents.shape[1], here.stream))
+        _on(self.device, self._i32, before.shape, after=after)
+        _on(self.device, self._i32, (table.n_seqs,), lens=lens)
+        _on(self.device, self._i32, parents.shape, parents=parents)
+        if parents.numel() != table.n_seqs:
+            _bad(f"parents: {table.n_seqs} beams expected, not {list(parents.shape)}")
+        _enqueue(self.device, lib().nnc_page_reorder, self._desc, ctypes.byref(table), after.data_ptr(), lens.data_ptr(), parents.data_ptr(),
+                 parents.shape[1])
 
 
 def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
@@ -395,25 +409,27 @@ def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
     import torch
     if logits.dim() != 3 or logits.device.type != "cuda":
         _bad("logits: [groups, width, vocab] in device memory expected")
-    g, w, v = logits.shape
-    if logits.numel() and (logits.stride(2) != 1 or (g > 1 and logits.stride(0) != w * logits.stride(1))):
+    (g, w, v), (between, row, one), device = logits.shape, logits.stride(), logits.device
+    if g and w and (one != 1 or (g > 1 and between != w * row)):
         _bad("logits: rows of adjacent elements, one distance between all rows, expected")
-    _on(logits.device, torch.float32, (g, w), scores=scores)
     if finished is not None and finished.dtype != torch.bool:
         _bad("finished: bool expected")
-    _on(logits.device, torch.bool, (g, w), finished=finished)
-    with _Here(logits.device) as here:
-        tokens, parents = (torch.empty((g, w), dtype=torch.int32, device=logits.device) for _ in range(2))
-        out, ended = torch.empty_like(scores), torch.empty((g, w), dtype=torch.bool, device=logits.device)
-        beam = NncBeam(logits.data_ptr(), _dtype_of(logits), logits.stride(1), g, w, v, scores.data_ptr(), _ptr(finished), eos, tokens.data_ptr(),
-                       parents.data_ptr(), out.data_ptr(), ended.data_ptr())
-        if workspace is None:
-            n = ctypes.c_size_t()
-            _check(lib().nnc_beam_select_workspace(ctypes.byref(beam), ctypes.byref(n)))
-            workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
-        elif workspace.device != logits.device or not workspace.is_contiguous():
-            _bad("workspace: contiguous memory of the logits' device expected")
-        _check(lib().nnc_beam_select(ctypes.byref(beam), _ptr(workspace), workspace.numel() * workspace.element_size(), here.stream))
+    _on(device, torch.float32, (g, w), scores=scores)
+    _on(device, torch.bool, (g, w), finished=finished)
+    tokens = torch.empty((g, w), dtype=torch.int32, device=device)
+    parents, out, ended = torch.empty_like(tokens), torch.empty_like(scores), torch.empty_like(scores, dtype=torch.bool)
+    beam = NncBeam(logits.data_ptr(), _dtype_of(logits), row, g, w, v, scores.data_ptr(), _ptr(finished), eos, tokens.data_ptr(),
+                   parents.data_ptr(), out.data_ptr(), ended.data_ptr())
+    if workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib().nnc_beam_select_workspace(ctypes.byref(beam), ctypes.byref(n)))
+        size = n.value
+        workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _bad("workspace: contiguous memory of the logits' device expected")
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _enqueue(device, lib().nnc_beam_select, ctypes.byref(beam), workspace.data_ptr(), size)
     return tokens, parents, out, ended
 
 

@@ -1,11 +1,13 @@
 // Selection of a beam search: the `width` best of width x vocabulary continuations of every group.
 //   score(w, v) = scores[w] + logit(w, v) - log sum_u e^(logit(w, u))
-// Two kernels.  k_beam_scan reads the logits once: every workgroup takes TILE elements of one beam and leaves their
-// maximum m, sum of e^(x - m) and `width` largest as sortable keys.  k_beam_pick, a workgroup per group, makes the log-sum
-// of every beam, that beam's best and then the group's.  Within a beam the order of scores is the order of logits, so the
-// scan needs no scores; scores of different beams are compared in 64 bits, since they may be as close as the logits' own
-// rounding.  Which thread adds what depends on the element's index alone, never on the alignment of a row: beams with equal
-// logits get equal sums, and ties between them go to the lowest index.
+// Two kernels.  k_beam_scan reads the logits once: a wave takes a chunk of a beam's row and leaves its maximum m and the sum
+// of e^(x - m).  k_beam_pick, a workgroup per group, adds the sums up, finds the `width` chunks with the largest maxima and
+// looks for the best continuations in those alone: whatever is not in them is preceded by the maxima of all of them.
+// Within a beam the order of scores is the order of logits; scores of different beams are compared in 64 bits, since they
+// may be as close as the logits' own rounding.  Which lane adds what depends on the element's index alone, never on the
+// alignment of a row: beams with equal logits get equal sums, and ties between them go to the lowest index.
+#include <type_traits>
+
 #include "nnc_internal.h"
 #include "nnc_pages.h"
 
@@ -13,202 +15,299 @@ namespace nnc {
 
 namespace {
 
-constexpr int SCAN_ELEMS = 16;                  // elements of a thread
-constexpr uint32_t TILE = 256 * SCAN_ELEMS;
-constexpr uint32_t MAX_PARTS = 64;              // partial results of a beam
+constexpr uint32_t CHUNK = 1024;           // elements that a wave loads at once, sixteen a lane
+constexpr uint32_t MAX_CHUNKS = 512;       // per row; longer rows have larger chunks, a multiple of this one
+constexpr int PICK_WAVES = 16, LIST = 64;  // waves of a workgroup, candidates that a wave collects
+constexpr float LOG2E = 1.44269504088896341f;
 
 struct SelArgs {
   BeamSelect b;
-  uint32_t parts, tiles;  // per beam; tiles per part
-  float* ms;              // [row][parts][2]
-  uint64_t* keys;         // [row][parts][width]
+  uint32_t chunks, mult;  // of a row; CHUNK elements in each
+  float2* ms;             // [row][chunks] maximum (NaN if the chunk holds one), sum
 };
 
-// Larger value first, then the lower index; NaN above everything; 0 is less than every element's key.
-__device__ __forceinline__ uint64_t sort_key(float x, uint32_t index) {
-  const uint32_t b = __float_as_uint(x + 0.f);  // (-0 counts as 0)
-  const uint32_t o = x != x ? 0xffffffffu : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return ((uint64_t)o << 32) | (0xffffffffu - index);
+// 32 bits that order like the values: NaN above everything, -0 counts as 0; 0 below every value, all ones above (with the lowest
+// index, too, a key stays below 2^64 - 1).
+constexpr uint32_t ORDER_NAN = 0xfffffffeu;
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? ORDER_NAN : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t o = (uint32_t)(k >> 32);
-  if (o == 0xffffffffu) return __uint_as_float(0x7fc00000u);
+__device__ __forceinline__ float value_of(uint32_t o) {
+  if (o == ORDER_NAN) return __uint_as_float(0x7fc00000u);
   return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
+// Larger value first, then the lower index.
+__device__ __forceinline__ uint64_t sort_key(uint32_t order, uint32_t index) { return ((uint64_t)order << 32) | (0xffffffffu - index); }
+
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+  auto get = [](uint32_t x, auto ctrl) __attribute__((always_inline)) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR1>{}));
+  v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR2>{}));
+  v = max(v, get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{}));
+  v = max(v, get(v, std::integral_constant<int, DPP_ROW_MIRROR>{}));
+  auto lane = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)v, i); };
+  return max(max(lane(0), lane(16)), max(lane(32), lane(48)));
+}
+// Largest of 64 bits: the upper halves, then the lower ones of the lanes that have that upper half.
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint64_t u = __shfl_xor((unsigned long long)v, o, 64);
-    v = u > v ? u : v;
-  }
-  return v;
+  const uint32_t hi = wave_umax((uint32_t)(v >> 32));
+  return ((uint64_t)hi << 32) | wave_umax((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
 }
 
+// The lane's sixteen elements of the CHUNK at element c0 of a row, and their indices: runs of VEC neighbours, sixteen bytes.
 template <int DT>
-__device__ __forceinline__ float logit_at(const void* base, int64_t i) {
-  if constexpr (DT == DT_F32) return static_cast<const float*>(base)[i];
-  else if constexpr (DT == DT_BF16) return Bf16::widen(static_cast<const uint16_t*>(base)[i]);
-  else return Fp16::widen(static_cast<const uint16_t*>(base)[i]);
+struct Lane16 {
+  static constexpr int VEC = DT == DT_F32 ? 4 : 8;
+  static __device__ __forceinline__ uint32_t index(uint32_t c0, int lane, int i) { return c0 + (i / VEC) * 64 * VEC + lane * VEC + i % VEC; }
+  // elements past the end: -infinity
+  static __device__ __forceinline__ void load(const void* row, bool wide, uint32_t c0, uint32_t vocab, int lane, float (&x)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16 / VEC; ++j) {
+      const uint32_t at = index(c0, lane, j * VEC);
+      if (wide && at + VEC <= vocab) {
+        if constexpr (DT == DT_F32) {
+          const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(row) + at);
+          x[j * 4] = v.x; x[j * 4 + 1] = v.y; x[j * 4 + 2] = v.z; x[j * 4 + 3] = v.w;
+        } else {
+          using HF = std::conditional_t<DT == DT_BF16, Bf16, Fp16>;
+          const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + at);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[j * 8 + 2 * e] = HF::lo(w[e]);
+            x[j * 8 + 2 * e + 1] = HF::hi(w[e]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          x[j * VEC + e] = -INFINITY;
+          if (at + e < vocab) {
+            if constexpr (DT == DT_F32) x[j * VEC + e] = static_cast<const float*>(row)[at + e];
+            else if constexpr (DT == DT_BF16) x[j * VEC + e] = Bf16::widen(static_cast<const uint16_t*>(row)[at + e]);
+            else x[j * VEC + e] = Fp16::widen(static_cast<const uint16_t*>(row)[at + e]);
+          }
+        }
+      }
+    }
+  }
+};
+template <int DT>
+__device__ __forceinline__ const void* row_of(const SelArgs& a, uint32_t g, uint32_t w, bool& wide) {
+  const char* p = static_cast<const char*>(a.b.logits) + ((int64_t)g * a.b.group + (int64_t)w * a.b.row) * (DT == DT_F32 ? 4 : 2);
+  wide = reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  return p;
 }
 
 template <int DT>
 __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
-  __shared__ uint64_t best[4], kept[BEAM_MAX_WIDTH];
-  __shared__ float rm[4], rs[4];
-  const uint32_t row = blockIdx.y, part = blockIdx.x, width = a.b.width;
-  const uint32_t g = row / width, w = row - g * width;
+  const uint32_t row = blockIdx.y, g = row / a.b.width, w = row - g * a.b.width;
+  const uint32_t chunk = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (chunk >= a.chunks) return;
   // a beam that is not in use, or has ended, has no logits to look at
   if (a.b.scores[row] == -INFINITY || (a.b.finished && a.b.finished[row])) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t base = (int64_t)g * a.b.group + (int64_t)w * a.b.row;
+  const int lane = threadIdx.x & 63;
+  bool wide;
+  const void* p = row_of<DT>(a, g, w, wide);
   float m = -INFINITY, sum = 0.f;
-  if (tid < (int)width) kept[tid] = 0;
-  for (uint32_t tile = 0; tile < a.tiles; ++tile) {
-    const uint64_t t0 = ((uint64_t)part * a.tiles + tile) * TILE;
-    if (t0 >= a.b.vocab) break;
-    float x[SCAN_ELEMS];
-    uint64_t key[SCAN_ELEMS];
+  bool nan = false;
+  for (uint32_t i = 0; i < a.mult; ++i) {
+    const uint64_t c0 = ((uint64_t)chunk * a.mult + i) * CHUNK;
+    if (c0 >= a.b.vocab) break;
+    float x[16];
+    Lane16<DT>::load(p, wide, (uint32_t)c0, a.b.vocab, lane, x);
+    float top = x[0];
 #pragma unroll
-    for (int i = 0; i < SCAN_ELEMS; ++i) {
-      const uint64_t v = t0 + (uint64_t)i * 256 + tid;
-      const bool in = v < a.b.vocab;
-      x[i] = in ? logit_at<DT>(a.b.logits, base + (int64_t)v) : -INFINITY;
-      key[i] = in ? sort_key(x[i], (uint32_t)v) : 0;
-    }
-    float tm = m;
-    bool nan = false;
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
 #pragma unroll
-    for (int i = 0; i < SCAN_ELEMS; ++i) {
-      tm = fmaxf(tm, x[i]);
-      nan |= x[i] != x[i];
-    }
-    const float ts = tm == -INFINITY ? 0.f : tm;
-    sum *= exp2f((m - ts) * 1.44269504088896341f);
+    for (int e = 0; e < 16; ++e) nan |= x[e] != x[e];
+    top = wave_max(fmaxf(top, m));
+    const float base = top == -INFINITY ? 0.f : top;
+    sum *= __builtin_amdgcn_exp2f((m - base) * LOG2E);
 #pragma unroll
-    for (int i = 0; i < SCAN_ELEMS; ++i) sum += exp2f((x[i] - ts) * 1.44269504088896341f);
-    if (nan) sum = NAN;
-    m = tm;
-    // the tile's best join what earlier tiles left
-    uint64_t mine = tid < (int)width ? kept[tid] : 0;
-    __syncthreads();
-    for (uint32_t r = 0; r < width; ++r) {
-      uint64_t top = mine;
-#pragma unroll
-      for (int i = 0; i < SCAN_ELEMS; ++i) top = key[i] > top ? key[i] : top;
-      top = wave_max_u64(top);
-      if (lane == 0) best[wave] = top;
-      __syncthreads();
-      top = best[0];
-      for (int i = 1; i < 4; ++i) top = best[i] > top ? best[i] : top;
-      if (tid == 0) kept[r] = top;
-      if (mine == top) mine = 0;
-#pragma unroll
-      for (int i = 0; i < SCAN_ELEMS; ++i)
-        if (key[i] == top) key[i] = 0;
-      __syncthreads();
-    }
+    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((x[e] - base) * LOG2E);
+    m = top;
   }
-  const float M = wave_max(m), Ms = M == -INFINITY ? 0.f : M;
-  const float S = wave_sum(sum * (m == -INFINITY ? 0.f : exp2f((m - Ms) * 1.44269504088896341f)) + (sum != sum ? NAN : 0.f));
-  if (lane == 0) {
-    rm[wave] = M;
-    rs[wave] = S;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    float bm = -INFINITY;
-    for (int i = 0; i < 4; ++i) bm = fmaxf(bm, rm[i]);
-    const float bs = bm == -INFINITY ? 0.f : bm;
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i) s += rs[i] * (rs[i] == rs[i] ? exp2f((rm[i] - bs) * 1.44269504088896341f) : 1.f);
-    a.ms[((size_t)row * a.parts + part) * 2] = bm;
-    a.ms[((size_t)row * a.parts + part) * 2 + 1] = s;
-  }
-  if (tid < (int)width) a.keys[((size_t)row * a.parts + part) * width + tid] = kept[tid];
+  sum = wave_sum(sum);
+  if (__any(nan)) m = NAN;
+  if (lane == 0) a.ms[(size_t)row * a.chunks + chunk] = make_float2(m, sum);
 }
 
-// One wave per beam makes its list of up to `width` (score, token); then the first wave takes the lists' heads in turn.
-__global__ __launch_bounds__(1024) void k_beam_pick(SelArgs a) {
-  __shared__ double score[BEAM_MAX_WIDTH][BEAM_MAX_WIDTH];
-  __shared__ int32_t token[BEAM_MAX_WIDTH][BEAM_MAX_WIDTH];
-  __shared__ uint32_t count[BEAM_MAX_WIDTH];
-  __shared__ uint8_t ended[BEAM_MAX_WIDTH];
-  const uint32_t g = blockIdx.x, width = a.b.width;
-  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  for (uint32_t w = threadIdx.x >> 6; w < width; w += waves) {
-    const uint32_t row = g * width + w;
-    const float start = a.b.scores[row];
+// A row is looked at by `share` waves, each of which leaves up to `width` keys; then every thread takes one of those keys and
+// counts how many come before it.  Bound: latency from one end to the other, and the fetching of code that runs once; hence few
+// passes, counting in place of sorting, and one copy of the loop over the elements.
+template <int DT>
+__global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
+  __shared__ uint64_t found[PICK_WAVES][LIST];
+  __shared__ uint64_t keys[BEAM_MAX_WIDTH * BEAM_MAX_WIDTH], rank[BEAM_MAX_WIDTH * BEAM_MAX_WIDTH];  // [list][place]; 0: none
+  __shared__ uint32_t best_chunk[PICK_WAVES][BEAM_MAX_WIDTH];
+  __shared__ double lse[BEAM_MAX_WIDTH];
+  const uint32_t g = blockIdx.x, width = a.b.width, V = a.b.vocab;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t share = width < PICK_WAVES ? PICK_WAVES / width : 1, slots = width * share * width;
+  static_assert(BEAM_MAX_WIDTH * BEAM_MAX_WIDTH <= 64 * PICK_WAVES, "a thread for every key");
+  // scores and ends of a slot's beam, read while nothing has been written (the outputs may be the inputs)
+  const uint32_t my_beam = threadIdx.x / (share * width), my_row = g * width + min(my_beam, width - 1);
+  const float my_start = a.b.scores[my_row];
+  const bool my_end = a.b.finished && a.b.finished[my_row];
+  for (uint32_t l = wave; l < width * share; l += PICK_WAVES) {  // list l: part l % share of beam l / share
+    const uint32_t w = l / share, part = l - w * share, row = g * width + w;
+    uint64_t* list = keys + l * width;
+    if (lane < (int)width) list[lane] = 0;
     const bool done = a.b.finished && a.b.finished[row];
-    if (lane == 0) {
-      ended[w] = done;
-      count[w] = done ? 1u : width < a.b.vocab ? width : a.b.vocab;
-    }
-    if (done) {
-      if (lane == 0) {
-        score[w][0] = start;
-        token[w][0] = a.b.eos;
-      }
+    if (done || a.b.scores[row] == -INFINITY) {
+      // one continuation; or every one of them at -infinity, in order
+      const uint32_t n = part ? 0u : done ? 1u : min(width, V);
+      if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), done ? (uint32_t)a.b.eos : (uint32_t)lane);
       continue;
     }
-    if (start == -INFINITY) {
-      if (lane < (int)width) {
-        score[w][lane] = -INFINITY;
-        token[w][lane] = lane;
-      }
-      continue;
-    }
-    const float* ms = a.ms + (size_t)row * a.parts * 2;
-    const bool has = lane < (int)a.parts;
-    const float m = has ? ms[lane * 2] : -INFINITY, s = has ? ms[lane * 2 + 1] : 0.f;
-    const float M = wave_max(m);
-    double sum = m == -INFINITY ? (double)(s != s ? s : 0.f) : (double)s * exp((double)m - (double)M);
+    // chunks: lane i has chunks i, 64 + i, ...
+    const float2* ms = a.ms + (size_t)row * a.chunks;
+    uint32_t key[MAX_CHUNKS / 64];
+    float2 v[MAX_CHUNKS / 64];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    const double lse = (double)M + log(sum);
-    // the parts' lists are in order: lane i holds list i and moves on when its head is taken
-    const uint64_t* keys = a.keys + (size_t)row * a.parts * width;
-    uint32_t at = 0;
-    uint64_t head = has ? keys[(size_t)lane * width] : 0;
-    for (uint32_t r = 0; r < width; ++r) {
-      const uint64_t top = wave_max_u64(head);
-      if (head == top && top) {
-        const float x = key_value(top);
-        score[w][r] = x == -INFINITY ? (double)x : (double)start + ((double)x - lse);
-        token[w][r] = (int32_t)(0xffffffffu - (uint32_t)top);
-        ++at;
-        head = at < width ? keys[(size_t)lane * width + at] : 0;
+    for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i) {
+      const uint32_t c = i * 64 + lane;
+      v[i] = c < a.chunks ? ms[c] : make_float2(-INFINITY, 0.f);
+      key[i] = c < a.chunks ? order_of(v[i].x) : 0u;
+    }
+    const uint32_t chunks = min(width, a.chunks);
+    uint32_t least = 0, top = 0;
+#pragma unroll 1
+    for (uint32_t r = 0; r < chunks; ++r) {
+      uint32_t k = key[0], c = lane;
+#pragma unroll
+      for (int i = 1; i < (int)(MAX_CHUNKS / 64); ++i)
+        if (key[i] > k) {
+          k = key[i];
+          c = i * 64 + lane;
+        }
+      least = wave_umax(k);
+      const uint32_t at = 0xffffffffu - wave_umax(k == least ? 0xffffffffu - c : 0u);
+#pragma unroll
+      for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i)
+        if (at == (uint32_t)(i * 64 + lane)) key[i] = 0;
+      if (lane == 0) best_chunk[wave][r] = at;
+      if (r == 0) top = least;
+    }
+    if (part == 0) {
+      // (a NaN among the maxima is the largest: M, and with it the sum, is NaN)
+      const float M = value_of(top);
+      double sum = 0.;
+#pragma unroll
+      for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i)
+        if (v[i].x != -INFINITY) sum += (double)v[i].y * (double)__builtin_amdgcn_exp2f((v[i].x - M) * LOG2E);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      if (lane == 0) lse[w] = (double)M + log(sum);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    // This wave's share of those chunks.  COLLECT: the elements that are not below `least`, the smallest of the chunks' maxima
+    // (`width` elements are not).  Where that are more than LIST (large values side by side) or there are fewer chunks than
+    // places, LANES raises it to the width-th largest of the lanes' maxima.  PLACES, for many equal values: all elements
+    // once more for every place.
+    bool wide;
+    const void* p = row_of<DT>(a, g, w, wide);
+    enum { LANES, COLLECT, PLACES } mode = a.chunks < width ? LANES : COLLECT;
+    if (a.chunks < width) least = 0;
+    bool raised = false;
+    uint32_t n = 0, place = 0;
+    uint64_t below = ~0ull;
+    while (true) {
+      uint64_t best = 0;
+      uint32_t mine = 0;
+      n = 0;
+#pragma unroll 1
+      for (uint32_t r = part; r < chunks; r += share)
+#pragma unroll 1
+        for (uint32_t i = 0; i < a.mult; ++i) {
+          const uint64_t c0 = ((uint64_t)best_chunk[wave][r] * a.mult + i) * CHUNK;
+          if (c0 >= V) break;
+          float x[16];
+          Lane16<DT>::load(p, wide, (uint32_t)c0, V, lane, x);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t at = Lane16<DT>::index((uint32_t)c0, lane, e), o = order_of(x[e]);
+            const bool in = at < V && o >= least;
+            const uint64_t who = __ballot(in);
+            if (!who) continue;
+            const uint64_t t = sort_key(o, at);
+            if (mode == COLLECT) {
+              const uint32_t to = n + __popcll(who & ((1ull << lane) - 1));
+              if (in && to < LIST) found[wave][to] = t;
+              n += __popcll(who);
+            } else if (in) {
+              mine = max(mine, o);
+              if (t < below && t > best) best = t;
+            }
+          }
+        }
+      if (mode == COLLECT) {
+        if (n <= LIST) break;
+        mode = raised ? PLACES : LANES;
+      } else if (mode == LANES) {
+        uint32_t nth = 0;
+#pragma unroll 1
+        for (uint32_t r = 0; r < width; ++r) {
+          nth = wave_umax(mine);
+          const uint64_t who = __ballot(mine == nth);
+          if (lane == __ffsll((unsigned long long)who) - 1) mine = 0;
+        }
+        least = max(least, nth);
+        raised = true;
+        mode = COLLECT;
+      } else {
+        below = wave_max_u64(best);
+        if (lane == 0) list[place] = below;
+        if (!below || ++place == width) break;
       }
+    }
+    if (mode == COLLECT) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const uint64_t k = lane < (int)n ? found[wave][lane] : 0;
+      uint32_t before = 0;
+#pragma unroll 1
+      for (uint32_t i = 0; i < n; ++i) before += found[wave][i] > k;
+      if (k && before < width) list[before] = k;
     }
   }
   __syncthreads();
-  if (threadIdx.x >= 64) return;
-  uint32_t at = 0;
-  const bool in = lane < (int)width;
-  for (uint32_t r = 0; r < width; ++r) {
-    // NaN before everything, then the larger score, then the lower beam
-    bool there = in && at < count[lane];
-    double best = there ? score[lane][at] : 0.;
-    int who = there ? lane : -1;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const double os = __shfl_xor(best, o, 64);
-      const int ow = __shfl_xor(who, o, 64);
-      const bool mn = best != best, on = os != os;
-      const bool take = ow >= 0 && (who < 0 || (on && !mn) || (on == mn && (os > best || ((os == best || on) && ow < who))));
-      if (take) {
-        best = os;
-        who = ow;
-      }
+  // A slot's place: NaN before everything, then the larger score, then the lower beam, then the better key of a beam.
+  const uint32_t t = threadIdx.x;
+  const uint64_t k = t < slots ? keys[t] : 0;
+  double s = 0.;
+  uint64_t o = 0;
+  if (k) {
+    const float x = value_of((uint32_t)(k >> 32));
+    s = my_end ? (double)my_start : x == -INFINITY ? (double)x : (double)my_start + ((double)x - lse[my_beam]);
+    const uint64_t b = (uint64_t)__double_as_longlong(s + 0.);
+    o = s != s ? ~0ull : (b >> 63) ? ~b : b | (1ull << 63);
+  }
+  if (t < slots) rank[t] = o;
+  __syncthreads();
+  if (!k) return;
+  uint32_t before = 0;
+#pragma unroll 4
+  for (uint32_t i = 0; i < slots; ++i) {
+    const uint64_t u = rank[i];
+    before += u > o;
+    if (u == o && i != t) {
+      const uint32_t beam = i / (share * width);
+      before += beam < my_beam || (beam == my_beam && keys[i] > k);
     }
-    if (lane == who) {
-      const uint32_t o = g * width + r;
-      const int32_t v = token[lane][at];
-      a.b.tokens[o] = v;
-      a.b.parents[o] = who;
-      a.b.scores_out[o] = (float)best;
-      if (a.b.finished_out) a.b.finished_out[o] = ended[lane] || v == a.b.eos;
-      ++at;
-    }
+  }
+  if (before < width) {
+    const uint32_t to = g * width + before;
+    const int32_t v = (int32_t)(0xffffffffu - (uint32_t)k);
+    a.b.tokens[to] = v;
+    a.b.parents[to] = (int32_t)my_beam;
+    a.b.scores_out[to] = (float)s;
+    if (a.b.finished_out) a.b.finished_out[to] = my_end || v == a.b.eos;
   }
 }
 
@@ -222,16 +321,17 @@ __global__ void k_beam_start(float* scores, uint8_t* finished, uint32_t n, uint3
 
 }  // namespace
 
-static void scan_shape(uint32_t vocab, uint32_t& parts, uint32_t& tiles) {
-  const uint32_t all = (uint32_t)(((uint64_t)vocab + TILE - 1) / TILE);
-  tiles = (all + MAX_PARTS - 1) / MAX_PARTS;
-  parts = (all + tiles - 1) / tiles;
+static void scan_shape(uint32_t vocab, uint32_t& chunks, uint32_t& mult) {
+  const uint32_t all = (uint32_t)(((uint64_t)vocab + CHUNK - 1) / CHUNK);
+  mult = (all + MAX_CHUNKS - 1) / MAX_CHUNKS;
+  chunks = (all + mult - 1) / mult;
 }
 
 size_t beam_select_bytes(uint32_t rows, uint32_t width, uint32_t vocab) {
-  uint32_t parts, tiles;
-  scan_shape(vocab, parts, tiles);
-  return (size_t)rows * parts * (8 + 8 * (size_t)width);
+  (void)width;
+  uint32_t chunks, mult;
+  scan_shape(vocab, chunks, mult);
+  return (size_t)rows * chunks * sizeof(float2);
 }
 
 hipError_t launch_beam_select(hipStream_t s, const BeamSelect& b, void* workspace) {
@@ -239,16 +339,18 @@ hipError_t launch_beam_select(hipStream_t s, const BeamSelect& b, void* workspac
   if (b.width == 0 || b.width > BEAM_MAX_WIDTH || b.vocab == 0 || (uint64_t)b.n_groups * b.width > 65535) return hipErrorInvalidValue;
   SelArgs a;
   a.b = b;
-  scan_shape(b.vocab, a.parts, a.tiles);
-  const uint32_t rows = b.n_groups * b.width;
-  a.keys = static_cast<uint64_t*>(workspace);
-  a.ms = reinterpret_cast<float*>(a.keys + (size_t)rows * a.parts * b.width);
-  const dim3 grid(a.parts, rows);
-  if (b.dtype == DT_F32) k_beam_scan<DT_F32><<<grid, 256, 0, s>>>(a);
-  else if (b.dtype == DT_BF16) k_beam_scan<DT_BF16><<<grid, 256, 0, s>>>(a);
-  else if (b.dtype == DT_F16) k_beam_scan<DT_F16><<<grid, 256, 0, s>>>(a);
+  scan_shape(b.vocab, a.chunks, a.mult);
+  a.ms = static_cast<float2*>(workspace);
+  const dim3 grid((a.chunks + 3) / 4, b.n_groups * b.width);
+#define NNC_SELECT(DT)                                         \
+  do {                                                         \
+    k_beam_scan<DT><<<grid, 256, 0, s>>>(a);                   \
+    k_beam_pick<DT><<<b.n_groups, 64 * PICK_WAVES, 0, s>>>(a); \
+  } while (0)
+  if (b.dtype == DT_F32) NNC_SELECT(DT_F32);
+  else if (b.dtype == DT_BF16) NNC_SELECT(DT_BF16);
+  else if (b.dtype == DT_F16) NNC_SELECT(DT_F16);
   else return hipErrorInvalidValue;
-  k_beam_pick<<<b.n_groups, 64 * (b.width < 16 ? b.width : 16), 0, s>>>(a);
   return hipGetLastError();
 }
 

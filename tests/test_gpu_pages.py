@@ -328,6 +328,24 @@ def test_select_ties_go_to_the_lower_beam_and_token(nnc):
         check_select(nnc, low, torch.zeros((1, 3), device=DEV))
 
 
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("v", [70, 1500, 33000, 600000])
+def test_select_where_the_best_are_neighbours_or_equal(nnc, rows, v):
+    """Sorted rows (the best in one chunk), rows with few different values, rows whose best are all in one lane of the scan."""
+    g, w = 2, 6
+    gen = torch.Generator(device=DEV).manual_seed(v)
+    scores = -torch.rand((g, w), generator=gen, device=DEV) - 1
+    logits = torch.randn((g, w, v), generator=gen, device=DEV)
+    check_select(nnc, logits.sort(-1, descending=True)[0].to(pu.ROWS[rows]), scores)
+    check_select(nnc, logits.sort(-1)[0].to(pu.ROWS[rows]), scores)
+    check_select(nnc, (logits * 0.4).round().to(pu.ROWS[rows]), scores)
+    check_select(nnc, torch.full_like(logits, 1.25).to(pu.ROWS[rows]), scores)
+    stripe = logits.clone()
+    stripe[:, :, 8:v:256] += 20
+    stripe[:, :, 9:v:256] += 20
+    check_select(nnc, stripe.to(pu.ROWS[rows]), scores)
+
+
 def test_select_shows_a_failed_beam(nnc):
     logits = torch.randn((2, 3, 5000), device=DEV)
     scores = torch.full((2, 3), -1.0, device=DEV)
