@@ -16,8 +16,8 @@ namespace nnc {
 namespace {
 
 constexpr uint32_t CHUNK = 1024;           // elements that a wave loads at once, sixteen a lane
-constexpr uint32_t MAX_CHUNKS = 512;       // per row; longer rows have larger chunks, a multiple of this one
-constexpr int PICK_WAVES = 16, LIST = 64;  // waves of a workgroup, candidates that a wave collects
+constexpr uint32_t MAX_CHUNKS = 256;       // per row; longer rows have larger chunks, a multiple of this one
+constexpr int PICK_WAVES = 16, LIST = 64, BATCH = 4;  // waves of a workgroup, candidates that a wave collects, loads of a wave at once
 constexpr float LOG2E = 1.44269504088896341f;
 
 struct SelArgs {
@@ -136,76 +136,95 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
   if (lane == 0) a.ms[(size_t)row * a.chunks + chunk] = make_float2(m, sum);
 }
 
-// A row is looked at by `share` waves, each of which leaves up to `width` keys; then every thread takes one of those keys and
-// counts how many come before it.  Bound: latency from one end to the other, and the fetching of code that runs once; hence few
-// passes, counting in place of sorting, and one copy of the loop over the elements.
+// First a wave for every beam finds its best chunks (another one its log-sum), then `share` waves look into them and leave up to
+// `width` keys each, then a place is found for every key by counting those that come before it.  Bound: latency and, with sixteen
+// waves on one CU, the issue of instructions; so what one wave can find is not found by all, and an element that is no candidate
+// costs a comparison.
 template <int DT>
 __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
+  constexpr int KEYS = MAX_CHUNKS / 64, SLOTS = BEAM_MAX_WIDTH * BEAM_MAX_WIDTH;
   __shared__ uint64_t found[PICK_WAVES][LIST];
-  __shared__ uint64_t keys[BEAM_MAX_WIDTH * BEAM_MAX_WIDTH], rank[BEAM_MAX_WIDTH * BEAM_MAX_WIDTH];  // [list][place]; 0: none
-  __shared__ uint32_t best_chunk[PICK_WAVES][BEAM_MAX_WIDTH];
+  __shared__ uint64_t keys[SLOTS], rank[SLOTS];  // [list][place]; 0: none
+  __shared__ uint32_t best_chunk[BEAM_MAX_WIDTH][BEAM_MAX_WIDTH], floor_of[BEAM_MAX_WIDTH];
   __shared__ double lse[BEAM_MAX_WIDTH];
+  __shared__ float start[BEAM_MAX_WIDTH];
+  __shared__ uint32_t state[BEAM_MAX_WIDTH];  // 0: a running beam, 1: ended, 2: not in use
+  __shared__ uint32_t n_found[PICK_WAVES], places[SLOTS], winner[BEAM_MAX_WIDTH];
   const uint32_t g = blockIdx.x, width = a.b.width, V = a.b.vocab;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t share = width < PICK_WAVES ? PICK_WAVES / width : 1, slots = width * share * width;
-  static_assert(BEAM_MAX_WIDTH * BEAM_MAX_WIDTH <= 64 * PICK_WAVES, "a thread for every key");
-  // scores and ends of a slot's beam, read while nothing has been written (the outputs may be the inputs)
-  const uint32_t my_beam = threadIdx.x / (share * width), my_row = g * width + min(my_beam, width - 1);
-  const float my_start = a.b.scores[my_row];
-  const bool my_end = a.b.finished && a.b.finished[my_row];
-  for (uint32_t l = wave; l < width * share; l += PICK_WAVES) {  // list l: part l % share of beam l / share
+  const uint32_t share = width < PICK_WAVES ? PICK_WAVES / width : 1, lists = width * share, slots = lists * width;
+  const uint32_t chunks = min(width, a.chunks);
+  static_assert(SLOTS <= 64 * PICK_WAVES, "a thread for every key");
+  if (threadIdx.x < slots) keys[threadIdx.x] = 0;
+  for (uint32_t l = wave; l < lists; l += PICK_WAVES) {  // list l: part l % share of beam l / share
     const uint32_t w = l / share, part = l - w * share, row = g * width + w;
-    uint64_t* list = keys + l * width;
-    if (lane < (int)width) list[lane] = 0;
-    const bool done = a.b.finished && a.b.finished[row];
-    if (done || a.b.scores[row] == -INFINITY) {
-      // one continuation; or every one of them at -infinity, in order
-      const uint32_t n = part ? 0u : done ? 1u : min(width, V);
-      if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), done ? (uint32_t)a.b.eos : (uint32_t)lane);
-      continue;
-    }
-    // chunks: lane i has chunks i, 64 + i, ...
+    if (part > 1) continue;
+    // chunks: lane i has chunks i, 64 + i, ... (of a beam without logits they are numbers that nobody uses)
     const float2* ms = a.ms + (size_t)row * a.chunks;
-    uint32_t key[MAX_CHUNKS / 64];
-    float2 v[MAX_CHUNKS / 64];
+    float2 v[KEYS];
 #pragma unroll
-    for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i) {
+    for (int i = 0; i < KEYS; ++i) {
       const uint32_t c = i * 64 + lane;
       v[i] = c < a.chunks ? ms[c] : make_float2(-INFINITY, 0.f);
-      key[i] = c < a.chunks ? order_of(v[i].x) : 0u;
     }
-    const uint32_t chunks = min(width, a.chunks);
-    uint32_t least = 0, top = 0;
-#pragma unroll 1
-    for (uint32_t r = 0; r < chunks; ++r) {
-      uint32_t k = key[0], c = lane;
-#pragma unroll
-      for (int i = 1; i < (int)(MAX_CHUNKS / 64); ++i)
-        if (key[i] > k) {
-          k = key[i];
-          c = i * 64 + lane;
-        }
-      least = wave_umax(k);
-      const uint32_t at = 0xffffffffu - wave_umax(k == least ? 0xffffffffu - c : 0u);
-#pragma unroll
-      for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i)
-        if (at == (uint32_t)(i * 64 + lane)) key[i] = 0;
-      if (lane == 0) best_chunk[wave][r] = at;
-      if (r == 0) top = least;
+    const float begin = a.b.scores[row];
+    const uint32_t st = a.b.finished && a.b.finished[row] ? 1u : begin == -INFINITY ? 2u : 0u;
+    if (part == 0 && lane == 0) {
+      start[w] = begin;
+      state[w] = st;
     }
+    if (st) continue;
     if (part == 0) {
-      // (a NaN among the maxima is the largest: M, and with it the sum, is NaN)
-      const float M = value_of(top);
-      double sum = 0.;
+      uint32_t key[KEYS], least = 0;
 #pragma unroll
-      for (int i = 0; i < (int)(MAX_CHUNKS / 64); ++i)
-        if (v[i].x != -INFINITY) sum += (double)v[i].y * (double)__builtin_amdgcn_exp2f((v[i].x - M) * LOG2E);
+      for (int i = 0; i < KEYS; ++i) key[i] = i * 64 + lane < (int)a.chunks ? order_of(v[i].x) : 0u;
+#pragma unroll 1
+      for (uint32_t r = 0; r < chunks; ++r) {
+        uint32_t k = key[0], c = lane;
+#pragma unroll
+        for (int i = 1; i < KEYS; ++i)
+          if (key[i] > k) {
+            k = key[i];
+            c = i * 64 + lane;
+          }
+        least = wave_umax(k);
+        const uint64_t who = __ballot(k == least);
+        const uint32_t at = who & (who - 1) ? 0xffffffffu - wave_umax(k == least ? 0xffffffffu - c : 0u)
+                                            : (uint32_t)__builtin_amdgcn_readlane((int)c, __ffsll((unsigned long long)who) - 1);
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i)
+          if (at == (uint32_t)(i * 64 + lane)) key[i] = 0;
+        if (lane == 0) best_chunk[w][r] = at;
+      }
+      if (lane == 0) floor_of[w] = least;
+    }
+    if (part == 1 || share == 1) {
+      bool nan = false;
+      float M = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < KEYS; ++i) {
+        M = fmaxf(M, v[i].x);
+        nan |= v[i].x != v[i].x;
+      }
+      M = wave_max(M);
+      double sum = nan ? NAN : 0.;
+#pragma unroll
+      for (int i = 0; i < KEYS; ++i)
+        if (v[i].x > -INFINITY) sum += (double)(v[i].y * __builtin_amdgcn_exp2f((v[i].x - M) * LOG2E));
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
       if (lane == 0) lse[w] = (double)M + log(sum);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  for (uint32_t l = wave; l < lists; l += PICK_WAVES) {
+    const uint32_t w = l / share, part = l - w * share, st = state[w];
+    uint64_t* list = keys + l * width;
+    if (st) {  // one continuation; or every one of them at -infinity, in order
+      const uint32_t n = part ? 0u : st == 1 ? 1u : min(width, V);
+      if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), st == 1 ? (uint32_t)a.b.eos : (uint32_t)lane);
+      continue;
+    }
     // This wave's share of those chunks.  COLLECT: the elements that are not below `least`, the smallest of the chunks' maxima
     // (`width` elements are not).  Where that are more than LIST (large values side by side) or there are fewer chunks than
     // places, LANES raises it to the width-th largest of the lanes' maxima.  PLACES, for many equal values: all elements
@@ -213,40 +232,53 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
     bool wide;
     const void* p = row_of<DT>(a, g, w, wide);
     enum { LANES, COLLECT, PLACES } mode = a.chunks < width ? LANES : COLLECT;
-    if (a.chunks < width) least = 0;
+    uint32_t least = a.chunks < width ? 0u : floor_of[w];
+    const uint32_t pieces = (chunks - min(part, chunks) + share - 1) / share * a.mult;
     bool raised = false;
-    uint32_t n = 0, place = 0;
+    uint32_t place = 0, n;
     uint64_t below = ~0ull;
     while (true) {
+      const float floor = value_of(least);  // (least 0: a NaN, below which no value is)
       uint64_t best = 0;
       uint32_t mine = 0;
-      n = 0;
+      if (lane == 0) n_found[wave] = 0;
+      // (BATCH loads on their way at once)
 #pragma unroll 1
-      for (uint32_t r = part; r < chunks; r += share)
-#pragma unroll 1
-        for (uint32_t i = 0; i < a.mult; ++i) {
-          const uint64_t c0 = ((uint64_t)best_chunk[wave][r] * a.mult + i) * CHUNK;
-          if (c0 >= V) break;
-          float x[16];
-          Lane16<DT>::load(p, wide, (uint32_t)c0, V, lane, x);
+      for (uint32_t q0 = 0; q0 < pieces; q0 += BATCH) {
+        float x[BATCH][16];
+        uint32_t first[BATCH];
+        bool there[BATCH];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+          const uint32_t q = min(q0 + j, pieces - 1), of = q / a.mult;  // (without a branch: it would keep the loads apart)
+          const uint64_t c0 = ((uint64_t)best_chunk[w][part + of * share] * a.mult + (q - of * a.mult)) * CHUNK;
+          first[j] = c0 < V ? (uint32_t)c0 : 0u;
+          there[j] = q0 + j < pieces && c0 < V;
+          Lane16<DT>::load(p, wide, first[j], V, lane, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+          if (!there[j]) continue;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const uint32_t at = Lane16<DT>::index((uint32_t)c0, lane, e), o = order_of(x[e]);
-            const bool in = at < V && o >= least;
-            const uint64_t who = __ballot(in);
-            if (!who) continue;
+            if (x[j][e] < floor) continue;
+            const uint32_t at = Lane16<DT>::index(first[j], lane, e), o = order_of(x[j][e]);
+            if (at >= V || o < least) continue;
             const uint64_t t = sort_key(o, at);
             if (mode == COLLECT) {
-              const uint32_t to = n + __popcll(who & ((1ull << lane) - 1));
-              if (in && to < LIST) found[wave][to] = t;
-              n += __popcll(who);
-            } else if (in) {
+              const uint32_t to = atomicAdd(&n_found[wave], 1u);
+              if (to < LIST) found[wave][to] = t;
+            } else {
               mine = max(mine, o);
               if (t < below && t > best) best = t;
             }
           }
         }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
       if (mode == COLLECT) {
+        n = n_found[wave];
         if (n <= LIST) break;
         mode = raised ? PLACES : LANES;
       } else if (mode == LANES) {
@@ -267,8 +299,6 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
       }
     }
     if (mode == COLLECT) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
       const uint64_t k = lane < (int)n ? found[wave][lane] : 0;
       uint32_t before = 0;
 #pragma unroll 1
@@ -277,37 +307,46 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
     }
   }
   __syncthreads();
-  // A slot's place: NaN before everything, then the larger score, then the lower beam, then the better key of a beam.
-  const uint32_t t = threadIdx.x;
+  // A slot's place: NaN before everything, then the larger score, then the lower beam, then the better key of a beam.  Every slot
+  // is compared by several threads, with a part of the others each.
+  uint32_t pow2 = 64;
+  while (pow2 < slots) pow2 *= 2;
+  const uint32_t t = threadIdx.x & (pow2 - 1), seg = threadIdx.x / pow2, segs = 64 * PICK_WAVES / pow2;
+  const uint32_t w = t / (share * width);
   const uint64_t k = t < slots ? keys[t] : 0;
-  double s = 0.;
   uint64_t o = 0;
   if (k) {
     const float x = value_of((uint32_t)(k >> 32));
-    s = my_end ? (double)my_start : x == -INFINITY ? (double)x : (double)my_start + ((double)x - lse[my_beam]);
+    const double s = state[w] == 1 ? (double)start[w] : x == -INFINITY ? (double)x : (double)start[w] + ((double)x - lse[w]);
     const uint64_t b = (uint64_t)__double_as_longlong(s + 0.);
     o = s != s ? ~0ull : (b >> 63) ? ~b : b | (1ull << 63);
   }
-  if (t < slots) rank[t] = o;
-  __syncthreads();
-  if (!k) return;
-  uint32_t before = 0;
-#pragma unroll 4
-  for (uint32_t i = 0; i < slots; ++i) {
-    const uint64_t u = rank[i];
-    before += u > o;
-    if (u == o && i != t) {
-      const uint32_t beam = i / (share * width);
-      before += beam < my_beam || (beam == my_beam && keys[i] > k);
-    }
+  if (seg == 0 && t < slots) {
+    rank[t] = o;
+    places[t] = 0;
   }
-  if (before < width) {
-    const uint32_t to = g * width + before;
-    const int32_t v = (int32_t)(0xffffffffu - (uint32_t)k);
+  __syncthreads();
+  if (k) {
+    const uint32_t beam0 = w * share * width, beam1 = beam0 + share * width;
+    uint32_t before = 0;
+#pragma unroll 4
+    for (uint32_t i = seg; i < slots; i += segs) {
+      const uint64_t u = rank[i];
+      if (u >= o && i != t) before += u > o || i < beam0 || (i < beam1 && keys[i] > k);
+    }
+    if (before) atomicAdd(&places[t], before);
+  }
+  __syncthreads();
+  if (seg == 0 && k && places[t] < width) winner[places[t]] = t;
+  __syncthreads();
+  if (threadIdx.x < width) {
+    const uint32_t t = winner[threadIdx.x], to = g * width + threadIdx.x, w = t / (share * width);
+    const int32_t v = (int32_t)(0xffffffffu - (uint32_t)keys[t]);
+    const uint64_t o = rank[t], b = (o >> 63) ? o & ~(1ull << 63) : ~o;
     a.b.tokens[to] = v;
-    a.b.parents[to] = (int32_t)my_beam;
-    a.b.scores_out[to] = (float)s;
-    if (a.b.finished_out) a.b.finished_out[to] = my_end || v == a.b.eos;
+    a.b.parents[to] = (int32_t)w;
+    a.b.scores_out[to] = o == ~0ull ? NAN : (float)__longlong_as_double((long long)b);
+    if (a.b.finished_out) a.b.finished_out[to] = state[w] == 1 || v == a.b.eos;
   }
 }
 
