@@ -157,32 +157,43 @@ __global__ __launch_bounds__(256) void k_page_reorder(PageReorder r, uint32_t nt
   const uint32_t b = blockIdx.x - nt;
   const uint32_t chunk = b % nchunks, which = b / nchunks % 2, lh = b / nchunks / 2;
   const uint32_t layer = lh / r.n_kv_heads, head = lh - layer * r.n_kv_heads;
-  auto at = [&](int32_t page) { return (((size_t)layer * r.n_pages + page) * r.n_kv_heads + head) * r.page_tokens; };
-  auto moves = [&](int j) {
-    return j < (int)r.width && src[j] != dst[j] && (uint32_t)src[j] < r.n_pages && (uint32_t)dst[j] < r.n_pages;
-  };
-  const uint32_t bytes = part * r.row_bytes, o = chunk * 4096 + tid * 16;
-  if (o < bytes) {
-    char* base = static_cast<char*>(which ? r.v : r.k);
-    u32x4_v x[W];
+  // (a beam's pages are the same for the whole workgroup: scalar registers, scalar branches)
+  int32_t from[W], to[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j)
-      if (moves(j)) x[j] = *reinterpret_cast<const u32x4_v*>(base + at(src[j]) * r.row_bytes + o);
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-      if (moves(j)) *reinterpret_cast<u32x4_v*>(base + at(dst[j]) * r.row_bytes + o) = x[j];
-  }
-  if (chunk == 0 && r.k_scale) {
-    float* base = which ? r.v_scale : r.k_scale;
-    for (uint32_t i = tid; i < part; i += 256) {
-      float x[W];
-#pragma unroll
-      for (int j = 0; j < W; ++j)
-        if (moves(j)) x[j] = base[at(src[j]) + i];
-#pragma unroll
-      for (int j = 0; j < W; ++j)
-        if (moves(j)) base[at(dst[j]) + i] = x[j];
+  for (int j = 0; j < W; ++j) {
+    from[j] = to[j] = -1;
+    if (j < (int)r.width) {
+      from[j] = __builtin_amdgcn_readfirstlane(src[j]);
+      to[j] = __builtin_amdgcn_readfirstlane(dst[j]);
     }
+    if (from[j] == to[j] || (uint32_t)from[j] >= r.n_pages || (uint32_t)to[j] >= r.n_pages) from[j] = -1;
+  }
+  auto at = [&](int32_t page) { return (((size_t)layer * r.n_pages + page) * r.n_kv_heads + head) * r.page_tokens; };
+  const uint32_t bytes = part * r.row_bytes, o = chunk * 4096 + tid * 16;
+  char* base = static_cast<char*>(which ? r.v : r.k);
+  float* scale = chunk == 0 ? (which ? r.v_scale : r.k_scale) : nullptr;
+  u32x4_v x[W];
+  float y[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+    if (from[j] >= 0) {
+      if (o < bytes) x[j] = *reinterpret_cast<const u32x4_v*>(base + at(from[j]) * r.row_bytes + o);
+      if (scale && tid < part) y[j] = scale[at(from[j]) + tid];
+    }
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+    if (from[j] >= 0) {
+      if (o < bytes) *reinterpret_cast<u32x4_v*>(base + at(to[j]) * r.row_bytes + o) = x[j];
+      if (scale && tid < part) scale[at(to[j]) + tid] = y[j];
+    }
+  if (!scale) return;
+  for (uint32_t i = 256 + tid; i < part; i += 256) {  // pages of more than 256 positions
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (from[j] >= 0) y[j] = scale[at(from[j]) + i];
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (from[j] >= 0) scale[at(to[j]) + i] = y[j];
   }
 }
 
