@@ -82,28 +82,45 @@ __device__ __forceinline__ float page_quotient(float x, float scale, float inv) 
   if (r != 0.f && !(b & 1u) && y != 0.f) y = __uint_as_float((r > 0.f) == (y > 0.f) ? b + 1u : b - 1u);
   return y;
 }
-// four quotients -> four stored bytes
+// An integer 1.5 2^23 + n as a float has n in its low byte, and adding that number rounds to the nearest integer.
+constexpr float PAGE_ROUND = 12582912.f;
+// four quotients -> four stored bytes.  (None exceeds the largest stored value by more than its rounding, which ends there.)
 template <int STORE>
 __device__ __forceinline__ uint32_t page_bytes4(float a, float b, float c, float d) {
   if constexpr (STORE == PS_I8) {
-    auto q = [](float y) __attribute__((always_inline)) {
-      return (uint32_t)(int)fminf(fmaxf(rintf(y), -127.f), 127.f) & 0xffu;
-    };
-    return q(a) | (q(b) << 8) | (q(c) << 16) | (q(d) << 24);
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(b + PAGE_ROUND), __float_as_uint(a + PAGE_ROUND), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(d + PAGE_ROUND), __float_as_uint(c + PAGE_ROUND), 0x04000c0cu);
+    return lo | hi;
   } else {
-    auto q = [](float y) __attribute__((always_inline)) { return fminf(fmaxf(y, -448.f), 448.f); };
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
   }
 }
-// eight values -> eight stored bytes.  A row without a scale (NaN) keeps zeros.
+// Eight values -> eight stored bytes.  A row without a scale (NaN) keeps zeros.  x times the reciprocal of the scale is within
+// 2^-21 of the quotient; only where a border of the stored format is that near (or, for e4m3, the value below the normal
+// XX
 template <int STORE>
 __device__ __forceinline__ uint2 page_bytes8(const float (&x)[8], float scale) {
   if (!(scale == scale)) return make_uint2(0, 0);
-  const float inv = 1.f / scale;
-  float y[8];
+  const float inv = __builtin_amdgcn_rcpf(scale);
+  float y[8], small = INFINITY, off = 0.f;
+  uint32_t border = ~0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = page_quotient(x[i], scale, inv);
+  for (int i = 0; i < 8; ++i) {
+#pragma clang fp contract(off)
+    y[i] = x[i] * inv;
+    if constexpr (STORE == PS_I8) {
+      off = fmaxf(off, fabsf(y[i] - ((y[i] + PAGE_ROUND) - PAGE_ROUND)));
+    } else {
+      border = min(border, (__float_as_uint(y[i]) + 0x80008u) & 0xfffffu);
+      small = fminf(small, fabsf(y[i]));
+    }
+  }
+  const bool near = STORE == PS_I8 ? off >= 0.5f - 0x1p-13f : border <= 16u || small < 0x1p-6f;
+  if (near) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = page_quotient(x[i], scale, inv);
+  }
   return make_uint2(page_bytes4<STORE>(y[0], y[1], y[2], y[3]), page_bytes4<STORE>(y[4], y[5], y[6], y[7]));
 }
 // four stored bytes -> the values they stand for, without their scale (exact)

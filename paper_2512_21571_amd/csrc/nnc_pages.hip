@@ -28,7 +28,7 @@ namespace nnc {
     }                                                                \
   } while (0)
 
-// Largest of LPR (8 or 16) neighbouring lanes, in all of them.
+// Largest of LPR (4 or 8) neighbouring lanes, in all of them.
 template <int LPR>
 __device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
   auto get = [](uint32_t x, auto ctrl) __attribute__((always_inline)) {
@@ -36,66 +36,90 @@ __device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
   };
   v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR1>{}));
   v = max(v, get(v, std::integral_constant<int, DPP_QUAD_XOR2>{}));
-  v = max(v, get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{}));
-  if constexpr (LPR == 16) v = max(v, get(v, std::integral_constant<int, DPP_ROW_MIRROR>{}));
+  if constexpr (LPR == 8) v = max(v, get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{}));
   return v;
 }
 
-// Eight values per thread, head_dim / 8 neighbouring threads per (row, kv head), K in blockIdx.y 0 and V in 1.
-template <int STORE, int DT, int LPR>
-__global__ __launch_bounds__(256) void k_page_append(PagePool p, PageTable t, PageRows r, bool wide) {
+// Sixteen values per thread (elements 8 lane and 8 (LPR + lane) on of a row, so that neighbours move neighbouring bytes),
+// head_dim / 16 neighbouring threads per (row, kv head), K in blockIdx.y 0 and V in 1.
+template <int LPR>
+__device__ __forceinline__ void row_of_thread(const PagePool& p, const FastDiv& by_head, uint32_t& row, uint32_t& head) {
   const uint32_t id = (blockIdx.x * 256u + threadIdx.x) / LPR;
+  row = fdiv(id, by_head);
+  head = id - row * p.n_kv_heads;
+}
+
+template <int STORE, int DT, int LPR>
+__global__ __launch_bounds__(256) void k_page_append(PagePool p, PageTable t, PageRows r, FastDiv by_head, bool wide) {
   const int lane = threadIdx.x % LPR;
-  const uint32_t row = id / p.n_kv_heads, head = id - row * p.n_kv_heads;
+  uint32_t row, head;
+  row_of_thread<LPR>(p, by_head, row, head);
   if (row >= r.n) return;
   const bool is_v = blockIdx.y;
+  // (the row's values are on their way before its place is known)
+  const int64_t from = (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8;
+  float x[2][8];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) load8<DT>(is_v ? r.v : r.k, from + j * LPR * 8, wide, x[j]);
   const int64_t at = page_row(p, t, r.seq ? r.seq[row] : r.seq0, r.pos ? r.pos[row] : r.pos0 + (int32_t)row, head);
   if (at < 0) return;
-  float x[8];
-  load8<DT>(is_v ? r.v : r.k, (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8, wide, x);
   void* pool = is_v ? p.v : p.k;
-  const int64_t e = at * (LPR * 8) + lane * 8;
+  const int64_t e = at * (LPR * 16) + lane * 8;
   if constexpr (page_scaled(STORE)) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[j][i]) & 0x7fffffffu);
     const float scale = page_scale_of(lanes_umax<LPR>(top), STORE);
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + e) = page_bytes8<STORE>(x, scale);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + e + j * LPR * 8) = page_bytes8<STORE>(x[j], scale);
     if (lane == 0) (is_v ? p.v_scale : p.k_scale)[at] = scale;
   } else {
-    store8<STORE>(pool, e, true, x);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) store8<STORE>(pool, e + j * LPR * 8, true, x[j]);
   }
 }
 
 template <int STORE, int DT, int LPR>
-__global__ __launch_bounds__(256) void k_page_read(PagePool p, PageTable t, PageRows r, bool wide) {
-  const uint32_t id = (blockIdx.x * 256u + threadIdx.x) / LPR;
+__global__ __launch_bounds__(256) void k_page_read(PagePool p, PageTable t, PageRows r, FastDiv by_head, bool wide) {
   const int lane = threadIdx.x % LPR;
-  const uint32_t row = id / p.n_kv_heads, head = id - row * p.n_kv_heads;
-  if (row >= r.n) return;
   const bool is_v = blockIdx.y;
   void* out = is_v ? r.v : r.k;
   if (!out) return;
+  uint32_t row, head;
+  row_of_thread<LPR>(p, by_head, row, head);
+  if (row >= r.n) return;
   const int64_t at = page_row(p, t, r.seq ? r.seq[row] : r.seq0, r.pos ? r.pos[row] : r.pos0 + (int32_t)row, head);
-  float x[8];
+  float x[2][8];
   if (at < 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7fc00000u);
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[j][i] = __uint_as_float(0x7fc00000u);
   } else {
     const void* pool = is_v ? p.v : p.k;
-    const int64_t e = at * (LPR * 8) + lane * 8;
+    const int64_t e = at * (LPR * 16) + lane * 8;
     if constexpr (page_scaled(STORE)) {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + e);
       const float scale = (is_v ? p.v_scale : p.k_scale)[at];
-      page_widen4<STORE>(w.x, x);
-      page_widen4<STORE>(w.y, x + 4);
+      uint2 b[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= scale;
+      for (int j = 0; j < 2; ++j) b[j] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + e + j * LPR * 8);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        page_widen4<STORE>(b[j].x, x[j]);
+        page_widen4<STORE>(b[j].y, x[j] + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] *= scale;
+      }
     } else {
-      load8<STORE>(pool, e, true, x);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load8<STORE>(pool, e + j * LPR * 8, true, x[j]);
     }
   }
-  store8<DT>(out, (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8, wide, x);
+  const int64_t to = (int64_t)row * (is_v ? r.v_row : r.k_row) + (int64_t)head * (is_v ? r.v_head : r.k_head) + lane * 8;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) store8<DT>(out, to + j * LPR * 8, wide, x[j]);
 }
 
 // Whether eight elements of every row can be moved sixteen bytes at a time.
@@ -106,13 +130,14 @@ static bool rows_wide(const PageRows& r) {
 }
 
 #define NNC_PAGE_ROWS_LAUNCH(kernel)                                                                                   \
-  const uint64_t threads = (uint64_t)r.n * p.n_kv_heads * (p.head_dim / 8);                                            \
+  const uint64_t threads = (uint64_t)r.n * p.n_kv_heads * (p.head_dim / 16);                                            \
   if (threads == 0) return hipSuccess;                                                                                 \
   if (threads > 0xffffff00ull || (p.head_dim != 64 && p.head_dim != 128)) return hipErrorInvalidValue;                 \
   const dim3 grid((unsigned)((threads + 255) / 256), 2);                                                               \
   const bool wide = rows_wide(r);                                                                                      \
-  NNC_FOR_STORE(p.store, NNC_FOR_ROWS(r.dtype, if (p.head_dim == 128) kernel<STORE, DT, 16><<<grid, 256, 0, s>>>(p, t, r, wide); \
-                                      else kernel<STORE, DT, 8><<<grid, 256, 0, s>>>(p, t, r, wide)));                 \
+  const FastDiv by_head = fast_div(p.n_kv_heads);                                                                      \
+  NNC_FOR_STORE(p.store, NNC_FOR_ROWS(r.dtype, if (p.head_dim == 128) kernel<STORE, DT, 8><<<grid, 256, 0, s>>>(p, t, r, by_head, wide); \
+                                      else kernel<STORE, DT, 4><<<grid, 256, 0, s>>>(p, t, r, by_head, wide)));                 \
   return hipGetLastError()
 
 hipError_t launch_page_append(hipStream_t s, const PagePool& p, const PageTable& t, const PageRows& r) { NNC_PAGE_ROWS_LAUNCH(k_page_append); }
