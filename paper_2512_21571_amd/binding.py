@@ -594,10 +594,15 @@ class Model:
         return x
 
     # -- pages --------------------------------------------------------------------------
+    def _paged(self, pages: Pages, tables):
+        if pages.device != self.stream.device:
+            _bad(f"pages on {pages.device}, the model is on {self.stream.device}")
+        return pages._table(tables)
+
     def pages_store(self, pages: Pages, tables, seq: int, slot: int, pos0: int = 0, n: int | None = None):
         """Positions pos0 .. pos0 + n - 1 (to the slot's end) of a slot's cache to the same positions of a sequence in pages."""
         n = self.slot_len(slot) - pos0 if n is None else n
-        table = pages._table(tables)
+        table = self._paged(pages, tables)
         self._before()
         try:
             _check(lib().nnc_pages_store(self.h, ctypes.byref(pages.desc), ctypes.byref(table), seq, slot, pos0, n))
@@ -606,7 +611,7 @@ class Model:
 
     def decode_step_paged(self, pages: Pages, tables, lens, tokens, max_len: int = 0, want_logits: bool = True):
         """nnc_decode_step_paged: lens and tokens are int32 tensors [sequences]; lens grow by one."""
-        table = pages._table(tables)
+        table = self._paged(pages, tables)
         b = tables.shape[0]
         _on(pages.device, self.torch.int32, (b,), lens=lens, tokens=tokens)
         logits = self._empty((b, self.V), self.torch.float32) if want_logits else None
@@ -624,7 +629,7 @@ class Model:
         """nnc_decode_beam.  Begin: first_logits [groups, vocab] and width.  Go on: tokens, scores, finished [groups, width] of the
         call before.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
         torch, beams = self.torch, tables.shape[0]
-        table = pages._table(tables)
+        table = self._paged(pages, tables)
         if first_logits is not None:
             groups = first_logits.shape[0]
             if width is None or groups * width != beams:
