@@ -300,10 +300,10 @@ class Pages:
             _bad(f"{name}: contiguous int32 [{n}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")
         return x.data_ptr(), 0
 
-    def _strides(self, x, n, dtype, what):
-        """(row stride, head stride) of rows [n, heads, head_dim] whose elements lie next to each other."""
-        if x.dtype != dtype or x.device != self.device or x.dim() != 3 or x.shape[0] != n or x.shape[2] != self.head_dim:
-            _bad(f"{what}: {dtype} [{n}, heads, {self.head_dim}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")
+    def _heads(self, x, n, what):
+        """(row stride, head stride) of a tensor [n, heads, head_dim] whose elements of a head lie next to each other."""
+        if x.dim() != 3 or x.shape[0] != n or x.shape[2] != self.head_dim or x.device != self.device:
+            _bad(f"{what}: [{n}, heads, {self.head_dim}] on {self.device} expected, not {list(x.shape)} on {x.device}")
         row, head, one = x.stride()
         if one != 1 and n:
             _bad(f"{what}: the elements of a head must lie next to each other")
@@ -313,17 +313,19 @@ class Pages:
         some = v if k is None else k
         if some is None:
             _bad("rows: k and v are both None")
-        n, dtype = some.shape[0], some.dtype
-        kr = kh = vr = vh = 0
-        if k is not None:
-            kr, kh = self._strides(k, n, dtype, "k")
-        if v is not None:
-            vr, vh = self._strides(v, n, dtype, "v")
-        if some.shape[1] != self.n_kv_heads or (k is not None and v is not None and v.shape[1] != self.n_kv_heads):
-            _bad(f"rows: {self.n_kv_heads} kv heads expected, not {some.shape[1]}")
+        shape = some.shape
+        n = shape[0] if len(shape) == 3 else 0
+        if len(shape) != 3 or shape[1] != self.n_kv_heads:
+            _bad(f"rows: [rows, {self.n_kv_heads}, {self.head_dim}] expected, not {list(shape)}")
+        row, head = self._heads(some, n, "rows")
+        v_row, v_head = row, head
+        if v is not None and v is not some:
+            if v.shape != shape or v.dtype != some.dtype:
+                _bad(f"rows: k and v of one type and shape expected, not {k.dtype} {list(shape)} and {v.dtype} {list(v.shape)}")
+            v_row, v_head = self._heads(v, n, "rows")
         sp, s0 = self._index(seq, n, "seq")
         pp, p0 = self._index(pos, n, "pos")
-        return NncPageRows(_ptr(k), _ptr(v), _dtype_of(some), kr, kh, vr, vh, n, sp, pp, s0, p0)
+        return NncPageRows(_ptr(k), _ptr(v), _dtype_of(some), row, head, v_row, v_head, n, sp, pp, s0, p0)
 
     def append(self, layer: int, k, v, tables, seq, pos):
         """Write rows [n, kv heads, head_dim] (any strides between rows and heads) as positions `pos` of sequences `seq`: int32
@@ -348,12 +350,12 @@ class Pages:
         return k, v
 
     def _query(self, q, n, lens, max_len, scale, window, out):
-        row, head = self._strides(q, n, q.dtype, "q")
+        row, head = self._heads(q, n, "q")
         o_row = o_head = 0
         if out is not None:
-            o_row, o_head = self._strides(out, n, q.dtype, "out")
-            if out.shape != q.shape:
-                _bad("out: shape of q expected")
+            o_row, o_head = self._heads(out, n, "out")
+            if out.shape != q.shape or out.dtype != q.dtype:
+                _bad("out: type and shape of q expected")
         if lens.dtype != self._i32 or lens.shape != (n,) or lens.device != self.device or not lens.is_contiguous():
             _bad(f"lens: contiguous int32 [{n}] on {self.device} expected, not {lens.dtype} {list(lens.shape)} on {lens.device}")
         return NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), q.shape[1], row, head, o_row, o_head, lens.data_ptr(), max_len, window,
