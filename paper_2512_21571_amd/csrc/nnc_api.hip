@@ -795,7 +795,7 @@ nnc_status persistent_steps(nnc_model* m, const uint32_t* slots, const int32_t* 
 // True once a resident launch has given up on a wait (a lost exchange word): every workgroup
 // of that launch exited early and its outputs are invalid.  The condition is sticky.
 bool resident_failed(nnc_model* m, bool wait) {
-  if (m->mk_error_pending) {
+  if (m->mk_error_pending && !being_captured(m)) {  // (asking an event during a caller's capture would end that)
     hipError_t e = wait ? hipEventSynchronize(m->mk_error_event) : hipEventQuery(m->mk_error_event);
     if (e == hipSuccess) {
       m->mk_error_pending = false;

@@ -211,3 +211,83 @@ def test_a_search_of_one_beam_is_greedy(nnc):
     first = logits.argmax(-1).tolist()
     want, _ = m.decode_greedy([0, 1], first, steps - 1)
     assert toks[0, :, 0].tolist() == first and torch.equal(toks[1:, :, 0], want) and (pars == 0).all()
+
+
+def test_steps_and_searches_in_a_callers_graph(nnc):
+    """A step and a search step captured on the model's stream and replayed over a page boundary, eager work in between, against
+    the same calls on a second model (one max_len for all of them: the same launches)."""
+    shape, prompt, steps, width = SMALL_BF16, 28, 7, 3
+    blob = synth.make_blob(shape, weight_std=0.05)
+    sides = []
+    for _ in range(2):
+        _, m, pages, tables, logits, lens = begin(nnc, shape, 1, width, prompt, steps + 2, torch.bfloat16, blob)
+        toks, _, scores, fin = m.decode_beam(pages, tables, lens, 1, first_logits=logits, width=width)
+        sides.append(dict(m=m, pages=pages, tables=tables, lens=lens, tok=toks[-1].clone(), scores=scores, fin=fin))
+    a, b = sides
+
+    def call(s):
+        return s["m"].decode_beam(s["pages"], s["tables"], s["lens"], 1, tokens=s["tok"], scores=s["scores"], finished=s["fin"], max_len=prompt + steps)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=a["m"].stream):
+        got = call(a)
+    for _ in range(steps - 1):
+        graph.replay()
+        want = call(b)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+        assert torch.equal(a["tables"], b["tables"]) and torch.equal(a["lens"], b["lens"])
+        for s, out in ((a, got), (b, want)):
+            s["tok"].copy_(out[0][-1])
+            s["scores"].copy_(out[2])
+            s["fin"].copy_(out[3])
+        a["m"].decode_step([0], [1])                      # (other work of the model between the replays)
+        torch.cuda.synchronize()
+    step = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(step, stream=a["m"].stream):
+        logits, nxt = a["m"].decode_step_paged(a["pages"], a["tables"], a["lens"], a["tok"].reshape(-1), max_len=prompt + steps + 1)
+    for _ in range(2):
+        step.replay()
+        wl, wn = b["m"].decode_step_paged(b["pages"], b["tables"], b["lens"], b["tok"].reshape(-1), max_len=prompt + steps + 1)
+        torch.cuda.synchronize()
+        assert torch.equal(logits, wl) and torch.equal(nxt, wn) and torch.equal(a["lens"], b["lens"])
+
+
+def test_searches_that_cannot_be_run_are_refused(nnc):
+    shape, prompt = SMALL_BF16, 20
+    blob, m, pages, tables, logits, lens = begin(nnc, shape, 1, 3, prompt, 12, torch.int8)
+    tables0, lens0 = tables.clone(), lens.clone()
+
+    def refused(status, **change):
+        args = dict(n_steps=3, first_logits=logits, width=3, eos=2, max_len=prompt)
+        args.update(change)
+        with pytest.raises(nnc.NncError) as e:
+            m.decode_beam(pages, tables, lens, **args)
+        assert e.value.status == status
+
+    refused(nnc.E_ARG, n_steps=0)
+    refused(nnc.E_ARG, eos=shape.vocab)
+    refused(nnc.E_ARG, eos=-2)
+    refused(nnc.E_ARG, width=2)
+    refused(nnc.E_ARG, first_logits=logits.double())
+    refused(nnc.E_ARG, first_logits=None)
+    refused(nnc.E_KV_FULL, n_steps=14)                    # two pages of 16 hold 32: prompt + 13 passes exceed them
+    refused(nnc.E_KV_FULL, max_len=31)
+    wide = torch.zeros((22, 2), dtype=torch.int32, device=DEV)
+    with pytest.raises(nnc.NncError) as e:                # more beams than a step has columns
+        m.decode_beam(pages, wide, torch.full((22,), 5, dtype=torch.int32, device=DEV), 2, first_logits=logits.expand(2, -1).contiguous(), width=11)
+    assert e.value.status == nnc.E_ARG
+    with pytest.raises(nnc.NncError) as e:
+        m.decode_step_paged(pages, wide, torch.full((22,), 5, dtype=torch.int32, device=DEV), torch.zeros(22, dtype=torch.int32, device=DEV))
+    assert e.value.status == nnc.E_ARG
+    layer = nnc.Model(synth.ModelShape("layer", hidden=256, n_layers=2, n_q_heads=4, n_kv_heads=2, head_dim=128, ffn=512, vocab=0,
+                                       has_embed_and_head=False, tied_lm_head=False, dtype=synth.F32),
+                      synth.make_blob(synth.ModelShape("layer", hidden=256, n_layers=2, n_q_heads=4, n_kv_heads=2, head_dim=128, ffn=512, vocab=0,
+                                                       has_embed_and_head=False, tied_lm_head=False, dtype=synth.F32)), 1, 32)
+    with pytest.raises(nnc.NncError) as e:
+        layer.decode_step_paged(pages, tables, lens, torch.zeros(3, dtype=torch.int32, device=DEV))
+    assert e.value.status == nnc.E_STATE
+    torch.cuda.synchronize()
+    assert torch.equal(tables, tables0) and torch.equal(lens, lens0)   # nothing was enqueued

@@ -346,6 +346,18 @@ def test_select_where_the_best_are_neighbours_or_equal(nnc, rows, v):
     check_select(nnc, stripe.to(pu.ROWS[rows]), scores)
 
 
+def test_select_rows_far_apart(nnc):
+    """Rows more than 2^32 bytes apart."""
+    step = 1_100_000_007
+    base = torch.empty(step + 6000, device=DEV)
+    logits = base.as_strided((2, 1, 5000), (step, step, 1))
+    for g in range(2):
+        logits[g, 0].copy_(torch.randn(5000, generator=torch.Generator(device=DEV).manual_seed(g), device=DEV))
+    check_select(nnc, logits, torch.tensor([[-1.0], [-2.0]], device=DEV))
+    with pytest.raises(nnc.NncError):                                      # rows of a group and groups at different distances
+        nnc.beam_select(base.as_strided((2, 2, 100), (1000, 100, 1)), torch.zeros((2, 2), device=DEV))
+
+
 def test_select_shows_a_failed_beam(nnc):
     logits = torch.randn((2, 3, 5000), device=DEV)
     scores = torch.full((2, 3), -1.0, device=DEV)
