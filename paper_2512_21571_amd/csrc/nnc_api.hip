@@ -2050,7 +2050,7 @@ nnc_status nnc_decode_beam(nnc_model* m, const nnc_pages* pages, const nnc_beam_
   const uint32_t passes = run->n_steps - (begin ? 1 : 0);
   uint32_t room = 0;
   if (nnc_status st = paged_room(m, pages, run->max_pages, run->max_len, passes, &room)) return st;
-  if (beam_select_bytes(n, run->width, m->V()) > (size_t)MAX_COLS * m->c.n_q_heads * m->max_chunks * 132 * 4)
+  if (beam_select_bytes(n, m->V()) > (size_t)MAX_COLS * m->c.n_q_heads * m->max_chunks * 132 * 4)
     return fail(NNC_E_ARG, "the selection of %u beams out of %u tokens does not fit the workspace", n, m->V());
   hipStream_t s = m->stream;
   if (begin) RUN(FAM_BEAM, 0, 0, launch_beam_start(s, run->scores, run->finished, run->n_groups, run->width));

@@ -200,7 +200,7 @@ nnc_status nnc_page_reorder(const nnc_pages* pages, const nnc_page_table* before
 nnc_status nnc_beam_select_workspace(const nnc_beam* beam, size_t* bytes) {
   if (!bytes) return fail(NNC_E_ARG, "bytes is NULL");
   if (nnc_status st = check_select(beam)) return st;
-  *bytes = beam_select_bytes(beam->n_groups * beam->width, beam->width, beam->vocab);
+  *bytes = beam_select_bytes(beam->n_groups * beam->width, beam->vocab);
   return NNC_OK;
 }
 
@@ -215,7 +215,7 @@ nnc_status nnc_beam_select(const nnc_beam* beam, void* workspace, size_t workspa
   if (bad_align(beam->logits, e) || bad_align(beam->scores, 4) || bad_align(beam->tokens_out, 4) || bad_align(beam->parents_out, 4) ||
       bad_align(beam->scores_out, 4))
     return fail(NNC_E_ARG, "beam: not aligned to its elements");
-  const size_t need = beam_select_bytes(beam->n_groups * beam->width, beam->width, beam->vocab);
+  const size_t need = beam_select_bytes(beam->n_groups * beam->width, beam->vocab);
   if (!workspace || workspace_bytes < need || bad_align(workspace, 16))
     return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, need);
   BeamSelect b;

@@ -141,7 +141,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Part& w, const f
 // fp32 pages, on the fp32 matrix instruction (16 x 16 x 4), tiles of 16 positions.  Its operands are one value per lane, so
 // nothing has to be turned: for S^T = K Q^T lane (c, g) loads dims 16 i + 4 g .. + 3 of row c and product j takes element j
 // (the sum over dims may run in any order that both operands share); for O^T = V^T P^T product (i, b, j) takes dim 64 b + 4 c + j of row
-// 4 g + i, whose weight the lane holds.
+// 4 g + i, whose weight the lane holds.  4 sequences of 4096 positions, 8 kv heads: 28 us, 4.8 TB/s.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_tiles) {
   constexpr int LD = D / 16, NB = D / 64, OPITCH = D + 4;
@@ -190,13 +190,18 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
   {
     const int64_t qo = (int64_t)w.seq * a.a.q_row + (int64_t)(w.head0 + min((uint32_t)c, w.nh - 1)) * a.a.q_head;
 #pragma unroll
-    for (int i = 0; i < LD; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t o = qo + i * 16 + g * 4 + j;
-        q[i][j] = a.a.q_dtype == DT_F32 ? static_cast<const float*>(a.a.q)[o]
-                  : a.a.q_dtype == DT_BF16 ? Bf16::widen(static_cast<const uint16_t*>(a.a.q)[o]) : Fp16::widen(static_cast<const uint16_t*>(a.a.q)[o]);
+    for (int i = 0; i < LD; ++i) {
+      const int64_t o = qo + i * 16 + g * 4;
+      if (a.a.q_dtype == DT_F32 && a.q_wide) {
+        const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.a.q) + o);
+        q[i][0] = v.x; q[i][1] = v.y; q[i][2] = v.z; q[i][3] = v.w;
+        continue;
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        q[i][j] = a.a.q_dtype == DT_F32 ? static_cast<const float*>(a.a.q)[o + j]
+                  : a.a.q_dtype == DT_BF16 ? Bf16::widen(static_cast<const uint16_t*>(a.a.q)[o + j]) : Fp16::widen(static_cast<const uint16_t*>(a.a.q)[o + j]);
+    }
   }
   float m = -INFINITY, l = 0.f;
   f32x4_t acc[NB][4];
@@ -313,6 +318,12 @@ __device__ __forceinline__ u32x2_v lds_column4(const char* p) {
 // pieces; weights in three (fp32 output) or two (16-bit output: 2^-17, 1/256 of that output's rounding).  Integers of 8
 // bits and e4m3 values are exact in bf16; their row scales multiply scores and weights.  Binary16 products: weights are
 // carried 2^10 larger and fp32 queries at a power of two near 2^14, so that the pieces are normal numbers.
+//
+// Bound: the cache's bytes, which two workgroups of a CU keep on their way with two tiles of every wave (16 sequences of 4096
+// positions, 8 kv heads, bf16: 51 us, 5.2 TB/s; one of 131072, e4m3: 54 us, 5.1 TB/s; 48 of 1 .. 6000, int8: 68 us, 4.4 TB/s, where
+// the sequences' ends do not meet; a copy reaches 4.85 TB/s).  With the table read in front of the rows of the same tile,
+// which then wait for it, and e4m3 widened by way of fp32, these were 57, 71 and 100.  V^T by LDS, not by a transposed cache: the
+// LDS path moves a few bytes per cycle of its 128, and a row stays a row for append, read and reorder.
 template <int STORE, int D, bool FULL>
 __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_tiles) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
@@ -553,11 +564,8 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
   finish<D>(a, w, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
 }
 
-// Grid: heads, sequences, splits, so that the workgroups of one split go to all XCDs in turn (with the splits innermost, four of them
-// and eight heads, a split stays on two of the eight XCDs, and where most sequences have no fourth one those two idle: 48 sequences
-// of 1 .. 6000 positions as 2 splits 81 -> 68 us), and the splits that few sequences reach come last.
-//
-// Merge of a sequence's records for one query head: eight groups of threads take the splits in turn, four dims a thread.
+// Merge of a sequence's records for one query head: eight groups of threads take the splits in turn, four dims a thread (64 splits
+// of 32 heads 3.9 us; one thread per dim walking 128 of them took 40).
 template <int D>
 __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
   constexpr int NT = 2 * D, LANES = D / 4;
@@ -640,6 +648,9 @@ hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTab
   // queries that enter the product as they are (and an output whose rounding hides two-piece weights)
   const bool lite = !a.packed && a.q_dtype != DT_F32 && a.q_dtype == (p.store == PS_F16 ? DT_F16 : DT_BF16);
   const int ht = (a.n_q_heads / (int)p.n_kv_heads + 15) / 16;
+  // Heads, sequences, splits, so that the workgroups of one split go to all XCDs in turn (with the splits innermost, four of them and
+  // eight heads, a split stays on two of the eight XCDs, and where most sequences have no fourth one those two idle: 48 sequences
+  // of 1 .. 6000 positions as 2 splits 81 -> 68 us), and the splits that few sequences reach come last.
   const dim3 mc(p.n_kv_heads * ht, t.n_seqs, plan.splits);
 #define NNC_ATTN_CASE(ST)                                                                  \
   case ST:                                                                                 \

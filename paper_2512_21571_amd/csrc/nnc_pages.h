@@ -269,7 +269,7 @@ struct BeamSelect {
   float* scores_out;
   uint8_t* finished_out;
 };
-size_t beam_select_bytes(uint32_t rows, uint32_t width, uint32_t vocab);
+size_t beam_select_bytes(uint32_t rows, uint32_t vocab);
 hipError_t launch_beam_select(hipStream_t s, const BeamSelect& b, void* workspace);
 
 // ---- decode steps of a model over pages ------------------------------------------------------------------------
