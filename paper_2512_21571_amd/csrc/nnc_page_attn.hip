@@ -52,19 +52,28 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, uint32_t seq, uint3
   else static_cast<uint16_t*>(a.a.out)[o] = (uint16_t)(a.a.q_dtype == DT_BF16 ? Bf16::bits(v) : Fp16::bits(v));
 }
 
-// Where a workgroup is: heads head0 .. + nh - 1 of one kv head, positions begin .. end - 1 of a sequence.
-struct Part {
-  uint32_t split, seq, kvh, nh, head0, begin, end;
+// A workgroup's heads: head0 .. + nh - 1 of one kv head.
+struct Heads {
+  uint32_t kvh, head0, nh;
+};
+__device__ __forceinline__ Heads heads_of(const AttnArgs& a, uint32_t head_tiles) {
+  Heads h;
+  h.kvh = blockIdx.x / head_tiles;
+  const uint32_t G = a.a.n_q_heads / a.p.n_kv_heads, h0 = (blockIdx.x - h.kvh * head_tiles) * 16;
+  h.nh = min(16u, G - h0);
+  h.head0 = h.kvh * G + h0;
+  return h;
+}
+// ... and positions begin .. end - 1 of a sequence.
+struct Part : Heads {
+  uint32_t split, seq, begin, end;
   bool bad, idle;
 };
-__device__ __forceinline__ Part part_of(const AttnArgs& a, uint32_t head_tiles) {
+__device__ __forceinline__ Part part_of(const AttnArgs& a, const Heads& h) {
   Part w;
+  static_cast<Heads&>(w) = h;
   w.split = blockIdx.z;
   w.seq = blockIdx.y;
-  w.kvh = blockIdx.x / head_tiles;
-  const uint32_t G = a.a.n_q_heads / a.p.n_kv_heads, h0 = (blockIdx.x - w.kvh * head_tiles) * 16;
-  w.nh = min(16u, G - h0);
-  w.head0 = w.kvh * G + h0;
   const Reach r = reach(a, w.seq);
   w.begin = r.lo + w.split * a.plan.chunk;
   w.end = min(r.hi, w.begin + a.plan.chunk);
@@ -163,13 +172,18 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
 #pragma unroll
     for (int i = 0; i < 4; ++i) find.look(p0 + g * 4 + i, t.page[i], t.row[i]);
   };
-  // (the table is asked before the sequence's length is known, unless a window moves the first position)
-  Where p;
-  if (!a.a.window) look(p, blockIdx.z * a.plan.chunk + wave * 16);
-  const Part w = part_of(a, head_tiles);
+  Where here, next;
+  if (!a.a.window) {
+    look(here, blockIdx.z * a.plan.chunk + wave * 16);
+    look(next, blockIdx.z * a.plan.chunk + wave * 16 + 64);
+  }
+  const Part w = part_of(a, heads_of(a, head_tiles));
   if (w.idle) return;
   uint32_t p0 = w.begin + wave * 16;
-  if (a.a.window) look(p, p0);
+  if (a.a.window) {
+    look(here, p0);
+    look(next, p0 + 64);
+  }
   // (rows behind the end are the tile's first row again)
   auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
     uint64_t at = find.at(p.page[4], p.row[4], p0 + c < w.end, missing);
@@ -248,16 +262,15 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
   };
   if (p0 < w.end) {
     Tile t0, t1;
-    load(t0, p, p0);
-    look(p, p0 + 64);
+    load(t0, here, p0);
     while (true) {
-      load(t1, p, p0 + 64);
-      look(p, p0 + 128);
+      if (p0 + 64 < w.end) load(t1, next, p0 + 64);
+      if (p0 + 128 < w.end) look(next, p0 + 128);
       step(t0, p0);
       p0 += 64;
       if (p0 >= w.end) break;
-      load(t0, p, p0 + 64);
-      look(p, p0 + 128);
+      if (p0 + 64 < w.end) load(t0, next, p0 + 64);
+      if (p0 + 128 < w.end) look(next, p0 + 128);
       step(t1, p0);
       p0 += 64;
       if (p0 >= w.end) break;
@@ -320,12 +333,14 @@ __device__ __forceinline__ u32x2_v lds_column4(const char* p) {
 // carried 2^10 larger and fp32 queries at a power of two near 2^14, so that the pieces are normal numbers.
 //
 // Bound: the cache's bytes, which two workgroups of a CU keep on their way with two tiles of every wave (16 sequences of 4096
-// positions, 8 kv heads, bf16: 51 us, 5.2 TB/s; one of 131072, e4m3: 54 us, 5.1 TB/s; 48 of 1 .. 6000, int8: 68 us, 4.4 TB/s, where
+// positions, 8 kv heads, bf16: 50 us, 5.3 TB/s; one of 131072, e4m3: 52 us, 5.3 TB/s; 48 of 1 .. 6000, int8: 70 us, 4.3 TB/s, where
 // the sequences' ends do not meet; a copy reaches 4.85 TB/s).  With the table read in front of the rows of the same tile,
-// which then wait for it, and e4m3 widened by way of fp32, these were 57, 71 and 100.  V^T by LDS, not by a transposed cache: the
+// which then wait for it, and e4m3 widened by way of fp32, these were 57, 71 and 100.  Short sequences: latency (one of 100 positions
+// 6.7 us, 7.5 with the queries and the table of the second tile asked for later).  int8 with 16-bit queries is held to 168 registers,
+// three workgroups a CU (64 sequences of 2048 57 us, two workgroups 59; 48 of 1 .. 6000 70, 77); e4m3 spills at that (57 us at two, 68 at three).  V^T by LDS, not by a transposed cache: the
 // LDS path moves a few bytes per cycle of its 128, and a row stays a row for append, read and reorder.
 template <int STORE, int D, bool FULL>
-__global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_tiles) {
+__global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_attn_mc(AttnArgs a, int head_tiles) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
   constexpr bool B8 = page_scaled(STORE);
   constexpr int NQ = FULL ? 3 : 1, NP = FULL ? 3 : 2, KT = D / 32, DT = D / 16;
@@ -354,14 +369,40 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
 #pragma unroll
     for (int h = 0; h < 2; ++h) find.look(p0 + h * 16 + c, p.page[h], p.row[h]);
   };
-  // (the table is asked before the sequence's length is known, unless a window moves the first position)
-  Where p;
-  if (!a.a.window) look(p, blockIdx.z * a.plan.chunk + wave * 32);
-  const Part w = part_of(a, head_tiles);
+  // What does not wait for anything goes first: the queries (head c; columns past the last head repeat it and are not used; eight
+  // dims per k tile), then the table, before the sequence's length is known, unless a window moves the first position.
+  const Heads hd = heads_of(a, head_tiles);
+  const int64_t qo = (int64_t)blockIdx.y * a.a.q_row + (int64_t)(hd.head0 + min((uint32_t)c, hd.nh - 1)) * a.a.q_head;
+  auto dim_of = [&](int kt) { return B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8; };
+  u32x4_v qf[KT][NQ];
+  float qx[FULL ? KT : 1][8];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    if constexpr (FULL) {
+      load_query8(a, qo + dim_of(kt), a.q_wide, qx[kt]);
+    } else {
+      const uint16_t* p = static_cast<const uint16_t*>(a.a.q) + qo + dim_of(kt);
+      if (a.q_wide) {
+        qf[kt][0] = *reinterpret_cast<const u32x4_v*>(p);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qf[kt][0][i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+      }
+    }
+  }
+  Where here, next;
+  if (!a.a.window) {
+    look(here, blockIdx.z * a.plan.chunk + wave * 32);
+    look(next, blockIdx.z * a.plan.chunk + wave * 32 + 128);
+  }
+  const Part w = part_of(a, hd);
   if (w.idle) return;
   const uint32_t end = w.end;
   uint32_t p0 = w.begin + wave * 32;
-  if (a.a.window) look(p, p0);
+  if (a.a.window) {
+    look(here, p0);
+    look(next, p0 + 128);
+  }
   auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
     uint64_t at[2];
 #pragma unroll
@@ -379,20 +420,14 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
     // lanes 0 .. 31: the K scales of the tile's positions, 32 .. 63: those of V
     if constexpr (B8) t.scale = (g < 2 ? a.p.k_scale : a.p.v_scale)[(g & 1) ? at[1] : at[0]];
   };
-  // queries: head c (columns past the last head repeat it and are not used), eight dims per k tile
-  u32x4_v qf[KT][NQ];
   float fac = a.a.scale * 1.44269504088896341f;
-  {
-    const int64_t qo = (int64_t)w.seq * a.a.q_row + (int64_t)(w.head0 + min((uint32_t)c, w.nh - 1)) * a.a.q_head;
-    float x[KT][8];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) load_query8(a, qo + (B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8), a.q_wide, x[kt]);
-    if constexpr (FULL && HF::kNarrowRange) {
+  if constexpr (FULL) {
+    if constexpr (HF::kNarrowRange) {
       float top = 0.f;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[kt][e]));
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(qx[kt][e]));
       top = col4_max(top);
       int e = 0;
       (void)frexpf(top, &e);
@@ -400,21 +435,17 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[kt][i] = ldexpf(x[kt][i], -e);
+        for (int i = 0; i < 8; ++i) qx[kt][i] = ldexpf(qx[kt][i], -e);
       fac = ldexpf(fac, e);
     }
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (FULL) {
-          uint32_t w[3];
-          split_pair3<HF>(x[kt][2 * i], x[kt][2 * i + 1], w);
+        uint32_t piece[3];
+        split_pair3<HF>(qx[kt][2 * i], qx[kt][2 * i + 1], piece);
 #pragma unroll
-          for (int pc = 0; pc < 3; ++pc) qf[kt][pc][i] = w[pc];
-        } else {
-          qf[kt][0][i] = HF::pack2(x[kt][2 * i], x[kt][2 * i + 1]);
-        }
+        for (int pc = 0; pc < 3; ++pc) qf[kt][pc][i] = piece[pc];
       }
   }
 
@@ -529,16 +560,15 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_mc(AttnArgs a, int head_ti
   // two tiles in registers: the next one is on its way while this one is worked on
   if (p0 < end) {
     Tile t0, t1;
-    load(t0, p, p0);
-    look(p, p0 + 128);
+    load(t0, here, p0);
     while (true) {
-      load(t1, p, p0 + 128);
-      look(p, p0 + 256);
+      if (p0 + 128 < end) load(t1, next, p0 + 128);
+      if (p0 + 256 < end) look(next, p0 + 256);
       step(t0, p0);
       p0 += 128;
       if (p0 >= end) break;
-      load(t0, p, p0 + 128);
-      look(p, p0 + 256);
+      if (p0 + 128 < end) load(t0, next, p0 + 128);
+      if (p0 + 256 < end) look(next, p0 + 256);
       step(t1, p0);
       p0 += 128;
       if (p0 >= end) break;
@@ -616,17 +646,17 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
 
 // Workgroups along a sequence.  Two workgroups fit a CU, so 512 of them fill the chip; more only add starts, records and joining
 // (16384 positions of one sequence, 8 kv heads, bf16, us with the join: 64 splits 20.5, 128 25.0), while a split of 128 positions,
-// a tile for each of the four waves, is worth its join from 512 positions on (512 positions: 4 splits 10.6, none 12.7; 256: 11.0 and 9.1).
-// The lengths are not known here, only their bound: where sequences are several, as many workgroups again, of 1024 positions at
-// least, let the long ones be shared when the short ones are done (32 sequences of 0 .. 4096, 2 / 4 splits: 79 / 70; where all are
-// equally long it costs the join: 64 of 2048, 1 / 2 splits 98.6 / 102.7).
+// a tile for each of the four waves, is worth its join from 512 positions on (512 positions: 4 splits 10.0, none 12.7; 256: 11.0 and 8.9).
+// The lengths are not known here, only their bound: where sequences are several, more workgroups, of 1024 positions at least, share the
+// long ones when the short ones are done (32 sequences of 0 .. 4096, 2 / 4 splits: 79 / 68; 48 of 1 .. 6000, 3 / 5: 130 / 118; where
+// all are equally long it costs the join: 64 of 2048, 1 / 2 splits 98.6 / 101).
 PageAttnPlan plan_page_attention(const PagePool& p, uint32_t n_seqs, const PageAttn& a, uint32_t max_splits) {
   const uint32_t span = a.window ? (a.window < a.max_len ? a.window : a.max_len) : a.max_len;
   const uint64_t rows = (uint64_t)n_seqs * a.n_q_heads;
   const uint64_t wgs = (uint64_t)n_seqs * p.n_kv_heads * ((a.n_q_heads / p.n_kv_heads + 15) / 16);
   const uint64_t one = wgs ? wgs : 1, most = span <= 256 ? 1 : (span + 127) / 128;
   uint64_t splits = (512 + one - 1) / one;
-  const uint64_t uneven = std::min<uint64_t>((1024 + one - 1) / one, span / 1024);
+  const uint64_t uneven = std::min<uint64_t>((2048 + one - 1) / one, span / 1024);
   if (n_seqs > 1 && splits < uneven) splits = uneven;
   if (splits > most) splits = most;
   if (splits > max_splits) splits = max_splits;
