@@ -291,3 +291,12 @@ def test_searches_that_cannot_be_run_are_refused(nnc):
     assert e.value.status == nnc.E_STATE
     torch.cuda.synchronize()
     assert torch.equal(tables, tables0) and torch.equal(lens, lens0)   # nothing was enqueued
+
+
+def test_profile_names_the_paged_kernels(nnc):
+    _, m, pages, tables, logits, lens = begin(nnc, SMALL_BF16, 1, 3, 20, 4, torch.bfloat16)
+    m.profile_begin()
+    m.pages_store(pages, tables, 0, 0)
+    m.decode_beam(pages, tables, lens, 2, first_logits=logits, width=3)
+    got = {r["name"]: r["launches"] for r in m.profile_end()}
+    assert got["page_rows"] == 2 and got["page_attention"] == 2 and got["beam"] == 5 and "attn_partial" not in got

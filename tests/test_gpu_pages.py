@@ -497,3 +497,62 @@ def test_calls_on_two_streams(nnc):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(o, runs[i][4]) for o in outs[i])
+
+
+def test_the_binding_refuses_what_does_not_fit(nnc):
+    p = make_pool(nnc, "i8", 2, 8, 16, 2, 128)
+    tables = torch.arange(8, dtype=torch.int32, device=DEV).reshape(2, 4)
+    x = torch.ones((3, 2, 128), device=DEV)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV)
+    q, ln = torch.ones((2, 4, 128), device=DEV), torch.tensor([3, 0], dtype=torch.int32, device=DEV)
+    before = raw(p)
+
+    def refused(f, *args, **kw):
+        with pytest.raises(nnc.NncError) as e:
+            f(*args, **kw)
+        assert e.value.status == nnc.E_ARG, str(e.value)
+
+    refused(p.append, 2, x, x, tables, 0, pos)                       # no such layer
+    refused(p.append, 0, x, None, tables, 0, pos)
+    refused(p.append, 0, x, x.half(), tables, 0, pos)                # two types
+    refused(p.append, 0, x.double(), x.double(), tables, 0, pos)
+    refused(p.append, 0, x[:, :1], x[:, :1], tables, 0, pos)         # too few heads
+    refused(p.append, 0, x[..., :64], x[..., :64], tables, 0, pos)
+    refused(p.append, 0, x.transpose(1, 2).contiguous().transpose(1, 2), x, tables, 0, pos)   # elements apart
+    refused(p.append, 0, x.cpu(), x.cpu(), tables, 0, pos)
+    refused(p.append, 0, x, x, tables.long(), 0, pos)
+    refused(p.append, 0, x, x, tables[:, ::2], 0, pos)
+    refused(p.append, 0, x, x, tables.cpu(), 0, pos)
+    refused(p.append, 0, x, x, tables, 0, pos[:2])
+    refused(p.append, 0, x, x, tables, 0, pos.long())
+    refused(p.append, 0, x, x, tables, 0, -1)
+    refused(p.read, 0, tables, 0, 0)                                 # how many?
+    refused(p.read, 0, tables, 0, 0, n=2, dtype=torch.float64)
+    refused(p.attention, 0, q[:1], tables, ln)
+    refused(p.attention, 0, q[:, :3], tables, ln)                    # three query heads of two kv heads
+    refused(p.attention, 0, q, tables, ln.long())
+    refused(p.attention, 0, q, tables, ln, max_len=65)
+    refused(p.attention, 0, q, tables, ln, scale=math.inf)
+    refused(p.attention, 0, q, tables, ln, out=torch.empty((2, 4, 128), device=DEV, dtype=torch.bfloat16))
+    refused(p.reorder, tables, tables, torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros((1, 3), dtype=torch.int32, device=DEV))
+    refused(p.reorder, tables, tables[:1], torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros((1, 2), dtype=torch.int32, device=DEV))
+    refused(p.reorder, tables, tables, torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros((1, 2), dtype=torch.int32, device=DEV))
+    logits, scores = torch.zeros((1, 2, 40), device=DEV), torch.zeros((1, 2), device=DEV)
+    refused(nnc.beam_select, logits, scores.double())
+    refused(nnc.beam_select, logits, scores.T)
+    refused(nnc.beam_select, logits.double(), scores)
+    refused(nnc.beam_select, logits[..., ::2], scores)
+    refused(nnc.beam_select, logits, scores, torch.zeros((1, 2), dtype=torch.bool, device=DEV))      # ended, by which token?
+    refused(nnc.beam_select, logits, scores, None, 40)
+    refused(nnc.beam_select, logits, scores, workspace=torch.empty(4, dtype=torch.uint8, device=DEV))
+    refused(nnc.beam_select, torch.zeros((1, 33, 40), device=DEV), torch.zeros((1, 33), device=DEV))
+    refused(nnc.Pages, p.k, p.v)                                     # scales are missing
+    refused(nnc.Pages, p.k, p.v[:, :4], p.k_scale, p.v_scale)
+    refused(nnc.Pages.empty, 1, 4, 16, 2, 128, torch.float64)
+    torch.cuda.synchronize()
+    assert all(same_bits(a, b) for a, b in zip(before, raw(p)))
+    # nothing to do is no error
+    assert p.attention(0, q[:0], tables[:0], ln[:0]).shape == (0, 4, 128)
+    p.append(0, x[:0], x[:0], tables, 0, pos[:0])
+    p.reorder(tables[:0], tables[:0], ln[:0], torch.zeros((0, 2), dtype=torch.int32, device=DEV))
+    assert nnc.beam_select(logits[:0], scores[:0])[0].shape == (0, 2)
