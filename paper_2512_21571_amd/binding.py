@@ -108,16 +108,18 @@ class NncError(RuntimeError):
 
 
 _lib = None
+_torch = None   # set with _lib: an import statement in a call that takes 8 us is one of 0.3
 
 
 def lib():
     """Load libnnc.so (building it first only if no built library exists)."""
-    global _lib
+    global _lib, _torch
     if _lib is None:
         # PyTorch ships its own HIP runtime (soname libamdhip64.so.7).  Import it first so
         # that libnnc.so binds to that already-loaded runtime: two HIP runtimes in one
         # process cannot both own the device.
-        import torch  # noqa: F401
+        import torch
+        _torch = torch
         if not os.path.exists(_build.LIB_PATH):
             _build.build(True)
         L = ctypes.CDLL(_build.LIB_PATH)   # raises OSError if the library cannot be loaded
@@ -210,18 +212,12 @@ def _bad(message: str):
     raise NncError(E_ARG, message)
 
 
-def _row_types():
-    import torch
-    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-
-
-_ROW_TYPES = None
+_ROW_TYPES: dict = {}
 
 
 def _dtype_of(t):
-    global _ROW_TYPES
-    if _ROW_TYPES is None:
-        _ROW_TYPES = _row_types()
+    if not _ROW_TYPES:
+        _ROW_TYPES.update({_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16})
     code = _ROW_TYPES.get(t.dtype)
     return _bad(f"{t.dtype} is not one of float32, bfloat16, float16") if code is None else code
 
@@ -238,15 +234,14 @@ def _ptr(t):
 
 
 def _enqueue(device, f, *args):
-    """f(*args, stream) on the caller's current stream of a device, which is made current for the call if it is not.  (The stream's
-    handle as torch's own launchers get it: a Stream object costs 2 us, device guard and ctypes call 5.)"""
-    import torch
-    i = device.index
-    if torch.cuda.current_device() == i:
-        st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    """f(*args, stream) on the caller's current stream of a device, which is made current for the call if it is not.  (Device and
+    stream as torch's own launchers get them: a device guard and a Stream object cost 3.4 us.)"""
+    i, c = device.index, _torch._C
+    if c._cuda_getDevice() == i:
+        st = f(*args, c._cuda_getCurrentRawStream(i))
     else:
-        with torch.cuda.device(i):
-            st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+        with _torch.cuda.device(i):
+            st = f(*args, c._cuda_getCurrentRawStream(i))
     if st != OK:
         raise NncError(st, last_error())
 
@@ -260,8 +255,8 @@ class Pages:
     pool's device; outputs and workspaces are allocated for that stream."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        import torch
-        self.torch = torch
+        lib()
+        self.torch = torch = _torch
         code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int8: I8, torch.float8_e4m3fn: E4M3}.get(k.dtype)
         if code is None or k.dim() != 5:
             _bad(f"k: a pool of five dimensions in float32, bfloat16, float16, int8 or float8_e4m3fn expected, not {k.dtype} {list(k.shape)}")
@@ -408,7 +403,7 @@ def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
     """The best continuations of every group of beams (nnc_beam_select): logits [groups, width, vocab] (float32, bfloat16,
     float16), scores [groups, width] float32, finished [groups, width] bool or None, eos: the token that ends a beam (-1: none).
     Returns tokens, parents (int32), scores, finished, each [groups, width], best first."""
-    import torch
+    L, torch = lib(), _torch
     if logits.dim() != 3 or logits.device.type != "cuda":
         _bad("logits: [groups, width, vocab] in device memory expected")
     (g, w, v), (between, row, one), device = logits.shape, logits.stride(), logits.device
@@ -424,14 +419,14 @@ def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
                    parents.data_ptr(), out.data_ptr(), ended.data_ptr())
     if workspace is None:
         n = ctypes.c_size_t()
-        _check(lib().nnc_beam_select_workspace(ctypes.byref(beam), ctypes.byref(n)))
+        _check(L.nnc_beam_select_workspace(ctypes.byref(beam), ctypes.byref(n)))
         size = n.value
         workspace = torch.empty(size, dtype=torch.uint8, device=device)
     elif workspace.device != device or not workspace.is_contiguous():
         _bad("workspace: contiguous memory of the logits' device expected")
     else:
         size = workspace.numel() * workspace.element_size()
-    _enqueue(device, lib().nnc_beam_select, ctypes.byref(beam), workspace.data_ptr(), size)
+    _enqueue(device, L.nnc_beam_select, ctypes.byref(beam), workspace.data_ptr(), size)
     return tokens, parents, out, ended
 
 

@@ -170,3 +170,35 @@ def test_the_binding_refuses_wrong_tensors(nnc):
 def test_structures_match_the_header(nnc):
     """Sizes as a C compiler lays the header's structures out (x86-64)."""
     assert [ctypes.sizeof(s) for s in (nnc.NncPages, nnc.NncPageTable, nnc.NncPageRows, nnc.NncPageQuery, nnc.NncBeam, nnc.NncBeamRun)] == [64, 16, 88, 80, 96, 96]
+
+
+def test_calls_run_on_the_device_of_their_tensors(nnc, monkeypatch):
+    """On stand-ins for torch's device and stream: the tensors' device is current during the call and the stream is that device's;
+    an error status becomes an exception after the device is back."""
+    import types
+    state = {"now": 0, "calls": []}
+
+    class device:
+        def __init__(self, i):
+            self.i = i
+
+        def __enter__(self):
+            self.before, state["now"] = state["now"], self.i
+
+        def __exit__(self, *exc):
+            state["now"] = self.before
+
+    fake = types.SimpleNamespace(cuda=types.SimpleNamespace(device=device),
+                                 _C=types.SimpleNamespace(_cuda_getDevice=lambda: state["now"], _cuda_getCurrentRawStream=lambda i: 1000 + i))
+    monkeypatch.setattr(nnc, "_torch", fake)
+
+    def f(*args):
+        state["calls"].append((state["now"], args))
+        return nnc.OK if args[0] == "fine" else nnc.E_ARG
+
+    for index in (0, 3):
+        nnc._enqueue(types.SimpleNamespace(index=index), f, "fine", 7)
+        with pytest.raises(nnc.NncError):
+            nnc._enqueue(types.SimpleNamespace(index=index), f, "wrong")
+    assert state["now"] == 0
+    assert state["calls"] == [(i, args) for i in (0, 3) for args in (("fine", 7, 1000 + i), ("wrong", 1000 + i))]
