@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
 }
 
 // First a wave for every beam finds its best chunks (another one its log-sum), then `share` waves look into them and leave up to
-// `width` keys each, then a place is found for every key by counting those that come before it.  Bound: latency and, with sixteen
+// `width` keys each, best first, then one wave merges those lists.  Bound: latency and, with sixteen
 // waves on one CU, the issue of instructions; so what one wave can find is not found by all, and an element that is no candidate
 // costs a comparison.  4 beams 8.0 us, 8 beams 13.5, 16 beams 32 (4 / 8 beams with every wave choosing the chunks, one chunk on its way at a
 // time and the first wave taking the lists' heads in turn: 14 / 28).
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
   __shared__ double lse[BEAM_MAX_WIDTH];
   __shared__ float start[BEAM_MAX_WIDTH];
   __shared__ uint32_t state[BEAM_MAX_WIDTH];  // 0: a running beam, 1: ended, 2: not in use
-  __shared__ uint32_t n_found[PICK_WAVES], places[SLOTS], winner[BEAM_MAX_WIDTH];
+  __shared__ uint32_t n_found[PICK_WAVES], winner[BEAM_MAX_WIDTH];
   const uint32_t g = blockIdx.x, width = a.b.width, V = a.b.vocab;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t share = width < PICK_WAVES ? PICK_WAVES / width : 1, lists = width * share, slots = lists * width;
@@ -310,37 +310,42 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
     }
   }
   __syncthreads();
-  // A slot's place: NaN before everything, then the larger score, then the lower beam, then the better key of a beam.  Every slot
-  // is compared by several threads, with a part of the others each.
-  uint32_t pow2 = 64;
-  while (pow2 < slots) pow2 *= 2;
-  const uint32_t t = threadIdx.x & (pow2 - 1), seg = threadIdx.x / pow2, segs = 64 * PICK_WAVES / pow2;
-  const uint32_t w = t / (share * width);
-  const uint64_t k = t < slots ? keys[t] : 0;
-  uint64_t o = 0;
-  if (k) {
-    const float x = value_of((uint32_t)(k >> 32));
-    const double s = state[w] == 1 ? (double)start[w] : x == -INFINITY ? (double)x : (double)start[w] + ((double)x - lse[w]);
-    const uint64_t b = (uint64_t)__double_as_longlong(s + 0.);
-    o = s != s ? ~0ull : (b >> 63) ? ~b : b | (1ull << 63);
-  }
-  if (seg == 0 && t < slots) {
-    rank[t] = o;
-    places[t] = 0;
-  }
-  __syncthreads();
-  if (k) {
-    const uint32_t beam0 = w * share * width, beam1 = beam0 + share * width;
-    uint32_t before = 0;
-#pragma unroll 4
-    for (uint32_t i = seg; i < slots; i += segs) {
-      const uint64_t u = rank[i];
-      if (u >= o && i != t) before += u > o || i < beam0 || (i < beam1 && keys[i] > k);
+  // The keys' scores, as numbers that order like them (NaN before everything), and their merge: lane l of the first wave holds list l,
+  // the best head goes to the next place.  Ties: the lower beam, then the better key of a beam.
+  if (threadIdx.x < slots) {
+    const uint32_t w = threadIdx.x / (share * width);
+    const uint64_t k = keys[threadIdx.x];
+    uint64_t o = 0;
+    if (k) {
+      const float x = value_of((uint32_t)(k >> 32));
+      const double s = state[w] == 1 ? (double)start[w] : x == -INFINITY ? (double)x : (double)start[w] + ((double)x - lse[w]);
+      const uint64_t b = (uint64_t)__double_as_longlong(s + 0.);
+      o = s != s ? ~0ull : (b >> 63) ? ~b : b | (1ull << 63);
     }
-    if (before) atomicAdd(&places[t], before);
+    rank[threadIdx.x] = o;
   }
   __syncthreads();
-  if (seg == 0 && k && places[t] < width) winner[places[t]] = t;
+  if (wave == 0) {
+    uint32_t at = lane * width;
+    const uint32_t stop = lane < (int)lists ? at + width : 0;
+    uint64_t o = at < stop ? rank[at] : 0;
+#pragma unroll 1
+    for (uint32_t r = 0; r < width; ++r) {
+      const uint64_t top = wave_max_u64(o);
+      uint64_t tied = __ballot(o == top);
+      if (tied & (tied - 1)) {
+        const uint32_t beam = (uint32_t)(__ffsll((unsigned long long)tied) - 1) / share;
+        const bool same = o == top && lane / share == beam;
+        const uint64_t k = same ? keys[at] : 0, best = wave_max_u64(k);
+        tied = __ballot(same && k == best);
+      }
+      if (lane == __ffsll((unsigned long long)tied) - 1) {
+        winner[r] = at;
+        ++at;
+        o = at < stop ? rank[at] : 0;
+      }
+    }
+  }
   __syncthreads();
   if (threadIdx.x < width) {
     const uint32_t t = winner[threadIdx.x], to = g * width + threadIdx.x, w = t / (share * width);
