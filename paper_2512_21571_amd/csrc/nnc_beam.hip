@@ -1,8 +1,9 @@
 // Selection of a beam search: the `width` best of width x vocabulary continuations of every group.
 //   score(w, v) = scores[w] + logit(w, v) - log sum_u e^(logit(w, u))
-// Two kernels.  k_beam_scan reads the logits once: a wave takes a chunk of a beam's row and leaves its maximum m and the sum
-// of e^(x - m).  k_beam_pick, a workgroup per group, adds the sums up, finds the `width` chunks with the largest maxima and
-// looks for the best continuations in those alone: whatever is not in them is preceded by the maxima of all of them.
+// Two kernels.  k_beam_scan reads the logits once: a wave takes a chunk of a beam's row and leaves its maximum m, the sum
+// of e^(x - m) and the maxima of its quarters.  k_beam_pick, a workgroup per group, adds the sums up, finds the `width` chunks with
+// the largest maxima and looks for the best continuations in those alone, and of those in the quarters that reach the smallest of the
+// maxima: whatever is not in them is preceded by the maxima of all of them.
 // Within a beam the order of scores is the order of logits; scores of different beams are compared in 64 bits, since they
 // may be as close as the logits' own rounding.  Which lane adds what depends on the element's index alone, never on the
 // alignment of a row: beams with equal logits get equal sums, and ties between them go to the lowest index.
@@ -15,15 +16,16 @@ namespace nnc {
 
 namespace {
 
-constexpr uint32_t CHUNK = 1024;           // elements that a wave loads at once, sixteen a lane
+constexpr uint32_t QUARTER = 256, CHUNK = 4 * QUARTER;  // elements that sixteen lanes, a wave load at once, sixteen a lane
 constexpr uint32_t MAX_CHUNKS = 256;       // per row; longer rows have larger chunks, a multiple of this one
-constexpr int PICK_WAVES = 16, LIST = 64, BATCH = 4;  // waves of a workgroup, candidates that a wave collects, loads of a wave at once
+constexpr int PICK_WAVES = 16, LIST = 64, BATCH = 2;  // waves of a workgroup, candidates that a wave collects, loads of a wave at once
 constexpr float LOG2E = 1.44269504088896341f;
 
 struct SelArgs {
   BeamSelect b;
-  uint32_t chunks, mult;  // of a row; CHUNK elements in each
+  uint32_t chunks, mult;  // of a row; mult times CHUNK elements in each, a quarter of them for each sixteen lanes
   float2* ms;             // [row][chunks] maximum (NaN if the chunk holds one), sum
+  float* quarter;         // [row][chunks][4] maxima
 };
 
 // 32 bits that order like the values: NaN above everything, -0 counts as 0; 0 below every value, all ones above (with the lowest
@@ -57,11 +59,11 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
   return ((uint64_t)hi << 32) | wave_umax((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
 }
 
-// The lane's sixteen elements of the CHUNK at element c0 of a row, and their indices: runs of VEC neighbours, sixteen bytes.
+// Sixteen lanes' 256 elements from element c0 of a row on: those of lane 0 .. 15, and their indices: runs of VEC neighbours, sixteen bytes.
 template <int DT>
 struct Lane16 {
   static constexpr int VEC = DT == DT_F32 ? 4 : 8;
-  static __device__ __forceinline__ uint32_t index(uint32_t c0, int lane, int i) { return c0 + (i / VEC) * 64 * VEC + lane * VEC + i % VEC; }
+  static __device__ __forceinline__ uint32_t index(uint32_t c0, int lane, int i) { return c0 + (i / VEC) * 16 * VEC + lane * VEC + i % VEC; }
   // elements past the end: -infinity
   static __device__ __forceinline__ void load(const void* row, bool wide, uint32_t c0, uint32_t vocab, int lane, float (&x)[16]) {
 #pragma unroll
@@ -114,18 +116,18 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
   const int lane = threadIdx.x & 63;
   bool wide;
   const void* p = row_of<DT>(a, g, w, wide);
-  float m = -INFINITY, sum = 0.f;
+  const uint32_t q0 = (chunk * 4 + lane / 16) * a.mult;  // (in quarters)
+  float m = -INFINITY, sum = 0.f, mine = -INFINITY;
   bool nan = false;
   for (uint32_t i = 0; i < a.mult; ++i) {
-    const uint64_t c0 = ((uint64_t)chunk * a.mult + i) * CHUNK;
-    if (c0 >= a.b.vocab) break;
     float x[16];
-    Lane16<DT>::load(p, wide, (uint32_t)c0, a.b.vocab, lane, x);
+    Lane16<DT>::load(p, wide, (q0 + i) * QUARTER, a.b.vocab, lane & 15, x);
     float top = x[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
 #pragma unroll
     for (int e = 0; e < 16; ++e) nan |= x[e] != x[e];
+    mine = fmaxf(mine, top);
     top = wave_max(fmaxf(top, m));
     const float base = top == -INFINITY ? 0.f : top;
     sum *= __builtin_amdgcn_exp2f((m - base) * LOG2E);
@@ -134,21 +136,26 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
     m = top;
   }
   sum = wave_sum(sum);
-  if (__any(nan)) m = NAN;
-  if (lane == 0) a.ms[(size_t)row * a.chunks + chunk] = make_float2(m, sum);
+  mine = row16_max(mine);
+  const uint64_t nans = __ballot(nan);
+  if ((nans >> (lane & 48)) & 0xffffu) mine = NAN;
+  const size_t at = (size_t)row * a.chunks + chunk;
+  if ((lane & 15) == 0) a.quarter[at * 4 + lane / 16] = mine;
+  if (lane == 0) a.ms[at] = make_float2(nans ? NAN : m, sum);
 }
 
 // First a wave for every beam finds its best chunks (another one its log-sum), then `share` waves look into them and leave up to
 // `width` keys each, best first, then one wave merges those lists.  Bound: latency and, with sixteen
 // waves on one CU, the issue of instructions; so what one wave can find is not found by all, and an element that is no candidate
-// costs a comparison.  4 beams 8.0 us, 8 beams 13.5, 16 beams 32 (4 / 8 beams with every wave choosing the chunks, one chunk on its way at a
-// time and the first wave taking the lists' heads in turn: 14 / 28).
+// costs a comparison.  1 x 4 beams 8.5 us, 16 x 8 beams 11.5, 1 x 16 beams 21 (4 / 8 beams with every wave choosing the chunks, one chunk on its
+// way at a time and the first wave taking the lists' heads in turn: 14 / 28; whole chunks in place of quarters 8.0 / 14, 16 beams 28).
 template <int DT>
 __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
   constexpr int KEYS = MAX_CHUNKS / 64, SLOTS = BEAM_MAX_WIDTH * BEAM_MAX_WIDTH;
   __shared__ uint64_t found[PICK_WAVES][LIST];
   __shared__ uint64_t keys[SLOTS], rank[SLOTS];  // [list][place]; 0: none
   __shared__ uint32_t best_chunk[BEAM_MAX_WIDTH][BEAM_MAX_WIDTH], floor_of[BEAM_MAX_WIDTH];
+  __shared__ uint32_t quarters[BEAM_MAX_WIDTH][4 * BEAM_MAX_WIDTH], n_quarters[BEAM_MAX_WIDTH];
   __shared__ double lse[BEAM_MAX_WIDTH];
   __shared__ float start[BEAM_MAX_WIDTH];
   __shared__ uint32_t state[BEAM_MAX_WIDTH];  // 0: a running beam, 1: ended, 2: not in use
@@ -199,7 +206,22 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
           if (at == (uint32_t)(i * 64 + lane)) key[i] = 0;
         if (lane == 0) best_chunk[w][r] = at;
       }
-      if (lane == 0) floor_of[w] = least;
+      if (a.chunks < width) least = 0;  // (then everything is looked at)
+      // the quarters of those chunks that have an element which is not below the smallest of the maxima
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      uint32_t n = 0;
+      for (uint32_t i = lane; i < (chunks * 4 + 63) / 64 * 64; i += 64) {
+        const uint32_t q = i < chunks * 4 ? best_chunk[w][i / 4] * 4 + i % 4 : 0;
+        const bool in = i < chunks * 4 && order_of(a.quarter[(size_t)row * a.chunks * 4 + q]) >= least;
+        const uint64_t who = __ballot(in);
+        if (in) quarters[w][n + __popcll(who & ((1ull << lane) - 1))] = q;
+        n += __popcll(who);
+      }
+      if (lane == 0) {
+        floor_of[w] = least;
+        n_quarters[w] = n;
+      }
     }
     if (part == 1 || share == 1) {
       bool nan = false;
@@ -228,15 +250,15 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
       if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), st == 1 ? (uint32_t)a.b.eos : (uint32_t)lane);
       continue;
     }
-    // This wave's share of those chunks.  COLLECT: the elements that are not below `least`, the smallest of the chunks' maxima
+    // This wave's share of those quarters, four at a time.  COLLECT: the elements that are not below `least`, the smallest of the chunks' maxima
     // (`width` elements are not).  Where that are more than LIST (large values side by side) or there are fewer chunks than
     // places, LANES raises it to the width-th largest of the lanes' maxima.  PLACES, for many equal values: all elements
     // once more for every place.
     bool wide;
     const void* p = row_of<DT>(a, g, w, wide);
     enum { LANES, COLLECT, PLACES } mode = a.chunks < width ? LANES : COLLECT;
-    uint32_t least = a.chunks < width ? 0u : floor_of[w];
-    const uint32_t pieces = (chunks - min(part, chunks) + share - 1) / share * a.mult;
+    uint32_t least = floor_of[w];
+    const uint32_t n_q = n_quarters[w], fours = (n_q + 3) / 4, pieces = (fours - min(part, fours) + share - 1) / share * a.mult;
     bool raised = false;
     uint32_t place = 0, n;
     uint64_t below = ~0ull;
@@ -250,22 +272,21 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
       for (uint32_t q0 = 0; q0 < pieces; q0 += BATCH) {
         float x[BATCH][16];
         uint32_t first[BATCH];
-        bool there[BATCH];
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
-          const uint32_t q = min(q0 + j, pieces - 1), of = q / a.mult;  // (without a branch: it would keep the loads apart)
-          const uint64_t c0 = ((uint64_t)best_chunk[w][part + of * share] * a.mult + (q - of * a.mult)) * CHUNK;
-          first[j] = c0 < V ? (uint32_t)c0 : 0u;
-          there[j] = q0 + j < pieces && c0 < V;
-          Lane16<DT>::load(p, wide, first[j], V, lane, x[j]);
+          const uint32_t q = min(q0 + j, pieces - 1), of = q / a.mult, slot = (part + of * share) * 4 + lane / 16;
+          const uint32_t c0 = (quarters[w][min(slot, n_q - 1)] * a.mult + (q - of * a.mult)) * QUARTER;
+          // (what is not there loads something that is: a branch would keep the loads apart)
+          first[j] = q0 + j < pieces && slot < n_q ? c0 : V;
+          Lane16<DT>::load(p, wide, c0, V, lane & 15, x[j]);
         }
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
-          if (!there[j]) continue;
+          const float bar = first[j] == V ? INFINITY : floor;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            if (x[j][e] < floor) continue;
-            const uint32_t at = Lane16<DT>::index(first[j], lane, e), o = order_of(x[j][e]);
+            if (x[j][e] < bar) continue;
+            const uint32_t at = Lane16<DT>::index(first[j], lane & 15, e), o = order_of(x[j][e]);
             if (at >= V || o < least) continue;
             const uint64_t t = sort_key(o, at);
             if (mode == COLLECT) {
@@ -377,7 +398,7 @@ static void scan_shape(uint32_t vocab, uint32_t& chunks, uint32_t& mult) {
 size_t beam_select_bytes(uint32_t rows, uint32_t vocab) {
   uint32_t chunks, mult;
   scan_shape(vocab, chunks, mult);
-  return (size_t)rows * chunks * sizeof(float2);
+  return (size_t)rows * chunks * (sizeof(float2) + 4 * sizeof(float));
 }
 
 hipError_t launch_beam_select(hipStream_t s, const BeamSelect& b, void* workspace) {
@@ -387,6 +408,7 @@ hipError_t launch_beam_select(hipStream_t s, const BeamSelect& b, void* workspac
   a.b = b;
   scan_shape(b.vocab, a.chunks, a.mult);
   a.ms = static_cast<float2*>(workspace);
+  a.quarter = reinterpret_cast<float*>(a.ms + (size_t)b.n_groups * b.width * a.chunks);
   const dim3 grid((a.chunks + 3) / 4, b.n_groups * b.width);
 #define NNC_SELECT(DT)                                         \
   do {                                                         \
