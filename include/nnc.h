@@ -460,7 +460,9 @@ typedef struct {
  * Attention of one new token per sequence over one layer: softmax(scale * q K^T) V over positions 0 .. lens[i] - 1
  * (the last `window` of them).  Sums, softmax statistics and scores are fp32-grade whatever the types; out is
  * rounded once.  A sequence of length 0 gives zeros; a negative length, one above max_len and a missing page
- * give NaN.  What pages hold beyond a sequence's length is not looked at.
+ * give NaN.  What pages hold beyond a sequence's length is not looked at.  A NaN or an infinity in reach shows in the results
+ * of the heads that read it, as NaN or an infinity, but for scores of -infinity: out of an fp32 pool they weigh nothing (where
+ * nothing else is left the result is zero), out of others they do that or give NaN.
  * Long sequences are split over several workgroups and their results joined in a fixed order: the same call gives the same
  * bits.  How they are split depends on max_len, n_seqs and the heads, so results for another max_len
  * differ in rounding.  workspace: nnc_page_attention_workspace bytes (which may be 0), on a multiple of 16.
@@ -479,7 +481,7 @@ nnc_status nnc_page_attention(const nnc_pages *pages, uint32_t layer, const nnc_
  *   the other entries of after stay: from f on they name pages of the beam's own, which no other beam of `after` has.
  * after: device [n_seqs][max_pages], may be before->entries itself (then a beam's page may be another's
  * source, in any permutation).  Full pages are shared, nothing of them is copied.  A length that is negative or does not fit
- * the table changes nothing; a missing page is not copied.  width: up to 32.
+ * the table changes nothing; a missing page is not copied.  width: up to 32; layers x kv heads x bytes of a head's page: up to 2^34.
  */
 nnc_status nnc_page_reorder(const nnc_pages *pages, const nnc_page_table *before, int32_t *after,
                             const int32_t *lens, const int32_t *parents, uint32_t width, void *stream);

@@ -290,6 +290,8 @@ class Pages:
     def _index(self, x, n, name):
         """seq or pos of n rows: (pointer, 0) of a tensor, (None, value) of a number."""
         if not isinstance(x, self.torch.Tensor):
+            if not -0x80000000 <= x <= 0x7fffffff:   # (ctypes would drop the upper bits)
+                _bad(f"{name}: {x} has more than 32 bits")
             return None, int(x)
         if x.dtype != self._i32 or x.shape != (n,) or x.device != self.device or not x.is_contiguous():
             _bad(f"{name}: contiguous int32 [{n}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")
@@ -328,7 +330,7 @@ class Pages:
         if k is None or v is None:
             _bad("rows: k or v is None")
         rows, table = self._rows(k, v, seq, pos), self._table(tables)
-        _enqueue(self.device, lib().nnc_page_append, self._desc, layer, ctypes.byref(table), ctypes.byref(rows))
+        _enqueue(self.device, lib().nnc_page_append, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(rows))
 
     def read(self, layer: int, tables, seq, pos, dtype=None, n: int | None = None, k=None, v=None):
         """Rows (k, v) [n, kv heads, head_dim] of the named positions, in `dtype` (float32).  n: with two numbers for seq and
@@ -341,10 +343,17 @@ class Pages:
             k = self.torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype or self.torch.float32, device=self.device)
             v = self.torch.empty_like(k)
         rows, table = self._rows(k, v, seq, pos), self._table(tables)
-        _enqueue(self.device, lib().nnc_page_read, self._desc, layer, ctypes.byref(table), ctypes.byref(rows))
+        _enqueue(self.device, lib().nnc_page_read, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(rows))
         return k, v
 
+    def _layer(self, layer):
+        if not 0 <= layer < self.n_layers:
+            _bad(f"layer {layer} of {self.n_layers}")
+        return layer
+
     def _query(self, q, n, lens, max_len, scale, window, out):
+        if not (0 <= max_len <= 0x7fffffff and 0 <= window <= 0x7fffffff):
+            _bad(f"max_len {max_len}, window {window}: 0 .. 2^31 - 1 expected")
         row, head = self._heads(q, n, "q")
         o_row = o_head = 0
         if out is not None:
@@ -381,7 +390,7 @@ class Pages:
             _bad("workspace: contiguous memory of the pool's device expected")
         else:
             size = workspace.numel() * workspace.element_size()
-        _enqueue(self.device, lib().nnc_page_attention, self._desc, layer, ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size)
+        _enqueue(self.device, lib().nnc_page_attention, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size)
         return out
 
     def reorder(self, before, after, lens, parents):
@@ -407,10 +416,14 @@ def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
     if logits.dim() != 3 or logits.device.type != "cuda":
         _bad("logits: [groups, width, vocab] in device memory expected")
     (g, w, v), (between, row, one), device = logits.shape, logits.stride(), logits.device
-    if g and w and (one != 1 or (g > 1 and between != w * row)):
+    if w == 1:
+        row = between   # (one beam a group: no rows are `row` apart)
+    if g and w and ((one != 1 and v > 1) or (g > 1 and between != w * row)):
         _bad("logits: rows of adjacent elements, one distance between all rows, expected")
     if finished is not None and finished.dtype != torch.bool:
         _bad("finished: bool expected")
+    if not -1 <= eos < v:
+        _bad(f"eos: {eos} is no token of {v}, nor -1")
     _on(device, torch.float32, (g, w), scores=scores)
     _on(device, torch.bool, (g, w), finished=finished)
     tokens = torch.empty((g, w), dtype=torch.int32, device=device)
@@ -600,6 +613,8 @@ class Model:
         """Positions pos0 .. pos0 + n - 1 (to the slot's end) of a slot's cache to the same positions of a sequence in pages."""
         n = self.slot_len(slot) - pos0 if n is None else n
         table = self._paged(pages, tables)
+        if min(seq, slot, pos0, n) < 0 or max(seq, slot, pos0, n) > 0x7fffffff:
+            _bad(f"sequence {seq}, slot {slot}, positions {pos0} .. + {n}")
         self._before()
         try:
             _check(lib().nnc_pages_store(self.h, ctypes.byref(pages.desc), ctypes.byref(table), seq, slot, pos0, n))
@@ -627,6 +642,8 @@ class Model:
         call before.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
         torch, beams = self.torch, tables.shape[0]
         table = self._paged(pages, tables)
+        if not -1 <= eos < self.V:
+            _bad(f"eos: {eos} is no token of {self.V}, nor -1")
         if first_logits is not None:
             groups = first_logits.shape[0]
             if width is None or groups * width != beams:

@@ -1987,6 +1987,8 @@ nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& tab
 nnc_status nnc_pages_store(nnc_model* m, const nnc_pages* pages, const nnc_page_table* table, uint32_t seq, uint32_t slot,
                            uint32_t pos0, uint32_t n) {
   if (!m) return fail(NNC_E_ARG, "model is NULL");
+  if (resident_failed(m, false))
+    return fail(NNC_E_DEVICE, "an earlier decode launch gave up waiting for its other workgroups; recreate the model");
   if (nnc_status st = check_model_pages(m, pages)) return st;
   if (nnc_status st = check_table(pages, table)) return st;
   if (seq >= table->n_seqs) return fail(NNC_E_ARG, "sequence %u of %u", seq, table->n_seqs);
@@ -2042,6 +2044,8 @@ nnc_status nnc_decode_beam(nnc_model* m, const nnc_pages* pages, const nnc_beam_
   if (n == 0 || n > MAX_DECODE_BATCH) return fail(NNC_E_ARG, "%u beams in all (1 .. %u)", n, MAX_DECODE_BATCH);
   const nnc_page_table table{run->tables, n, run->max_pages};
   if (nnc_status st = check_table(pages, &table)) return st;
+  if (reorder_grid(reorder_of(pages, &table, run->tables, run->lens, nullptr, run->width)).blocks > REORDER_MAX_BLOCKS)
+    return fail(NNC_E_ARG, "pages: more layers, kv heads and positions of a page than one reordering takes");
   if (!run->lens || !run->tokens_out || !run->parents_out || !run->scores || !run->finished || (!run->first_logits && !run->tokens))
     return fail(NNC_E_ARG, "NULL buffer");
   if (run->eos < -1 || (run->eos >= 0 && (uint32_t)run->eos >= m->c.vocab)) return fail(NNC_E_ARG, "end token %d", run->eos);

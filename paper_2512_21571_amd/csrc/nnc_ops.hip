@@ -193,7 +193,10 @@ nnc_status nnc_page_reorder(const nnc_pages* pages, const nnc_page_table* before
   if (before->n_seqs == 0) return NNC_OK;
   if (!after || !lens || !parents) return fail(NNC_E_ARG, "after, lens or parents is NULL");
   if (bad_align(after, 4) || bad_align(lens, 4) || bad_align(parents, 4)) return fail(NNC_E_ARG, "after, lens and parents must lie on a multiple of 4 bytes");
-  OPS_TRY(launch_page_reorder(static_cast<hipStream_t>(stream), reorder_of(pages, before, after, lens, parents, width)));
+  const PageReorder r = reorder_of(pages, before, after, lens, parents, width);
+  if (reorder_grid(r).blocks > REORDER_MAX_BLOCKS)
+    return fail(NNC_E_ARG, "%u layers x %u kv heads x pages of %u positions are too many for one call", r.n_layers, r.n_kv_heads, r.page_tokens);
+  OPS_TRY(launch_page_reorder(static_cast<hipStream_t>(stream), r));
   return NNC_OK;
 }
 

@@ -230,6 +230,20 @@ struct PageReorder {
   const int32_t *lens, *parents;
 };
 constexpr uint32_t BEAM_MAX_WIDTH = 32;
+// Workgroups along x: `tables` of them turn table columns, the rest copy `chunks` pieces of 4096 bytes of K and of V for every layer and head.
+// A launch has fewer than 2^32 threads along x.
+struct ReorderGrid {
+  uint32_t tables, chunks;
+  uint64_t blocks;
+};
+constexpr uint64_t REORDER_MAX_BLOCKS = 0xffffff;
+inline ReorderGrid reorder_grid(const PageReorder& r) {
+  ReorderGrid g;
+  g.tables = (r.max_pages + 255) / 256;
+  g.chunks = (uint32_t)(((uint64_t)r.page_tokens * r.row_bytes + 4095) / 4096);
+  g.blocks = g.tables + (uint64_t)r.n_layers * r.n_kv_heads * 2 * g.chunks;
+  return g;
+}
 hipError_t launch_page_reorder(hipStream_t s, const PageReorder& r);
 
 // One query row per sequence against its cached positions.

@@ -226,15 +226,13 @@ __global__ __launch_bounds__(256) void k_page_reorder(PageReorder r, uint32_t nt
 }
 
 hipError_t launch_page_reorder(hipStream_t s, const PageReorder& r) {
-  const uint32_t nt = (r.max_pages + 255) / 256;
-  const uint32_t nchunks = (uint32_t)(((uint64_t)r.page_tokens * r.row_bytes + 4095) / 4096);
-  const uint64_t blocks = nt + (uint64_t)r.n_layers * r.n_kv_heads * 2 * nchunks;
-  if (r.width == 0 || r.width > BEAM_MAX_WIDTH || blocks > 0x7fffffffull || r.n_groups > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks, r.n_groups);
-  if (r.width <= 4) k_page_reorder<4><<<grid, 256, 0, s>>>(r, nt, nchunks);
-  else if (r.width <= 8) k_page_reorder<8><<<grid, 256, 0, s>>>(r, nt, nchunks);
-  else if (r.width <= 16) k_page_reorder<16><<<grid, 256, 0, s>>>(r, nt, nchunks);
-  else k_page_reorder<32><<<grid, 256, 0, s>>>(r, nt, nchunks);
+  const ReorderGrid g = reorder_grid(r);
+  if (r.width == 0 || r.width > BEAM_MAX_WIDTH || g.blocks > REORDER_MAX_BLOCKS || r.n_groups > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)g.blocks, r.n_groups);
+  if (r.width <= 4) k_page_reorder<4><<<grid, 256, 0, s>>>(r, g.tables, g.chunks);
+  else if (r.width <= 8) k_page_reorder<8><<<grid, 256, 0, s>>>(r, g.tables, g.chunks);
+  else if (r.width <= 16) k_page_reorder<16><<<grid, 256, 0, s>>>(r, g.tables, g.chunks);
+  else k_page_reorder<32><<<grid, 256, 0, s>>>(r, g.tables, g.chunks);
   return hipGetLastError();
 }
 

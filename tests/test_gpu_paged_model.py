@@ -300,3 +300,23 @@ def test_profile_names_the_paged_kernels(nnc):
     m.decode_beam(pages, tables, lens, 2, first_logits=logits, width=3)
     got = {r["name"]: r["launches"] for r in m.profile_end()}
     assert got["page_rows"] == 2 and got["page_attention"] == 2 and got["beam"] == 5 and "attn_partial" not in got
+
+
+def test_rows_of_a_failed_launch_are_not_stored(nnc):
+    """A decode launch that gave up (a wait bounded to one poll, as in the tests of the slots) leaves rows that nobody may pass on."""
+    shape = SMALL_BF16
+    m = nnc.Model(shape, synth.make_blob(shape, weight_std=0.05), 16, 64)
+    pages = nnc.Pages.empty(shape.n_layers, 4, 16, shape.n_kv_heads, 128, torch.bfloat16, DEV)
+    tables = torch.arange(4, dtype=torch.int32, device=DEV).reshape(1, 4)
+    for s in range(16):
+        m.prefill(s, synth.tokens(9, shape.vocab, stream=s))
+    m.pages_store(pages, tables, 0, 3)
+    m.set_option(nnc.OPT_FUSE_NORM, 1)
+    m.set_option(nnc.OPT_SPIN_LIMIT, 1)
+    m.decode_greedy(list(range(16)), [1] * 16, 8)
+    with pytest.raises(nnc.NncError) as e:
+        m.synchronize()
+    assert e.value.status == nnc.E_DEVICE
+    with pytest.raises(nnc.NncError) as e:
+        m.pages_store(pages, tables, 0, 3)
+    assert e.value.status == nnc.E_DEVICE

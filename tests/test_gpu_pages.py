@@ -306,6 +306,19 @@ def test_select(nnc, rows, g, w, v):
     check_select(nnc, logits, scores, torch.zeros_like(finished), eos)
 
 
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+def test_select_one_beam_of_rows_anywhere(nnc, rows):
+    """Groups of one beam: only the distance between groups counts, whatever the stride of the beams' dimension says."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = (torch.randn((4, 3, 5003), generator=gen, device=DEV) * 3).to(pu.ROWS[rows])
+    scores = -torch.rand((4, 1), generator=gen, device=DEV)
+    check_select(nnc, x[:, 1:2], scores)
+    check_select(nnc, x[:, 2, 3:].unsqueeze(1), scores)
+    for bad in (7 + 5003, -2, 1 << 32):
+        with pytest.raises(nnc.NncError):
+            nnc.beam_select(x[:, :1], scores, None, bad)
+
+
 def test_select_ties_go_to_the_lower_beam_and_token(nnc):
     """Equal rows at different alignments have equal sums; equal logits, zeros of both signs, everything forbidden."""
     for v in (5, 777, 9001):

@@ -128,6 +128,12 @@ def test_bad_reorderings(nnc):
     assert L.nnc_page_reorder(ref(p), ref(table(nnc, n_seqs=0)), None, None, None, 2, None) == nnc.OK
 
 
+def test_reorderings_that_one_launch_cannot_do(nnc):
+    big, t = pages(nnc, n_layers=1024, n_kv_heads=1024, page_tokens=4096), table(nnc)
+    assert nnc.lib().nnc_page_reorder(ref(big), ref(t), P, P, P, 2, None) == nnc.E_ARG
+    assert "one call" in nnc.last_error()
+
+
 def test_bad_selections(nnc):
     L = nnc.lib()
     n = ctypes.c_size_t()
@@ -202,3 +208,35 @@ def test_calls_run_on_the_device_of_their_tensors(nnc, monkeypatch):
             nnc._enqueue(types.SimpleNamespace(index=index), f, "wrong")
     assert state["now"] == 0
     assert state["calls"] == [(i, args) for i in (0, 3) for args in (("fine", 7, 1000 + i), ("wrong", 1000 + i))]
+
+
+def test_numbers_that_the_structures_cannot_hold(nnc, monkeypatch):
+    """A number of more bits than its field is refused, not cut down to another position, sequence, layer or token.  (A pool on the
+    CPU, and nothing is called.)"""
+    import torch
+
+    def never(*args):
+        raise AssertionError("called")
+
+    monkeypatch.setattr(nnc, "_enqueue", never)
+    p = nnc.Pages.__new__(nnc.Pages)
+    p.torch, p.device, p._i32 = torch, torch.device("cpu"), torch.int32
+    p.n_layers, p.n_pages, p.n_kv_heads, p.page_tokens, p.head_dim = 2, 8, 2, 16, 64
+    p.desc = pages(nnc, dtype=nnc.BF16, head_dim=64, k_scale=None, v_scale=None)
+    p._desc = ctypes.byref(p.desc)
+    tables, lens = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    x, q = torch.zeros((3, 2, 64)), torch.zeros((2, 4, 64))
+    for layer, seq, pos in ((-1, 0, 0), (2, 0, 0), (1 << 32, 0, 0), (0, 1 << 32, 0), (0, 0, 1 << 32), (0, 0, 1 << 31), (0, -(1 << 32), 0)):
+        with pytest.raises(nnc.NncError) as e:
+            p.append(layer, x, x, tables, seq, pos)
+        assert e.value.status == nnc.E_ARG
+        with pytest.raises(nnc.NncError):
+            p.read(layer, tables, seq, pos, k=x)
+    for change in (dict(layer=-1), dict(layer=1 << 32), dict(max_len=1 << 32), dict(max_len=-1), dict(window=1 << 32), dict(window=-5)):
+        with pytest.raises(nnc.NncError) as e:
+            p.attention(**{**dict(layer=0, q=q, tables=tables, lens=lens), **change})
+        assert e.value.status == nnc.E_ARG
+    with pytest.raises(AssertionError):
+        p.append(1, x, x, tables, 1, 60)
+    with pytest.raises(AssertionError):
+        p.attention(1, q, tables, lens, max_len=64, window=3)
