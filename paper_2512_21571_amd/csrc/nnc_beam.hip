@@ -131,13 +131,13 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
     top = wave_max(fmaxf(top, m));
     const float base = top == -INFINITY ? 0.f : top;
     float s = 0.f;
-    if (fabsf(base) < 0x1p126f) {
+    if (fabsf(base) < 0x1p16f) {
       // x log2 e - base log2 e in one operation each; what the rounding of the second product took is put back afterwards
       const float bl = base * LOG2E;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], LOG2E, -bl));
       s *= __builtin_amdgcn_exp2f(__builtin_fmaf(base, -LOG2E, bl));
-    } else {  // (that product is no number)
+    } else {  // (where that rounding is no small number)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((x[e] - base) * LOG2E);
     }

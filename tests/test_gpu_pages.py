@@ -371,6 +371,20 @@ def test_select_rows_far_apart(nnc):
         nnc.beam_select(base.as_strided((2, 2, 100), (1000, 100, 1)), torch.zeros((2, 2), device=DEV))
 
 
+@pytest.mark.parametrize("v", [5003, 300001])
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+def test_select_rows_far_from_zero(nnc, rows, v):
+    """Logits a constant apart have the same probabilities; and logits so large that their product with log2(e) is no number."""
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.randn((1, 4, v), generator=gen, device=DEV) * 3
+    scores = -torch.rand((1, 4), generator=gen, device=DEV)
+    far = [800.0, -3e4] if rows == "f16" else [800.0, -3e4, 2.0 ** 125, -(2.0 ** 125), 1.2 * 2.0 ** 126, 1.9 * 2.0 ** 126, -1.9 * 2.0 ** 126]
+    for offset in far:
+        check_select(nnc, (x + offset).to(pu.ROWS[rows]), scores)
+        if abs(offset) > 1e30:
+            check_select(nnc, ((x / 64).clamp(-1, 1) * offset).to(pu.ROWS[rows]), scores)
+
+
 def test_select_shows_a_failed_beam(nnc):
     logits = torch.randn((2, 3, 5000), device=DEV)
     scores = torch.full((2, 3), -1.0, device=DEV)
