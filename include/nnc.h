@@ -458,8 +458,8 @@ typedef struct {
 
 /*
  * Attention of one new token per sequence over one layer: softmax(scale * q K^T) V over positions 0 .. lens[i] - 1
- * (the last `window` of them).  Sums, softmax statistics and scores are fp32-grade whatever the types; out is
- * rounded once.  A sequence of length 0 gives zeros; a negative length, one above max_len and a missing page
+ * (the last `window` of them).  Sums, softmax statistics, scores and weights are fp32-grade whatever the types (weights 22 bits for
+ * binary16 queries over a binary16 pool); out is rounded once.  A sequence of length 0 gives zeros; a negative length, one above max_len and a missing page
  * give NaN.  What pages hold beyond a sequence's length is not looked at.  A NaN or an infinity in reach shows in the results
  * of the heads that read it, as NaN or an infinity, but for scores of -infinity: out of an fp32 pool they weigh nothing (where
  * nothing else is left the result is zero), out of others they do that or give NaN.
