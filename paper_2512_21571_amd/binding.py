@@ -215,6 +215,13 @@ def _bad(message: str):
 _ROW_TYPES: dict = {}
 
 
+def _count(least, **numbers):
+    """Whole numbers least .. 2^31 - 1.  (ctypes would drop the upper bits of others: 2^32 + 5 would become 5.)"""
+    for name, n in numbers.items():
+        if not least <= n <= 0x7fffffff:
+            _bad(f"{name} {n}: {least} .. 2^31 - 1 expected")
+
+
 def _dtype_of(t):
     if not _ROW_TYPES:
         _ROW_TYPES.update({_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16})
@@ -623,6 +630,7 @@ class Model:
 
     def decode_step_paged(self, pages: Pages, tables, lens, tokens, max_len: int = 0, want_logits: bool = True):
         """nnc_decode_step_paged: lens and tokens are int32 tensors [sequences]; lens grow by one."""
+        _count(0, max_len=max_len)
         table = self._paged(pages, tables)
         b = tables.shape[0]
         _on(pages.device, self.torch.int32, (b,), lens=lens, tokens=tokens)
@@ -640,6 +648,8 @@ class Model:
                     eos: int = -1, max_len: int = 0):
         """nnc_decode_beam.  Begin: first_logits [groups, vocab] and width.  Go on: tokens, scores, finished [groups, width] of the
         call before.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
+        _count(0, max_len=max_len)
+        _count(1, n_steps=n_steps)
         torch, beams = self.torch, tables.shape[0]
         table = self._paged(pages, tables)
         if not -1 <= eos < self.V:
