@@ -544,7 +544,8 @@ nnc_status nnc_decode_step_paged(nnc_model *m, const nnc_pages *pages, const nnc
  * goes on from `tokens`, scores and finished as the call before left them (tokens: the last row of its tokens_out).
  * lens: device [n_groups * width], updated (a first step adds nothing); max_len as for nnc_decode_step_paged, before the call.
  * tokens_out, parents_out: device [n_steps][n_groups * width]; scores, finished: device [n_groups * width].
- * Beams that have ended keep their score and repeat eos.  n_groups * width: up to 21.
+ * Beams that have ended keep their score and repeat eos; in a run that goes on without one (eos -1) those that
+ * `finished` names stay ended too, and repeat their last token.  n_groups * width: up to 21.
  */
 typedef struct {
   int32_t *tables;

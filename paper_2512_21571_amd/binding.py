@@ -647,7 +647,7 @@ class Model:
     def decode_beam(self, pages: Pages, tables, lens, n_steps: int, first_logits=None, tokens=None, scores=None, finished=None, width: int | None = None,
                     eos: int = -1, max_len: int = 0):
         """nnc_decode_beam.  Begin: first_logits [groups, vocab] and width.  Go on: tokens, scores, finished [groups, width] of the
-        call before.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
+        call before; beams that have ended stay so whatever eos is now.  Returns tokens and parents [n_steps, groups, width], scores and finished [groups, width]."""
         _count(0, max_len=max_len)
         _count(1, n_steps=n_steps)
         torch, beams = self.torch, tables.shape[0]

@@ -2061,7 +2061,7 @@ nnc_status nnc_decode_beam(nnc_model* m, const nnc_pages* pages, const nnc_beam_
   BeamSelect b{};
   b.dtype = DT_F32; b.n_groups = run->n_groups; b.width = run->width; b.vocab = m->V();
   b.scores = run->scores; b.scores_out = run->scores;
-  b.finished = run->eos >= 0 ? run->finished : nullptr; b.finished_out = run->finished; b.eos = run->eos;
+  b.finished = run->finished; b.finished_out = run->finished; b.eos = run->eos;
   for (uint32_t step = 0; step < run->n_steps; ++step) {
     const bool first = begin && step == 0;
     if (!first) {
@@ -2070,6 +2070,7 @@ nnc_status nnc_decode_beam(nnc_model* m, const nnc_pages* pages, const nnc_beam_
       // (a bound on the lengths that is not known stays the table's)
       const uint32_t most = run->max_len ? run->max_len + done : room - 1;
       if (nnc_status st = paged_step(m, pages, PageTable{table.entries, n, table.max_pages}, run->lens, most, tok, m->logits, nullptr)) return st;
+      b.last = run->eos < 0 ? tok : nullptr;  // (beams that an earlier run with an end token has ended stay so)
     }
     // (at the start only beam 0 of a group is in use, the rows of the others are not looked at)
     b.logits = first ? run->first_logits : m->logits;

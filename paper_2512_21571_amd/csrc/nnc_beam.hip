@@ -260,7 +260,8 @@ __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {
     uint64_t* list = keys + l * width;
     if (st) {  // one continuation; or every one of them at -infinity, in order
       const uint32_t n = part ? 0u : st == 1 ? 1u : min(width, V);
-      if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), st == 1 ? (uint32_t)a.b.eos : (uint32_t)lane);
+      const uint32_t token = st == 2 ? (uint32_t)lane : (uint32_t)(a.b.last ? a.b.last[g * width + w] : a.b.eos);
+      if (lane < (int)n) list[lane] = sort_key(order_of(-INFINITY), token);
       continue;
     }
     // This wave's share of those quarters, four at a time.  COLLECT: the elements that are not below `least`, the smallest of the chunks' maxima

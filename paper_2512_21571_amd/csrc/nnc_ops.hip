@@ -224,7 +224,7 @@ nnc_status nnc_beam_select(const nnc_beam* beam, void* workspace, size_t workspa
   BeamSelect b;
   b.logits = beam->logits; b.dtype = (int)beam->dtype; b.row = beam->row_stride; b.group = beam->row_stride * (int64_t)beam->width;
   b.n_groups = beam->n_groups; b.width = beam->width; b.vocab = beam->vocab;
-  b.scores = beam->scores; b.finished = beam->finished; b.eos = beam->eos;
+  b.scores = beam->scores; b.finished = beam->finished; b.eos = beam->eos; b.last = nullptr;
   b.tokens = beam->tokens_out; b.parents = beam->parents_out; b.scores_out = beam->scores_out; b.finished_out = beam->finished_out;
   OPS_TRY(launch_beam_select(static_cast<hipStream_t>(stream), b, workspace));
   return NNC_OK;

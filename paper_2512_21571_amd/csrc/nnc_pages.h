@@ -279,6 +279,7 @@ struct BeamSelect {
   const float* scores;
   const uint8_t* finished;
   int32_t eos;
+  const int32_t* last;  // [rows] what a beam that has ended repeats, or NULL: eos
   int32_t *tokens, *parents;
   float* scores_out;
   uint8_t* finished_out;
