@@ -1,6 +1,7 @@
 """Build the gfx950 shared library in-tree with hipcc (no GPU needed to compile)."""
 from __future__ import annotations
 
+import glob
 import os
 import subprocess
 from concurrent.futures import ThreadPoolExecutor
@@ -10,7 +11,6 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libnnc.so")
 SOURCES = ["nnc_kernels.hip", "nnc_decode_mk.hip", "nnc_prefill.hip", "nnc_small.hip", "nnc_attn.hip", "nnc_pages.hip", "nnc_page_attn.hip", "nnc_beam.hip",
            "nnc_ops.hip", "nnc_api.hip", "nnc_plan.cpp"]
-HEADERS = [os.path.join(CSRC, "nnc_internal.h"), os.path.join(HERE, "..", "include", "nnc.h")]
 
 OBJ_DIR = os.path.join(HERE, "_build")
 HIPCC_FLAGS = [
@@ -27,11 +27,16 @@ HIPCC_FLAGS = [
 ]
 
 
+def headers() -> list[str]:
+    """Every header that a source may include: a change to one of them rebuilds all objects."""
+    return sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", "nnc.h")]
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
     t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
+    deps = [os.path.join(CSRC, s) for s in SOURCES] + headers()
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -49,7 +54,7 @@ def build(force: bool = True) -> str:
     """force: compile every source; otherwise only the sources newer than their object file
     (the sources are compiled side by side, one hipcc each, then linked)."""
     os.makedirs(OBJ_DIR, exist_ok=True)
-    hdr_time = max(os.path.getmtime(h) for h in HEADERS + [os.path.join(CSRC, n) for n in ("nnc_lanes.h", "nnc_half.h", "nnc_plan.h", "nnc_ahead.h", "nnc_pages.h")])
+    hdr_time = max(os.path.getmtime(h) for h in headers())
     jobs = []
     for src in SOURCES:
         sp, op = os.path.join(CSRC, src), os.path.join(OBJ_DIR, src + ".o")
