@@ -506,8 +506,8 @@ typedef struct {
  * logits of ended and unused beams are not looked at (every continuation of an unused one is -infinity).
  * Ties go to the lower beam, then to the lower token.  Sums in fp32 and wider; scores of different beams are
  * compared in 64 bits.  A logit of -infinity forbids its token (score -infinity: chosen only when
- * nothing else is left).  A beam with a NaN or a +infinity among its logits has NaN scores, and NaN ranks first, so that
- * such a failure shows; its tokens rank by logit.  width: up to 32.
+ * nothing else is left).  A beam with a NaN or a +infinity among its logits has NaN scores, but for the tokens that are
+ * forbidden, whose score stays -infinity; NaN ranks first, so that such a failure shows, and its tokens rank by logit.  width: up to 32.
  * workspace: nnc_beam_select_workspace bytes, on a multiple of 16.
  */
 nnc_status nnc_beam_select_workspace(const nnc_beam *beam, size_t *bytes);
