@@ -1,4 +1,4 @@
-"""The beam selection where its contract has an edge: failed beams with forbidden tokens."""
+"""The beam selection where its contract has an edge: failed beams with forbidden tokens, the error of the log-sum."""
 import math
 
 import numpy as np
@@ -39,3 +39,31 @@ def test_forbidden_tokens_of_a_failed_beam_stay_forbidden(nnc, rows, v, failure)
     tokens, parents, out, _ = nnc.beam_select(x, scores)
     assert tokens[0, :3].tolist() == [top, 9, 7] and out[0, :3].isnan().all() and (out[0, 3:] == -math.inf).all()
     assert parents[0, 3:].tolist() == [0] * 3 and tokens[0, 3:].tolist() == [0, 1, 2]
+
+
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("v", [40, 1024, 33000, 151936, 600000])
+@pytest.mark.parametrize("scale,offset", [(0.01, 0.0), (2.5, 0.0), (6.0, 0.0), (2.5, 800.0)])
+def test_the_log_sum_is_good_to_fp32(nnc, rows, v, scale, offset):
+    """Seen in scores next to zero (a beam that begins at its log-sum less its best logit), whose own rounding is below 2^-40.  An
+    exponential is off by 2^-23, its exponent (17 in base 2 at most where weight is) by 2^-24 of itself in the scan and again
+    when chunks are joined, 24 roundings of sums: 52 x 2^-24 and less in all, below 2^-18."""
+    gen = torch.Generator(device=DEV).manual_seed(v)
+    x = (torch.randn((16, 1, v), generator=gen, device=DEV) * scale + offset).to(pu.ROWS[rows])
+    d = x.double()
+    top = d.amax(-1)
+    lse = top + torch.log(torch.exp(d - top[..., None]).sum(-1))
+    start = (lse - top).float()
+    got = nnc.beam_select(x, start)
+    assert torch.equal(got[0], (x == x.amax(-1, keepdim=True)).int().argmax(-1).int())
+    assert float((got[2].double() - (start.double() + (top - lse))).abs().max()) <= 2.0 ** -18
+
+
+def test_equal_rows_have_equal_log_sums(nnc):
+    """Whatever the alignment of a row, so that a tie of two beams is a tie: the lower beam first."""
+    for v in (999, 20011, 151936):
+        gen = torch.Generator(device=DEV).manual_seed(v)
+        wide = torch.zeros((8, v + 1), device=DEV, dtype=torch.bfloat16)
+        wide[:, :v] = torch.randn(v, generator=gen, device=DEV)
+        tokens, parents, out, _ = nnc.beam_select(wide[:, :v][None], torch.full((1, 8), -3.0, device=DEV))
+        assert parents[0].tolist() == list(range(8)) and len(set(out[0].tolist())) == 1 and len(set(tokens[0].tolist())) == 1
