@@ -1,4 +1,5 @@
-"""The beam selection where its contract has an edge: failed beams with forbidden tokens, the error of the log-sum."""
+"""The beam selection where its contract has an edge: failed beams with forbidden tokens, the error of the log-sum;
+and wide searches over rows of more chunks than beams, where a wave looks into the best chunks of one beam or of two."""
 import math
 
 import numpy as np
@@ -67,3 +68,41 @@ def test_equal_rows_have_equal_log_sums(nnc):
         wide[:, :v] = torch.randn(v, generator=gen, device=DEV)
         tokens, parents, out, _ = nnc.beam_select(wide[:, :v][None], torch.full((1, 8), -3.0, device=DEV))
         assert parents[0].tolist() == list(range(8)) and len(set(out[0].tolist())) == 1 and len(set(tokens[0].tolist())) == 1
+
+
+WIDE = [(2, 12, 151936), (1, 16, 33000), (3, 9, 9217), (1, 17, 40000), (1, 24, 300001), (1, 32, 151936)]
+
+
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("g,w,v", WIDE)
+def test_wide_searches(nnc, rows, g, w, v):
+    gen = torch.Generator(device=DEV).manual_seed(v)
+    logits = (torch.randn((g * w, v + 3), generator=gen, device=DEV) * 3).to(pu.ROWS[rows])[:, 3:].unflatten(0, (g, w))
+    scores = -torch.rand((g, w), generator=gen, device=DEV) * 0.5 - 20      # (close together: every beam has its share of the best)
+    check_select(nnc, logits, scores)
+    finished = torch.rand((g, w), generator=gen, device=DEV) < 0.3
+    check_select(nnc, logits, scores, finished, v // 2)
+    check_select(nnc, logits.masked_fill(torch.rand((g, w, v), generator=gen, device=DEV) < 0.7, -math.inf), scores, finished, v // 2)
+    scores[:, 1:] = -math.inf                                               # one beam alone has all the continuations
+    check_select(nnc, logits, scores)
+
+
+@pytest.mark.parametrize("rows", list(pu.ROWS))
+@pytest.mark.parametrize("g,w,v", [(1, 16, 33000), (1, 17, 40000), (1, 32, 66000)])
+def test_wide_searches_where_the_best_are_neighbours_or_equal(nnc, rows, g, w, v):
+    """More candidates than a wave collects at once, in both of its beams and in one of them: the bar is raised, or every place looked for."""
+    gen = torch.Generator(device=DEV).manual_seed(w)
+    scores = -torch.rand((g, w), generator=gen, device=DEV) * 0.01 - 1
+    logits = torch.randn((g, w, v), generator=gen, device=DEV)
+    down, few = logits.sort(-1, descending=True)[0], (logits * 0.4).round()
+    check_select(nnc, down.to(pu.ROWS[rows]), scores)
+    check_select(nnc, logits.sort(-1)[0].to(pu.ROWS[rows]), scores)
+    check_select(nnc, few.to(pu.ROWS[rows]), scores)
+    check_select(nnc, torch.full_like(logits, 1.25).to(pu.ROWS[rows]), scores)
+    mixed = logits.clone()
+    mixed[:, ::2], mixed[:, 1::3] = few[:, ::2], down[:, 1::3]
+    check_select(nnc, mixed.to(pu.ROWS[rows]), scores)
+    stripe = logits.clone()                                                 # two large values in every quarter, always in the same lane
+    stripe[:, :, 8:v:256] += 20
+    stripe[:, :, 9:v:256] += 20
+    check_select(nnc, stripe.to(pu.ROWS[rows]), scores)
