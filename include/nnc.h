@@ -321,7 +321,8 @@ nnc_status nnc_set_option(nnc_model *m, nnc_option opt, int32_t value);
  * Per-kernel timing with HIP events on the model's stream.  After
  * nnc_profile_begin, every launch of the forward pass runs eagerly and is
  * bracketed by events; nnc_profile_end synchronises, stops profiling and fills up
- * to `cap` records (host), returning the number written in *n_out.
+ * to `cap` records (host), returning the number written in *n_out.  (A step on pages waits for the
+ * stream once while it is profiled: the lengths that its bytes follow from lie in device memory.)
  */
 typedef struct {
   char name[48];        /* kernel family, e.g. "attn_partial"; the skinny GEMM reports one record per

@@ -411,6 +411,11 @@ void plan_skinny(const nnc_model* m, GemmArgs& a, int epi, int max_slices, bool 
   a.kts_per_split = pl.kts_per_split;
 }
 
+// Bytes of one cached position of a layer in pages: K and V of every kv head, with their scales.
+double page_row_bytes(const nnc_model* m, int store) {
+  return 2.0 * (m->Dkv() * page_elem_bytes(store) + (page_scaled(store) ? m->c.n_kv_heads * 4.0 : 0.0));
+}
+
 struct Pass {
   int ncols = 0;          // sequences (columns) in the pass
   int nsplit = 1;         // bf16 pieces per activation
@@ -498,7 +503,7 @@ nnc_status run_pass(nnc_model* m, const Pass& p) {
       a.packed = m->Ap; a.pk_dt = dt; a.NC = nc; a.nsplit = ns;
       // (the workspace holds max_chunks records of 132 words for each of MAX_COLS columns and query head)
       const PageAttnPlan plan = plan_page_attention(pool, (uint32_t)n, a, (uint32_t)(MAX_COLS * m->max_chunks / n));
-      RUN(FAM_PAGE_ATTN, p.kv_rows * 2.0 * Dkv * page_elem_bytes(pool.store), p.kv_rows * 4.0 * Dq,
+      RUN(FAM_PAGE_ATTN, p.kv_rows * page_row_bytes(m, pool.store), p.kv_rows * 4.0 * Dq,
           launch_page_attention(s, pool, p.table, a, plan, m->partial));
     } else {
       const AttnFuseArgs fz{L.g_q, L.g_k, c.rms_eps, m->rope, qkv_slices, (long)n * Nqkv};
@@ -1972,7 +1977,12 @@ nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& tab
   p.pages = pages;
   p.table = table;
   p.max_len = max_len + 1;
-  p.kv_rows = (double)n * p.max_len;
+  if (m->profiling && !being_captured(m)) {  // (the lengths lie in device memory; a column that is not run has position -2)
+    int32_t pos[MAX_DECODE_BATCH];
+    HIP_TRY(hipMemcpyAsync(pos, m->st->pos, n * 4, hipMemcpyDeviceToHost, m->stream));
+    HIP_TRY(hipStreamSynchronize(m->stream));
+    for (uint32_t i = 0; i < n; ++i) p.kv_rows += std::max(pos[i] + 1, 0);
+  }
   p.ncols = (int)n;
   p.nsplit = decode_nsplit(m, n);
   p.head_ncols = (int)n;
@@ -2007,7 +2017,7 @@ nnc_status nnc_pages_store(nnc_model* m, const nnc_pages* pages, const nnc_page_
     r.n = n;
     r.seq0 = (int32_t)seq;
     r.pos0 = (int32_t)pos0;
-    RUN(FAM_PAGE_ROWS, (double)n * 2 * m->Dkv() * (m->esz() + page_elem_bytes((int)pages->dtype)), 0,
+    RUN(FAM_PAGE_ROWS, n * (2.0 * m->Dkv() * m->esz() + page_row_bytes(m, (int)pages->dtype)), 0,
         launch_page_append(m->stream, pool_layer(pages, li), PageTable{table->entries, table->n_seqs, table->max_pages}, r));
   }
   return NNC_OK;
