@@ -297,8 +297,8 @@ class Pages:
     def _index(self, x, n, name):
         """seq or pos of n rows: (pointer, 0) of a tensor, (None, value) of a number."""
         if not isinstance(x, self.torch.Tensor):
-            if not -0x80000000 <= x <= 0x7fffffff:   # (ctypes would drop the upper bits)
-                _bad(f"{name}: {x} has more than 32 bits")
+            if not -0x80000000 <= x <= 0x7fffffff or int(x) != x:   # (ctypes would drop the upper bits, int what is behind the point)
+                _bad(f"{name}: {x} is no whole number of 32 bits")
             return None, int(x)
         if x.dtype != self._i32 or x.shape != (n,) or x.device != self.device or not x.is_contiguous():
             _bad(f"{name}: contiguous int32 [{n}] on {self.device} expected, not {x.dtype} {list(x.shape)} on {x.device}")

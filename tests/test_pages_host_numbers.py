@@ -60,3 +60,21 @@ def test_what_fits_goes_on(nnc, model):
         m.decode_step_paged(p, tables, lens, tokens, max_len=7)
     with pytest.raises(AssertionError, match="nnc_decode_beam"):
         m.decode_beam(p, tables, lens, 3, first_logits=torch.zeros((1, 100)), width=2, max_len=(1 << 31) - 1)
+
+
+def test_positions_between_two_positions(nnc, model, monkeypatch):
+    """Position 2.7 is not position 2."""
+    import torch
+    _, p, tables, _, _ = model
+    p.n_layers, p.n_kv_heads, p.head_dim, p._desc = 1, 2, 64, None
+    x = torch.zeros((3, 2, 64))
+
+    def called(*args):
+        raise AssertionError("called")
+
+    monkeypatch.setattr(nnc, "_enqueue", called)
+    for seq, pos in ((0.5, 0), (0, 2.7), (0, float("nan")), (float("inf"), 0)):
+        refused(nnc, p.append, 0, x, x, tables, seq, pos)
+        refused(nnc, p.read, 0, tables, seq, pos, k=x)
+    with pytest.raises(AssertionError, match="called"):
+        p.append(0, x, x, tables, 1.0, 2)
