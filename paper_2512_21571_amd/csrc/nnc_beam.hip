@@ -107,7 +107,7 @@ __device__ __forceinline__ const void* row_of(const SelArgs& a, uint32_t g, uint
 }
 
 // Bound: the logits' bytes, and about half as long the vector instructions, one exponential and five others per logit (128 rows of
-// 151936 bf16 logits, 39 MB, 10.7 us: 3.6 TB/s; 4 rows of fp32 3.5 us, of which a launch is half).  With a test for NaN and a
+// 151936 bf16 logits, 39 MB, 11.1 us: 3.5 TB/s; 4 rows of fp32 3.5 us, of which a launch is half).  With a test for NaN and a
 // subtraction in front of the product for every logit 12.6 us; two or four chunks a wave 14.2, 15.1; looking for the best elements
 // here, in every chunk, 70.
 template <int DT>
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256) void k_beam_scan(SelArgs a) {
 // First a wave for every beam finds its best chunks (another one its log-sum), then `share` waves look into them and leave up to
 // `width` keys each, best first, then one wave merges those lists.  Bound: latency and, with sixteen
 // waves on one CU, the issue of instructions; so what one wave can find is not found by all, and an element that is no candidate
-// costs a comparison.  1 x 4 beams 8.5 us, 16 x 8 beams 11.5, 1 x 16 beams 21 (4 / 8 beams with every wave choosing the chunks, one chunk on its
+// costs a comparison.  1 x 4 beams 8.5 us, 16 x 8 beams 11.5, 1 x 16 beams 22, 1 x 32 beams 66 (4 / 8 beams with every wave choosing the chunks, one chunk on its
 // way at a time and the first wave taking the lists' heads in turn: 14 / 28; whole chunks in place of quarters 8.0 / 14, 16 beams 28).
 template <int DT>
 __global__ __launch_bounds__(64 * PICK_WAVES) void k_beam_pick(SelArgs a) {

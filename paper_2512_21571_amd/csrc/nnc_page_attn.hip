@@ -150,7 +150,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Part& w, const f
 // fp32 pages, on the fp32 matrix instruction (16 x 16 x 4), tiles of 16 positions.  Its operands are one value per lane, so
 // nothing has to be turned: for S^T = K Q^T lane (c, g) loads dims 16 i + 4 g .. + 3 of row c and product j takes element j
 // (the sum over dims may run in any order that both operands share); for O^T = V^T P^T product (i, b, j) takes dim 64 b + 4 c + j of row
-// 4 g + i, whose weight the lane holds.  4 sequences of 4096 positions, 8 kv heads: 28 us, 4.8 TB/s.
+// 4 g + i, whose weight the lane holds.  4 sequences of 4096 positions, 8 kv heads: 27.9 us, 4.8 TB/s.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_tiles) {
   constexpr int LD = D / 16, NB = D / 64, OPITCH = D + 4;
@@ -334,12 +334,14 @@ __device__ __forceinline__ u32x2_v lds_column4(const char* p) {
 // bits and e4m3 values are exact in bf16; their row scales multiply scores and weights.  Binary16 products: weights are
 // carried 2^10 larger and fp32 queries at a power of two near 2^14, so that the pieces are normal numbers.
 //
-// Bound: the cache's bytes, which two workgroups of a CU keep on their way with two tiles of every wave (16 sequences of 4096
-// positions, 8 kv heads, bf16: 50 us, 5.3 TB/s; one of 131072, e4m3: 52 us, 5.3 TB/s; 48 of 1 .. 6000, int8: 70 us, 4.3 TB/s, where
-// the sequences' ends do not meet; a copy reaches 4.85 TB/s).  With the table read in front of the rows of the same tile,
-// which then wait for it, and e4m3 widened by way of fp32, these were 57, 71 and 100.  Short sequences: latency (one of 100 positions
-// 6.7 us, 7.5 with the queries and the table of the second tile asked for later).  int8 with 16-bit queries is held to 168 registers,
-// three workgroups a CU (64 sequences of 2048 57 us, two workgroups 59; 48 of 1 .. 6000 70, 77); e4m3 spills at that (57 us at two, 68 at three).  V^T by LDS, not by a transposed cache: the
+// Bound: the cache's bytes and the serial part of a workgroup (first table entries, the four waves' merge); two workgroups of a CU keep
+// two tiles of every wave on their way.  16 sequences of 4096 positions, 8 kv heads, bf16: 49.4 us, 5.4 TB/s, with fp32 queries 51.8; one
+// of 131072, e4m3: 52.1 us, 5.3 TB/s; 48 of 1 .. 6000, int8: 73.8 us, 4.1 TB/s, where the sequences' ends do not meet.  A stream that only
+// reads reaches 6.2 TB/s.  With the table read in front of the rows of the same tile, which then wait for it, and e4m3
+// widened by way of fp32, these were 57 (fp32 queries), 100 and 71.  Short sequences: latency (one of 100 positions
+// 5.9 us, 0.8 more with the queries and the table of the second tile asked for later).  int8 with 16-bit queries is held to 168 registers,
+// three workgroups a CU (64 sequences of 2048 57.8 us, two workgroups 59.6; 48 of 1 .. 6000 alike, 72 to 74); e4m3 spills at that (one of
+// 131072 52 us at two, 58 at three).  V^T by LDS, not by a transposed cache: the
 // LDS path moves a few bytes per cycle of its 128, and a row stays a row for append, read and reorder.
 template <int STORE, int D, bool FULL>
 __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_attn_mc(AttnArgs a, int head_tiles) {
@@ -650,8 +652,9 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
 // (16384 positions of one sequence, 8 kv heads, bf16, us with the join: 64 splits 20.5, 128 25.0), while a split of 128 positions,
 // a tile for each of the four waves, is worth its join from 512 positions on (512 positions: 4 splits 10.0, none 12.7; 256: 11.0 and 8.9).
 // The lengths are not known here, only their bound: where sequences are several, more workgroups, of 1024 positions at least, share the
-// long ones when the short ones are done (32 sequences of 0 .. 4096, 2 / 4 splits: 79 / 68; 48 of 1 .. 6000, 3 / 5: 130 / 118; where
-// all are equally long it costs the join: 64 of 2048, 1 / 2 splits 98.6 / 101).
+// long ones when the short ones are done.  Without / with that, us a call with the join, bf16, int8, e4m3: 32 sequences of 0 .. 4096 (2 / 4 splits)
+// 75.4 / 67.8, 48.9 / 41.4, 44.5 / 43.2; 48 of 1 .. 6000 (2 / 5) 123.7 / 118.3, 72.4 / 76.4, 69.9 / 72.1; where all are equally long it
+// costs the join and more: 64 of 2048 (1 / 2) 94.8 / 100.6, 55.9 / 63.0.
 PageAttnPlan plan_page_attention(const PagePool& p, uint32_t n_seqs, const PageAttn& a, uint32_t max_splits) {
   const uint32_t span = a.window ? (a.window < a.max_len ? a.window : a.max_len) : a.max_len;
   const uint64_t rows = (uint64_t)n_seqs * a.n_q_heads;

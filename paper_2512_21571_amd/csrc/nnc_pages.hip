@@ -1,7 +1,8 @@
 // Rows into a paged KV cache and out of it, and the pages of beams that follow other beams.  Bound: memory traffic, and for few rows
-// the loads that wait for each other (index -> table -> row).  4096 rows of 8 heads x 128: bf16 -> e4m3 9.7 us, int8 -> bf16
-// 6.9 us (25.6 MB each, 5.3 us at the 4.85 TB/s of a large copy; every wave of these launches is resident at once, so what is
-// left is the chain of one of them); 16 rows of one decode step 3.2 us.
+// the loads that wait for each other (index -> table -> row).  4096 rows of 8 heads x 128, at the 4.85 TB/s of a large copy in brackets: bf16 -> e4m3
+// and int8 10.0 us (5.3), -> bf16 8.2 (6.9), -> fp32 12.3 (10.4); back to bf16 from int8 6.7 us (5.3), bf16 8.6 (6.9), fp32 10.0 (10.4).  Every wave
+// of these launches is resident at once.  The scattered scales of an append, four bytes to a line, are not written more than once: 8.9 MB leave
+// the caches where 8.65 have to.  16 rows of one decode step 3.2 us.
 #include <type_traits>
 
 #include "nnc_internal.h"
@@ -147,7 +148,7 @@ hipError_t launch_page_read(hipStream_t s, const PagePool& p, const PageTable& t
 
 // ---- beams -------------------------------------------------------------------------------------------------
 // Workgroups 0 .. nt - 1 of a group turn 256 table columns each, the others copy (16 beams, 28 layers x 8 heads x 26 rows of int8,
-// 48 MB in and out: 10.6 us, 4.5 TB/s; 4 beams, 36 layers x 8 x 11 rows of bf16, 13 MB: 5.1).  `before` and `after` may be the same
+// 49 MB in and out: 11.1 us, 4.4 TB/s; 4 beams, 36 layers x 8 x 11 rows of bf16, 13 MB: 5.6).  `before` and `after` may be the same
 // table and a beam's own page may be another beam's source: every thread loads what all beams need of its column (its 16
 // bytes) before it stores any of it, and no other thread touches that column.
 template <int W>
