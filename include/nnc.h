@@ -386,7 +386,8 @@ nnc_status nnc_plan_skinny_gemm_query(uint32_t rows, uint32_t k, uint32_t n_seq,
  * cache; nothing of this section is in it, all of it is defined here.)
  *
  * Operators of their own, without a model: nnc_page_append, nnc_page_read, nnc_page_attention,
- * nnc_page_reorder, nnc_beam_select.  They enqueue on `stream` (hipStream_t, NULL = default stream) of
+ * nnc_page_attention_shared, nnc_page_bound, nnc_page_pick, nnc_page_attention_picked, nnc_page_reorder, nnc_beam_select,
+ * nnc_draft_verify.  They enqueue on `stream` (hipStream_t, NULL = default stream) of
  * the current device, which must be the one that holds every buffer named in the call; they allocate
  * nothing, keep nothing and may be captured into a graph.  Buffers belong to the caller and must live
  * until the work has run; a workspace may serve any number of calls that follow each other in one
@@ -474,6 +475,85 @@ nnc_status nnc_page_attention(const nnc_pages *pages, uint32_t layer, const nnc_
                               const nnc_page_query *query, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Attention of rows that share the first positions of their contexts (a batch behind one prompt, the beams of a search, the new
+ * tokens of one sequence).  Query row g * width + w is row w of group g; query->lens: device [rows].
+ *   prefix not NULL: device [groups]; the table has a row for every query row.  Positions below prefix[g] are read once for
+ *     the whole group, through the table row of its first query row, the others through the row's own.  max_own: no row has
+ *     more positions behind its prefix (0: none has any).
+ *   prefix NULL: the table has a row for every group, whose query rows are new tokens of one sequence: row r sees its first lens[r]
+ *     positions, all of them read once (max_own is not looked at).
+ * The result of a row is that of nnc_page_attention for its length, but for the order of sums.  A length may end
+ * inside the prefix; it gives zeros where it is 0, and NaN where it is negative, above max_len or more than max_own behind the prefix, as
+ * does a negative prefix.  A row is NaN as a whole where one of its positions has no page or a value of V that is not finite
+ * and that other rows do not see.  What positions behind a row's own length hold does not reach it.  query->window must be 0.
+ * width: up to 65535; rows: up to 65535.  workspace: nnc_page_attention_shared_workspace bytes (which may be 0), on a multiple of 16.
+ */
+typedef struct {
+  uint32_t width;
+  const int32_t *prefix;
+  uint32_t max_own;
+} nnc_page_share;
+nnc_status nnc_page_attention_shared_workspace(const nnc_pages *pages, const nnc_page_table *table,
+                                               const nnc_page_query *query, const nnc_page_share *share, size_t *bytes);
+nnc_status nnc_page_attention_shared(const nnc_pages *pages, uint32_t layer, const nnc_page_table *table,
+                                     const nnc_page_query *query, const nnc_page_share *share, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
+/*
+ * Attention to a part of a long context: the pages whose keys promise the largest scores.
+ * nnc_page_bounds: for every page and kv head the smallest and the largest key, dimension by dimension, memory of the caller:
+ *   lo, hi  [n_layers][n_pages][n_kv_heads][head_dim], on a multiple of 16 bytes; in the pool's dtype, NNC_BF16 for pools of 8 bits
+ *           (whose values, with their scales, are rounded outwards: downwards in lo, upwards in hi)
+ */
+typedef struct {
+  void *lo, *hi;
+} nnc_page_bounds;
+
+/*
+ * Bring the bounds of a layer up to date: of every sequence i those of the pages that hold positions since[i] .. lens[i] - 1 (device
+ * arrays of n_seqs; since NULL: since0 for all), each from all of the page's positions below lens[i].  max_new: no sequence has more such
+ * positions (0: what the table holds); pages behind that many are left as they are.  A NaN among a page's keys makes the bounds of its dimension NaN.
+ * Nothing is done for a negative length or since, nor for a page that does not exist.
+ */
+nnc_status nnc_page_bound(const nnc_pages *pages, uint32_t layer, const nnc_page_bounds *bounds, const nnc_page_table *table,
+                          const int32_t *lens, const int32_t *since, int32_t since0, uint32_t max_new, void *stream);
+
+/* One query row per sequence, as in nnc_page_query, and how many pages it picks. */
+typedef struct {
+  const void *q;
+  uint32_t dtype, n_q_heads;
+  int64_t q_row_stride, q_head_stride;
+  const int32_t *lens;          /* device [n_seqs] */
+  uint32_t max_len;             /* none of them is larger; 0: what the table holds */
+  uint32_t keep;                /* pages picked for each kv head, 1 .. 65536 */
+  uint32_t first, last;         /* of them, the first ones and the last ones of the sequence, whatever they score; last >= 1 */
+  int32_t *tables_out;          /* device [n_seqs][n_kv_heads][keep] */
+  int32_t *lens_out;            /* device [n_seqs][n_kv_heads] */
+} nnc_pick;
+
+/*
+ * For every sequence and kv head, the `keep` pages with the largest scores, in the order of the sequence:
+ *   score of a page = the largest, over the query heads h of the kv head, of  sum_d max(q[h][d] lo[d], q[h][d] hi[d])
+ * which no key of the page exceeds.  (For a negative scale of the attention, pass -q.)  tables_out names them, -1 behind the last of them; lens_out
+ * is the number of their positions: all pages are full but the last one, which is the sequence's last.  Scores are
+ * formed and compared in 64 bits; ties go to the page that comes first.  A page that does not exist, and one whose score is NaN, comes before all others,
+ * so that it shows in the attention.  A length of 0 picks nothing; a negative length or one above max_len gives the
+ * length -1.  workspace: nnc_page_pick_workspace bytes, on a multiple of 16.
+ */
+nnc_status nnc_page_pick_workspace(const nnc_pages *pages, const nnc_page_table *table, const nnc_pick *pick, size_t *bytes);
+nnc_status nnc_page_pick(const nnc_pages *pages, uint32_t layer, const nnc_page_bounds *bounds, const nnc_page_table *table,
+                         const nnc_pick *pick, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * nnc_page_attention where every kv head has a table and a length of its own: row i * n_kv_heads + h of the table (n_seqs: sequences
+ * x kv heads), lens: device [n_seqs][n_kv_heads].  query->window must be 0.
+ */
+nnc_status nnc_page_attention_picked_workspace(const nnc_pages *pages, const nnc_page_table *table,
+                                               const nnc_page_query *query, size_t *bytes);
+nnc_status nnc_page_attention_picked(const nnc_pages *pages, uint32_t layer, const nnc_page_table *table,
+                                     const nnc_page_query *query, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Beams take over the cache of the beams that they continue.  Sequences g * width .. + width - 1 of the table are
  * the beams of group g, all of one length lens[g * width] (device [n_seqs]); parents: device [n_seqs], each
  * 0 .. width - 1 (another value: the beam continues itself).  With f full pages and r more rows:
@@ -515,8 +595,41 @@ typedef struct {
 nnc_status nnc_beam_select_workspace(const nnc_beam *beam, size_t *bytes);
 nnc_status nnc_beam_select(const nnc_beam *beam, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Drafted tokens of n sequences, up to k of each, and what the target and the draft think of them. */
+typedef struct {
+  const void *logits;         /* device, of the target: row i * (k + 1) + j at logits + that * row_stride, vocab elements of dtype:
+                                 the distribution of the token behind the first j drafts of sequence i */
+  const void *draft_logits;   /* ... of the draft: row i * k + j, that draft j was drawn from; NULL: drafts that were not drawn */
+  uint32_t dtype;             /* NNC_F32, NNC_BF16 or NNC_F16 */
+  int64_t row_stride, draft_row_stride;
+  uint32_t n, k, vocab;
+  const int32_t *drafts;      /* device [n][k] */
+  const int32_t *counts;      /* device [n]: drafts of each sequence, 0 .. k; NULL: k */
+  const float *uniforms;      /* device [n][k + 1], random numbers of [0, 1): one for each draft, the last one for the token behind them */
+  const float *temperatures;  /* device [n]; NULL: `temperature` for all.  0: the largest logit (the first of equals) has all the probability */
+  float temperature;
+  int32_t *tokens_out;        /* device [n][k + 1] */
+  int32_t *accepted_out;      /* device [n] */
+} nnc_drafts;
+
 /*
- * A model on pages.  The three calls below run on the model's stream like every other call on it; pages must have the
+ * Which drafts are kept, and the token behind them, so that the tokens are distributed as the target's would be:
+ *   p_j = softmax(logits_j / T), q_j = softmax(draft_logits_j / T), without draft_logits q_j = 1 for the draft itself
+ *   draft x_j is kept, as long as all before it are, if u_j q_j(x_j) < p_j(x_j)
+ *   then one token more: the first v for which  sum_{w <= v} r(w) > u_k sum_w r(w),  where r = max(p_j - q_j, 0) behind a draft that
+ *   was not kept (p_j itself if that is zero everywhere), and r = p_j of the row behind the last draft
+ * tokens_out: the kept drafts, that token, and -1 behind it; accepted_out: how many were kept.  Sums, exponentials and comparisons are in
+ * 64 bits (exponentials to 2^-47), and sums are taken in a fixed order: the same call gives the same tokens.  Rows behind a sequence's count are not looked at.
+ * A sequence whose count is none of 0 .. k or whose temperature is negative or not finite gives the token -1 and
+ * keeps nothing; where a row that has to be looked at has no distribution (a NaN, a +infinity, only -infinities), a draft is
+ * no token or a random number is NaN, the token there is -1, behind the drafts kept before.
+ * n (2 k + 1): up to 65535; workspace: nnc_draft_verify_workspace bytes, on a multiple of 16.
+ */
+nnc_status nnc_draft_verify_workspace(const nnc_drafts *drafts, size_t *bytes);
+nnc_status nnc_draft_verify(const nnc_drafts *drafts, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A model on pages.  The calls below run on the model's stream like every other call on it; pages must have the
  * model's layers, kv heads and head_dim, any dtype.  They do not touch the lengths of the model's slots.
  *
  * Copy positions pos0 .. pos0 + n - 1 of a slot's cache, all layers, to the same positions of sequence `seq` of the
@@ -536,6 +649,19 @@ nnc_status nnc_pages_store(nnc_model *m, const nnc_pages *pages, const nnc_page_
  */
 nnc_status nnc_decode_step_paged(nnc_model *m, const nnc_pages *pages, const nnc_page_table *table, int32_t *lens,
                                  uint32_t max_len, const int32_t *tokens, float *logits_out, int32_t *next_out);
+
+/*
+ * One pass over a token of each of the table's sequences and up to k drafts behind it: tokens: device [n_seqs][k + 1], token j of
+ * sequence i becomes position lens[i] + j, for j up to counts[i] (device, 0 .. k; NULL: k), in pages that must be there already; lens are
+ * not changed.  logits_out: device [n_seqs * (k + 1), vocab], what nnc_draft_verify takes; next_out: device [n_seqs * (k + 1)] or NULL.  A
+ * sequence of which a drafts are kept goes on with lens[i] + a + 1: what was cached behind that is overwritten and never looked at.
+ * Tokens behind the count, outside the vocabulary or at positions outside 0 .. max_len + k are not cached and
+ * have NaN logits; so has every token behind one that is not cached.  A pass reads a sequence's cache once for all of its tokens.  n_seqs * (k + 1): up to 21;
+ * max_len: as for nnc_decode_step_paged (no lens[i] is larger); sequences must not name the same page behind lens[i].
+ */
+nnc_status nnc_decode_step_drafts(nnc_model *m, const nnc_pages *pages, const nnc_page_table *table, const int32_t *lens,
+                                  uint32_t max_len, uint32_t k, const int32_t *tokens, const int32_t *counts,
+                                  float *logits_out, int32_t *next_out);
 
 /*
  * Beam search on the device: n_steps times a decode step of every beam, nnc_beam_select and nnc_page_reorder, without

@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libnnc.so")
-SOURCES = ["nnc_kernels.hip", "nnc_decode_mk.hip", "nnc_prefill.hip", "nnc_small.hip", "nnc_attn.hip", "nnc_pages.hip", "nnc_page_attn.hip", "nnc_beam.hip",
+SOURCES = ["nnc_kernels.hip", "nnc_decode_mk.hip", "nnc_prefill.hip", "nnc_small.hip", "nnc_attn.hip", "nnc_pages.hip", "nnc_page_attn.hip", "nnc_page_share.hip",
+           "nnc_page_pick.hip", "nnc_beam.hip", "nnc_verify.hip",
            "nnc_ops.hip", "nnc_api.hip", "nnc_plan.cpp"]
 
 OBJ_DIR = os.path.join(HERE, "_build")

@@ -36,6 +36,8 @@ EXPORTS = [
     "nnc_last_error", "nnc_plan_prefill_gemm_query", "nnc_plan_skinny_gemm_query",
     "nnc_page_append", "nnc_page_read", "nnc_page_attention_workspace", "nnc_page_attention", "nnc_page_reorder",
     "nnc_beam_select_workspace", "nnc_beam_select", "nnc_pages_store", "nnc_decode_step_paged", "nnc_decode_beam",
+    "nnc_page_attention_shared_workspace", "nnc_page_attention_shared", "nnc_page_attention_picked_workspace", "nnc_page_attention_picked",
+    "nnc_page_bound", "nnc_page_pick_workspace", "nnc_page_pick", "nnc_draft_verify_workspace", "nnc_draft_verify", "nnc_decode_step_drafts",
 ]
 
 
@@ -85,6 +87,27 @@ class NncPageQuery(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("dtype", ctypes.c_uint32), ("n_q_heads", ctypes.c_uint32)] + [
         (n, ctypes.c_int64) for n in ("q_row_stride", "q_head_stride", "out_row_stride", "out_head_stride")] + [
         ("lens", ctypes.c_void_p), ("max_len", ctypes.c_uint32), ("window", ctypes.c_uint32), ("scale", ctypes.c_float)]
+
+
+class NncPageShare(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_uint32), ("prefix", ctypes.c_void_p), ("max_own", ctypes.c_uint32)]
+
+
+class NncPageBounds(ctypes.Structure):
+    _fields_ = [("lo", ctypes.c_void_p), ("hi", ctypes.c_void_p)]
+
+
+class NncPick(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("dtype", ctypes.c_uint32), ("n_q_heads", ctypes.c_uint32), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("lens", ctypes.c_void_p)] + [(n, ctypes.c_uint32) for n in ("max_len", "keep", "first", "last")] + [
+        ("tables_out", ctypes.c_void_p), ("lens_out", ctypes.c_void_p)]
+
+
+class NncDrafts(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("draft_logits", ctypes.c_void_p), ("dtype", ctypes.c_uint32), ("row_stride", ctypes.c_int64),
+                ("draft_row_stride", ctypes.c_int64)] + [(n, ctypes.c_uint32) for n in ("n", "k", "vocab")] + [
+        (n, ctypes.c_void_p) for n in ("drafts", "counts", "uniforms", "temperatures")] + [("temperature", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("tokens_out", "accepted_out")]
 
 
 class NncBeam(ctypes.Structure):
@@ -150,6 +173,16 @@ def lib():
             "nnc_page_read": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageRows), vp]),
             "nnc_page_attention_workspace": (i32, [P(NncPages), P(NncPageTable), P(NncPageQuery), P(ctypes.c_size_t)]),
             "nnc_page_attention": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageQuery), vp, ctypes.c_size_t, vp]),
+            "nnc_page_attention_shared_workspace": (i32, [P(NncPages), P(NncPageTable), P(NncPageQuery), P(NncPageShare), P(ctypes.c_size_t)]),
+            "nnc_page_attention_shared": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageQuery), P(NncPageShare), vp, ctypes.c_size_t, vp]),
+            "nnc_page_attention_picked_workspace": (i32, [P(NncPages), P(NncPageTable), P(NncPageQuery), P(ctypes.c_size_t)]),
+            "nnc_page_attention_picked": (i32, [P(NncPages), u32, P(NncPageTable), P(NncPageQuery), vp, ctypes.c_size_t, vp]),
+            "nnc_page_bound": (i32, [P(NncPages), u32, P(NncPageBounds), P(NncPageTable), vp, vp, i32, u32, vp]),
+            "nnc_page_pick_workspace": (i32, [P(NncPages), P(NncPageTable), P(NncPick), P(ctypes.c_size_t)]),
+            "nnc_page_pick": (i32, [P(NncPages), u32, P(NncPageBounds), P(NncPageTable), P(NncPick), vp, ctypes.c_size_t, vp]),
+            "nnc_draft_verify_workspace": (i32, [P(NncDrafts), P(ctypes.c_size_t)]),
+            "nnc_draft_verify": (i32, [P(NncDrafts), vp, ctypes.c_size_t, vp]),
+            "nnc_decode_step_drafts": (i32, [vp, P(NncPages), P(NncPageTable), vp, u32, u32, vp, vp, vp, vp]),
             "nnc_page_reorder": (i32, [P(NncPages), P(NncPageTable), vp, vp, vp, u32, vp]),
             "nnc_beam_select_workspace": (i32, [P(NncBeam), P(ctypes.c_size_t)]),
             "nnc_beam_select": (i32, [P(NncBeam), vp, ctypes.c_size_t, vp]),
@@ -288,7 +321,9 @@ class Pages:
         scales = [torch.empty(shape[:-1], dtype=torch.float32, device=device) if dtype in (torch.int8, torch.float8_e4m3fn) else None for _ in range(2)]
         return cls(k, v, *scales)
 
-    def _table(self, tables, name="tables"):
+    def _table(self, tables, name="tables", heads=False):
+        if heads and tables.dim() == 3 and tables.shape[1] == self.n_kv_heads:   # (a table for every kv head)
+            tables = tables.flatten(0, 1)
         if tables.dtype != self._i32 or tables.dim() != 2 or tables.device != self.device or not tables.is_contiguous():
             _bad(f"{name}: contiguous int32 [sequences, pages] on {self.device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
         n, m = tables.shape
@@ -358,7 +393,18 @@ class Pages:
             _bad(f"layer {layer} of {self.n_layers}")
         return layer
 
-    def _query(self, q, n, lens, max_len, scale, window, out):
+    def _workspace(self, workspace, size, *args):
+        """(tensor to keep, pointer, bytes) of a call's workspace: what the caller passes, or a new one of size(*args) bytes."""
+        if workspace is None:
+            n = ctypes.c_size_t()
+            _check(size(*args, ctypes.byref(n)))
+            t = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device) if n.value else None
+            return t, _ptr(t), n.value
+        if workspace.device != self.device or not workspace.is_contiguous():
+            _bad("workspace: contiguous memory of the pool's device expected")
+        return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+    def _query(self, q, n, lens, max_len, scale, window, out, heads=False):
         if not (0 <= max_len <= 0x7fffffff and 0 <= window <= 0x7fffffff):
             _bad(f"max_len {max_len}, window {window}: 0 .. 2^31 - 1 expected")
         row, head = self._heads(q, n, "q")
@@ -367,8 +413,9 @@ class Pages:
             o_row, o_head = self._heads(out, n, "out")
             if out.shape != q.shape or out.dtype != q.dtype:
                 _bad("out: type and shape of q expected")
-        if lens.dtype != self._i32 or lens.shape != (n,) or lens.device != self.device or not lens.is_contiguous():
-            _bad(f"lens: contiguous int32 [{n}] on {self.device} expected, not {lens.dtype} {list(lens.shape)} on {lens.device}")
+        of = (n, self.n_kv_heads) if heads else (n,)
+        if lens.dtype != self._i32 or lens.shape != of or lens.device != self.device or not lens.is_contiguous():
+            _bad(f"lens: contiguous int32 {list(of)} on {self.device} expected, not {lens.dtype} {list(lens.shape)} on {lens.device}")
         return NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), q.shape[1], row, head, o_row, o_head, lens.data_ptr(), max_len, window,
                             self.head_dim ** -0.5 if scale is None else scale)
 
@@ -379,15 +426,23 @@ class Pages:
 
     def attention_workspace(self, q, tables, lens, max_len: int = 0, window: int = 0) -> int:
         """Bytes of workspace of the same call of `attention`."""
-        table = self._table(tables)
-        return self._attention_bytes(table, self._query(q, table.n_seqs, lens, max_len, None, window, None))
+        table, heads = self._table(tables, heads=True), tables.dim() == 3
+        query = self._query(q, q.shape[0] if heads else table.n_seqs, lens, max_len, None, window, None, heads)
+        if heads:
+            n = ctypes.c_size_t()
+            _check(lib().nnc_page_attention_picked_workspace(self._desc, ctypes.byref(table), ctypes.byref(query), ctypes.byref(n)))
+            return n.value
+        return self._attention_bytes(table, query)
 
     def attention(self, layer: int, q, tables, lens, max_len: int = 0, scale: float | None = None, window: int = 0, out=None, workspace=None):
         """One query row per sequence, q [sequences, query heads, head_dim], against the first lens[i] (int32) cached positions
         of each; max_len: an upper bound of lens (0: what the table holds); scale: 1 / sqrt(head_dim) unless given; window: only
-        that many last positions (0: all).  workspace: a tensor of attention_workspace bytes instead of a new one."""
+        that many last positions (0: all).  tables [sequences, kv heads, pages] with lens [sequences, kv heads], as `pick` leaves
+        them: every kv head has its own (then without a window).  workspace: a tensor of attention_workspace bytes instead of a new one."""
         if out is None:
             out = self.torch.empty_like(q, memory_format=self.torch.contiguous_format)
+        if tables.dim() == 3:
+            return self._attention_picked(layer, q, tables, lens, max_len, scale, window, out, workspace)
         table = self._table(tables)
         query = self._query(q, table.n_seqs, lens, max_len, scale, window, out)
         if workspace is None:
@@ -399,6 +454,117 @@ class Pages:
             size = workspace.numel() * workspace.element_size()
         _enqueue(self.device, lib().nnc_page_attention, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(query), _ptr(workspace), size)
         return out
+
+    def _attention_picked(self, layer, q, tables, lens, max_len, scale, window, out, workspace):
+        if tables.shape[1] != self.n_kv_heads:
+            _bad(f"tables: [sequences, {self.n_kv_heads}, pages] expected, not {list(tables.shape)}")
+        L, table = lib(), self._table(tables, heads=True)
+        query = self._query(q, tables.shape[0], lens, max_len, scale, window, out, True)
+        kept, at, size = self._workspace(workspace, L.nnc_page_attention_picked_workspace, self._desc, ctypes.byref(table), ctypes.byref(query))
+        _enqueue(self.device, L.nnc_page_attention_picked, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(query), at, size)
+        return out
+
+    def _share(self, q, tables, lens, prefix, max_len, max_own, scale, out):
+        """(table, query, share) of a call of attention_shared."""
+        if q.dim() != 4 or lens.shape != q.shape[:2] or q.shape[3] != self.head_dim:
+            _bad(f"q [groups, width, heads, {self.head_dim}] and lens [groups, width] expected, not {list(q.shape)} and {list(lens.shape)}")
+        groups, width, heads, _ = q.shape
+        rows = []
+        for name, x in (("q", q), ("out", out)):
+            if x is not None:
+                if x.shape != q.shape or x.dtype != q.dtype:
+                    _bad(f"{name}: type and shape of q expected")
+                between, row = x.stride()[:2]
+                if width == 1:
+                    row = between   # (one row a group: no rows are `row` apart)
+                if groups > 1 and between != width * row and x.numel():
+                    _bad(f"{name}: one distance between all rows expected")
+                rows.append(x.as_strided((groups * width, heads, self.head_dim), (row, *x.stride()[2:])))
+        if max_own is not None and not 0 <= max_own <= 0x7fffffff:
+            _bad(f"max_own {max_own}: 0 .. 2^31 - 1 expected")
+        if prefix is None:
+            if tables.dim() != 2 or tables.shape[0] != groups:
+                _bad(f"tables: a row for each of {groups} groups expected, not {list(tables.shape)}")
+        else:
+            tables = tables.flatten(0, 1) if tables.dim() == 3 and tables.is_contiguous() else tables
+            if tables.dim() != 2 or tables.shape[0] != groups * width:
+                _bad(f"tables: a row for each of {groups} x {width} sequences expected, not {list(tables.shape)}")
+            if prefix.dtype != self._i32 or prefix.shape != (groups,) or prefix.device != self.device or not prefix.is_contiguous():
+                _bad(f"prefix: contiguous int32 [{groups}] on {self.device} expected, not {prefix.dtype} {list(prefix.shape)} on {prefix.device}")
+        table = self._table(tables)
+        if not lens.is_contiguous():
+            _bad("lens: contiguous int32 [groups, width] expected")
+        query = self._query(rows[0], groups * width, lens.view(-1), max_len, scale, 0, rows[1] if out is not None else None)
+        if max_own is None:
+            max_own = max_len or table.max_pages * self.page_tokens
+        return table, query, NncPageShare(width, _ptr(prefix), max_own)
+
+    def attention_shared_workspace(self, q, tables, lens, prefix=None, max_len: int = 0, max_own: int | None = None) -> int:
+        """Bytes of workspace of the same call of `attention_shared`."""
+        if q.numel() == 0:
+            return 0
+        table, query, share = self._share(q, tables, lens, prefix, max_len, max_own, None, None)
+        n = ctypes.c_size_t()
+        _check(lib().nnc_page_attention_shared_workspace(self._desc, ctypes.byref(table), ctypes.byref(query), ctypes.byref(share), ctypes.byref(n)))
+        return n.value
+
+    def attention_shared(self, layer: int, q, tables, lens, prefix=None, max_len: int = 0, max_own: int | None = None, scale: float | None = None,
+                         out=None, workspace=None):
+        """Query rows q [groups, width, query heads, head_dim] against the first lens[g, w] (int32) cached positions of each, what the
+        rows of a group share being read once for all of them.  With prefix (int32 [groups]): a batch behind one prompt, or beams;
+        tables [groups, width, pages] or [groups * width, pages], the positions below prefix[g] are read through the group's first row.  Without:
+        new tokens of one sequence, tables [groups, pages].  max_len: an upper bound of lens (0: what the table holds); max_own: one of
+        what a row has behind its prefix (None: max_len's; 0: nothing).  workspace: a tensor of attention_shared_workspace bytes instead of a new one."""
+        L = lib()
+        if out is None:
+            out = self.torch.empty_like(q, memory_format=self.torch.contiguous_format)
+        table, query, share = self._share(q, tables, lens, prefix, max_len, max_own, scale, out)
+        layer = self._layer(layer)
+        if not table.n_seqs:
+            return out
+        kept, at, size = self._workspace(workspace, L.nnc_page_attention_shared_workspace, self._desc, ctypes.byref(table), ctypes.byref(query), ctypes.byref(share))
+        _enqueue(self.device, L.nnc_page_attention_shared, self._desc, layer, ctypes.byref(table), ctypes.byref(query), ctypes.byref(share), at, size)
+        return out
+
+    def empty_bounds(self):
+        """Two tensors (lo, hi) for the bounds of all pages: [layers, pages, kv heads, head_dim] of the pool's type, bfloat16 for 8 bits."""
+        dtype = self.torch.bfloat16 if self.dtype in (I8, E4M3) else self.k.dtype
+        return tuple(self.torch.empty((self.n_layers, self.n_pages, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in range(2))
+
+    def _bounds(self, bounds):
+        lo, hi = bounds
+        dtype = self.torch.bfloat16 if self.dtype in (I8, E4M3) else self.k.dtype
+        _on(self.device, dtype, (self.n_layers, self.n_pages, self.n_kv_heads, self.head_dim), lo=lo, hi=hi)
+        return NncPageBounds(lo.data_ptr(), hi.data_ptr())
+
+    def bound(self, layer: int, bounds, tables, lens, since=0, max_new: int = 0):
+        """Bring the bounds (lo, hi) of the pages up to date that hold positions since[i] .. lens[i] - 1 of every sequence: the smallest and
+        the largest key of each, dimension by dimension.  since: an int32 tensor [sequences] or one number; max_new: no sequence has more
+        such positions (0: what the table holds)."""
+        table = self._table(tables)
+        _count(0, max_new=max_new)
+        at, first = self._index(since, table.n_seqs, "since")
+        _on(self.device, self._i32, (table.n_seqs,), lens=lens)
+        b = self._bounds(bounds)
+        _enqueue(self.device, lib().nnc_page_bound, self._desc, self._layer(layer), ctypes.byref(b), ctypes.byref(table), lens.data_ptr(), at, first, max_new)
+
+    def pick(self, layer: int, bounds, q, tables, lens, keep: int, first: int = 1, last: int = 1, max_len: int = 0, workspace=None):
+        """The `keep` pages of every sequence and kv head that the query rows q [sequences, query heads, head_dim] may score highest on, by
+        the bounds (lo, hi) of their keys; the first and last ones of a sequence in any case.  Returns tables [sequences, kv heads, keep] and lens
+        [sequences, kv heads], int32, as `attention` takes them.  max_len: an upper bound of lens (0: what the table holds)."""
+        L, table = lib(), self._table(tables)
+        _count(0, max_len=max_len, first=first)
+        _count(1, keep=keep, last=last)
+        row, head = self._heads(q, table.n_seqs, "q")
+        _on(self.device, self._i32, (table.n_seqs,), lens=lens)
+        b = self._bounds(bounds)
+        picked = self.torch.empty((table.n_seqs, self.n_kv_heads, keep), dtype=self._i32, device=self.device)
+        seen = self.torch.empty((table.n_seqs, self.n_kv_heads), dtype=self._i32, device=self.device)
+        pick = NncPick(q.data_ptr(), _dtype_of(q), q.shape[1], row, head, lens.data_ptr(), max_len, keep, first, last, picked.data_ptr(), seen.data_ptr())
+        layer = self._layer(layer)
+        kept, at, size = self._workspace(workspace, L.nnc_page_pick_workspace, self._desc, ctypes.byref(table), ctypes.byref(pick))
+        _enqueue(self.device, L.nnc_page_pick, self._desc, layer, ctypes.byref(b), ctypes.byref(table), ctypes.byref(pick), at, size)
+        return picked, seen
 
     def reorder(self, before, after, lens, parents):
         """Beams take over the cache of their parents: tables before and after [groups * width, pages] (may be one tensor), lens
@@ -448,6 +614,55 @@ def beam_select(logits, scores, finished=None, eos: int = -1, workspace=None):
         size = workspace.numel() * workspace.element_size()
     _enqueue(device, L.nnc_beam_select, ctypes.byref(beam), workspace.data_ptr(), size)
     return tokens, parents, out, ended
+
+
+def _rows_apart(x, rows, name):
+    """Elements between the rows of a tensor [n, rows, vocab] whose rows are adjacent elements, all one distance apart."""
+    between, row, one = x.stride()
+    if x.shape[1] == 1:
+        row = between
+    if x.numel() and ((one != 1 and x.shape[2] > 1) or (x.shape[0] > 1 and between != rows * row)):
+        _bad(f"{name}: rows of adjacent elements, one distance between all rows, expected")
+    return row
+
+
+def draft_verify(logits, drafts, uniforms, draft_logits=None, counts=None, temperature=1.0, workspace=None):
+    """Which drafted tokens are kept and the token behind them (nnc_draft_verify): logits [n, k + 1, vocab] of the target (float32,
+    bfloat16, float16), drafts int32 [n, k], uniforms float32 [n, k + 1] of [0, 1), draft_logits [n, k, vocab] of the logits' type or None (drafts
+    that were not drawn), counts int32 [n] (0 .. k drafts each) or None, temperature: a number or float32 [n]; 0: greedy.
+    Returns tokens int32 [n, k + 1] (the kept drafts, one token more, then -1) and how many were kept, int32 [n]."""
+    L, torch = lib(), _torch
+    if logits.dim() != 3 or logits.device.type != "cuda":
+        _bad("logits: [n, k + 1, vocab] in device memory expected")
+    (n, rows, v), device = logits.shape, logits.device
+    if rows < 1:
+        _bad("logits: a row for every draft and one behind them expected")
+    row = _rows_apart(logits, rows, "logits")
+    draft_row = 0
+    if draft_logits is not None:
+        if draft_logits.dtype != logits.dtype or draft_logits.shape != (n, rows - 1, v) or draft_logits.device != device:
+            _bad(f"draft_logits: {logits.dtype} {[n, rows - 1, v]} on {device} expected, not {draft_logits.dtype} {list(draft_logits.shape)} on {draft_logits.device}")
+        draft_row = _rows_apart(draft_logits, rows - 1, "draft_logits")
+    _on(device, torch.int32, (n, rows - 1), drafts=drafts)
+    _on(device, torch.int32, (n,), counts=counts)
+    _on(device, torch.float32, (n, rows), uniforms=uniforms)
+    heat = temperature if isinstance(temperature, torch.Tensor) else None
+    _on(device, torch.float32, (n,), temperature=heat)
+    tokens = torch.empty((n, rows), dtype=torch.int32, device=device)
+    accepted = torch.empty((n,), dtype=torch.int32, device=device)
+    d = NncDrafts(logits.data_ptr(), _ptr(draft_logits), _dtype_of(logits), row, draft_row, n, rows - 1, v, drafts.data_ptr(), _ptr(counts),
+                  uniforms.data_ptr(), _ptr(heat), 1.0 if heat is not None else temperature, tokens.data_ptr(), accepted.data_ptr())
+    if workspace is None:
+        size = ctypes.c_size_t()
+        _check(L.nnc_draft_verify_workspace(ctypes.byref(d), ctypes.byref(size)))
+        size = size.value
+        workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _bad("workspace: contiguous memory of the logits' device expected")
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _enqueue(device, L.nnc_draft_verify, ctypes.byref(d), workspace.data_ptr(), size)
+    return tokens, accepted
 
 
 class Model:
@@ -640,6 +855,30 @@ class Model:
         try:
             _check(lib().nnc_decode_step_paged(self.h, ctypes.byref(pages.desc), ctypes.byref(table), lens.data_ptr(), max_len, tokens.data_ptr(),
                                                _ptr(logits), nxt.data_ptr()))
+        finally:
+            self._after()
+        return logits, nxt
+
+    def decode_step_drafts(self, pages: Pages, tables, lens, tokens, counts=None, max_len: int = 0, want_next: bool = False):
+        """nnc_decode_step_drafts: tokens int32 [sequences, k + 1], the newest token of each and k drafts behind it, become positions
+        lens[i] .. lens[i] + k (lens stay as they are); counts int32 [sequences]: drafts of each (None: k).  Returns logits
+        [sequences, k + 1, vocab], as draft_verify takes them, and the greedy tokens [sequences, k + 1] or None."""
+        _count(0, max_len=max_len)
+        table = self._paged(pages, tables)
+        b = tables.shape[0]
+        if tokens.dim() != 2 or tokens.shape[0] != b or tokens.shape[1] < 1:
+            _bad(f"tokens: int32 [{b}, drafts + 1] expected, not {list(tokens.shape)}")
+        k = tokens.shape[1] - 1
+        if b * (k + 1) > 21:
+            _bad(f"{b} sequences of {k} + 1 tokens (21 in all at most)")
+        _on(pages.device, self.torch.int32, (b,), lens=lens, counts=counts)
+        _on(pages.device, self.torch.int32, tokens.shape, tokens=tokens)
+        logits = self._empty((b, k + 1, self.V), self.torch.float32)
+        nxt = self._empty((b, k + 1), self.torch.int32) if want_next else None
+        self._before()
+        try:
+            _check(lib().nnc_decode_step_drafts(self.h, ctypes.byref(pages.desc), ctypes.byref(table), lens.data_ptr(), max_len, k, tokens.data_ptr(),
+                                                _ptr(counts), logits.data_ptr(), _ptr(nxt)))
         finally:
             self._after()
         return logits, nxt

@@ -435,7 +435,9 @@ struct Pass {
   int* pending_out = nullptr;  // hidden-state models: leave the last projection's partials unadded and say how many
   const nnc_pages* pages = nullptr;  // the cache is these pages (table, max_len) instead of the slots
   PageTable table{};
-  uint32_t max_len = 0;     // cached positions of the longest sequence, the new one among them
+  uint32_t max_len = 0;     // cached positions of the longest sequence, the new ones among them
+  double kv_seen = 0;       // (pages) the same where columns share rows: counted for each column that sees them
+  uint32_t width = 1;       // (pages) columns of a sequence, one position behind another: column i * width + j of sequence i
   bool decode = false;      // every column is a different slot: QK-norm, RoPE and the cache append may run inside the attention kernel
 };
 
@@ -502,9 +504,17 @@ nnc_status run_pass(nnc_model* m, const Pass& p) {
       a.scale = 0.08838834764831845f;
       a.packed = m->Ap; a.pk_dt = dt; a.NC = nc; a.nsplit = ns;
       // (the workspace holds max_chunks records of 132 words for each of MAX_COLS columns and query head)
-      const PageAttnPlan plan = plan_page_attention(pool, (uint32_t)n, a, (uint32_t)(MAX_COLS * m->max_chunks / n));
-      RUN(FAM_PAGE_ATTN, p.kv_rows * page_row_bytes(m, pool.store), p.kv_rows * 4.0 * Dq,
-          launch_page_attention(s, pool, p.table, a, plan, m->partial));
+      const uint32_t records = (uint32_t)(MAX_COLS * m->max_chunks / n);
+      if (p.width > 1) {
+        PageShare share;
+        share.width = p.width; share.n_rows = (uint32_t)n; share.per_group = true;
+        RUN(FAM_PAGE_ATTN, p.kv_rows * page_row_bytes(m, pool.store), p.kv_seen * 4.0 * Dq,
+            launch_page_share(s, pool, p.table, a, share, plan_page_share(pool, a, share, records), m->partial));
+      } else {
+        const PageAttnPlan plan = plan_page_attention(pool, (uint32_t)n, a, records);
+        RUN(FAM_PAGE_ATTN, p.kv_rows * page_row_bytes(m, pool.store), p.kv_rows * 4.0 * Dq,
+            launch_page_attention(s, pool, p.table, a, plan, m->partial));
+      }
     } else {
       const AttnFuseArgs fz{L.g_q, L.g_k, c.rms_eps, m->rope, qkv_slices, (long)n * Nqkv};
       if (!fuse)
@@ -1968,20 +1978,27 @@ nnc_status paged_room(const nnc_model* m, const nnc_pages* pages, uint32_t max_p
   return NNC_OK;
 }
 
-nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& table, int32_t* lens, uint32_t max_len, const int32_t* tokens,
-                      float* logits, int32_t* next) {
-  const uint32_t n = table.n_seqs;
-  HIP_TRY(launch_paged_state(m->stream, m->st, (int)n, tokens, lens, m->V(), max_len));
+// A pass of the columns whose state is set: `width` neighbouring positions of every sequence of the table.
+nnc_status paged_pass(nnc_model* m, const nnc_pages* pages, const PageTable& table, uint32_t width, uint32_t max_len, float* logits, int32_t* next) {
+  const uint32_t n = table.n_seqs * width;
   Pass p;
   p.decode = true;
   p.pages = pages;
   p.table = table;
-  p.max_len = max_len + 1;
+  p.width = width;
+  p.max_len = max_len + width;
   if (m->profiling && !being_captured(m)) {  // (the lengths lie in device memory; a column that is not run has position -2)
     int32_t pos[MAX_DECODE_BATCH];
     HIP_TRY(hipMemcpyAsync(pos, m->st->pos, n * 4, hipMemcpyDeviceToHost, m->stream));
     HIP_TRY(hipStreamSynchronize(m->stream));
-    for (uint32_t i = 0; i < n; ++i) p.kv_rows += std::max(pos[i] + 1, 0);
+    for (uint32_t i = 0; i < n; i += width) {  // (a sequence's rows are read once)
+      int32_t most = -1;
+      for (uint32_t j = 0; j < width; ++j) {
+        most = std::max(most, pos[i + j]);
+        p.kv_seen += std::max(pos[i + j] + 1, 0);
+      }
+      p.kv_rows += std::max(most + 1, 0);
+    }
   }
   p.ncols = (int)n;
   p.nsplit = decode_nsplit(m, n);
@@ -1990,6 +2007,12 @@ nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& tab
   p.logits_ld = m->V();
   p.next = next;
   return run_pass(m, p);
+}
+
+nnc_status paged_step(nnc_model* m, const nnc_pages* pages, const PageTable& table, int32_t* lens, uint32_t max_len, const int32_t* tokens,
+                      float* logits, int32_t* next) {
+  HIP_TRY(launch_paged_state(m->stream, m->st, (int)table.n_seqs, tokens, lens, m->V(), max_len));
+  return paged_pass(m, pages, table, 1, max_len, logits, next);
 }
 
 }  // namespace
@@ -2040,6 +2063,27 @@ nnc_status nnc_decode_step_paged(nnc_model* m, const nnc_pages* pages, const nnc
                                  logits_out ? logits_out : m->logits, next_out ? m->next : nullptr))
     return st;
   if (next_out) HIP_TRY(hipMemcpyAsync(next_out, m->next, table->n_seqs * 4, hipMemcpyDeviceToDevice, m->stream));
+  return fetch_tail_flag(m);
+}
+
+nnc_status nnc_decode_step_drafts(nnc_model* m, const nnc_pages* pages, const nnc_page_table* table, const int32_t* lens, uint32_t max_len,
+                                  uint32_t k, const int32_t* tokens, const int32_t* counts, float* logits_out, int32_t* next_out) {
+  if (!m || !lens || !tokens) return fail(NNC_E_ARG, "NULL argument");
+  if (!m->c.has_embed_and_head) return fail(NNC_E_STATE, "model has no embedding");
+  if (resident_failed(m, false))
+    return fail(NNC_E_DEVICE, "an earlier decode launch gave up waiting for its other workgroups; recreate the model");
+  if (nnc_status st = check_model_pages(m, pages)) return st;
+  if (nnc_status st = check_table(pages, table)) return st;
+  const uint64_t n = (uint64_t)table->n_seqs * ((uint64_t)k + 1);
+  if (n == 0 || n > MAX_DECODE_BATCH) return fail(NNC_E_ARG, "%u sequences of %u + 1 tokens (1 .. %u in all)", table->n_seqs, k, MAX_DECODE_BATCH);
+  uint32_t room = 0;
+  if (nnc_status st = paged_room(m, pages, table->max_pages, max_len, k + 1, &room)) return st;
+  const uint32_t most = max_len ? max_len : room - (k + 1);
+  HIP_TRY(launch_paged_state_drafts(m->stream, m->st, (int)n, (int)(k + 1), tokens, counts, lens, m->V(), most));
+  if (nnc_status st = paged_pass(m, pages, PageTable{table->entries, table->n_seqs, table->max_pages}, k + 1, most,
+                                 logits_out ? logits_out : m->logits, next_out ? m->next : nullptr))
+    return st;
+  if (next_out) HIP_TRY(hipMemcpyAsync(next_out, m->next, n * 4, hipMemcpyDeviceToDevice, m->stream));
   return fetch_tail_flag(m);
 }
 

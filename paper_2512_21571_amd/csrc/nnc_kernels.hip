@@ -205,6 +205,28 @@ hipError_t launch_paged_state(hipStream_t s, ColState* st, int ncols, const int3
   return hipGetLastError();
 }
 
+// The same for `width` neighbouring tokens of each sequence: column i * width + j is token j of sequence i at position lens[i] + j.
+// Behind a token that cannot be run, or behind counts[i], no other of that sequence is.
+__global__ __launch_bounds__(MAX_COLS) void k_paged_state_drafts(ColState* st, int ncols, int width, const int32_t* __restrict__ tok,
+                                                                 const int32_t* __restrict__ counts, const int32_t* __restrict__ lens,
+                                                                 uint32_t vocab, uint32_t max_len) {
+  const int c = threadIdx.x, i = c / width, j = c - i * width;
+  if (c >= ncols) return;
+  const int32_t n = lens[i], count = counts ? counts[i] : width - 1;
+  bool ok = (uint32_t)n <= max_len && j <= count && count < width;
+  for (int e = 0; e <= j; ++e) ok = ok && (uint32_t)tok[i * width + e] < vocab;
+  st->tok[c] = ok ? tok[c] : 0;
+  st->slot[c] = (uint32_t)i;
+  st->pos[c] = ok ? (uint32_t)(n + j) : (uint32_t)-2;
+  if (c == 0) st->step = 0;
+}
+
+hipError_t launch_paged_state_drafts(hipStream_t s, ColState* st, int ncols, int width, const int32_t* tok, const int32_t* counts,
+                                     const int32_t* lens, uint32_t vocab, uint32_t max_len) {
+  k_paged_state_drafts<<<1, MAX_COLS, 0, s>>>(st, ncols, width, tok, counts, lens, vocab, max_len);
+  return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------
 // embedding gather from the packed matrix: x[col][k] = E[tok[col]][k]
 // ---------------------------------------------------------------------------

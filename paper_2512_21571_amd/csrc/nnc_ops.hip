@@ -1,6 +1,8 @@
-// C entry points of the operators that need no model: a paged KV cache (append, read, decode attention, reordering of
-// beams) and the selection of a beam search.  Checks of what the host can see; table entries, positions and lengths lie in
+// C entry points of the operators that need no model: a paged KV cache (append, read, decode attention by one row, by rows
+// that share positions and over picked pages, bounds and picking of pages, reordering of beams), the selection of a beam
+// search and the verification of drafts.  Checks of what the host can see; table entries, positions and lengths lie in
 // device memory and are checked by the kernels.
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -133,6 +135,71 @@ nnc_status check_query(const nnc_pages* p, const nnc_page_table* t, const nnc_pa
   return NNC_OK;
 }
 
+// The rows of a call of nnc_page_attention_shared, whose table and query have passed check_query.
+nnc_status check_share(const nnc_page_table* t, const nnc_page_query* q, const nnc_page_share* s, PageShare& o) {
+  if (!s) return fail(NNC_E_ARG, "share is NULL");
+  if (s->width == 0 || s->width > 65535) return fail(NNC_E_ARG, "share: width %u (1 .. 65535)", s->width);
+  if (q->window) return fail(NNC_E_ARG, "query: no window in the attention of rows that share positions");
+  if (bad_align(s->prefix, 4)) return fail(NNC_E_ARG, "share: prefix must lie on a multiple of 4 bytes");
+  if ((uint64_t)s->width * q->n_q_heads > 1u << 27) return fail(NNC_E_ARG, "share: %u rows of %u query heads in a group (2^27 at most)", s->width, q->n_q_heads);
+  if (s->prefix && t->n_seqs % s->width) return fail(NNC_E_ARG, "share: %u rows are no groups of %u", t->n_seqs, s->width);
+  const uint64_t rows = s->prefix ? t->n_seqs : (uint64_t)t->n_seqs * s->width;
+  if (rows > 65535) return fail(NNC_E_ARG, "share: %llu rows (65535 at most)", (unsigned long long)rows);
+  o = PageShare{};
+  o.width = s->width; o.n_rows = (uint32_t)rows; o.per_group = !s->prefix; o.prefix = s->prefix; o.max_own = s->prefix ? s->max_own : 0;
+  return NNC_OK;
+}
+
+nnc_status check_picked(const nnc_pages* p, const nnc_page_table* t, const nnc_page_query* q, PageAttn& a) {
+  if (nnc_status st = check_query(p, t, q, a)) return st;
+  if (t->n_seqs % p->n_kv_heads) return fail(NNC_E_ARG, "%u rows of the table are no sequences of %u kv heads", t->n_seqs, p->n_kv_heads);
+  if (q->window) return fail(NNC_E_ARG, "query: no window over picked pages");
+  a.per_head = true;
+  return NNC_OK;
+}
+
+int bound_bytes(const nnc_pages* p) { return p->dtype == NNC_F32 ? 4 : 2; }
+nnc_status check_bounds(const nnc_page_bounds* b) {
+  if (!b) return fail(NNC_E_ARG, "bounds is NULL");
+  if (!b->lo || !b->hi || bad_align(b->lo, 16) || bad_align(b->hi, 16))
+    return fail(NNC_E_ARG, "bounds: lo and hi must be device memory on a multiple of 16 bytes");
+  return NNC_OK;
+}
+
+nnc_status check_pick(const nnc_pages* p, const nnc_page_table* t, const nnc_pick* k, PagePick& o) {
+  if (nnc_status st = check_pages(p)) return st;
+  if (nnc_status st = check_table(p, t)) return st;
+  if (!k) return fail(NNC_E_ARG, "pick is NULL");
+  if (k->dtype > NNC_F16) return fail(NNC_E_ARG, "pick: dtype %u is not one of fp32, bf16, binary16", k->dtype);
+  if (!k->n_q_heads || k->n_q_heads % p->n_kv_heads || k->n_q_heads > 65535)
+    return fail(NNC_E_ARG, "pick: %u query heads are no multiple of %u kv heads", k->n_q_heads, p->n_kv_heads);
+  const uint64_t cap = (uint64_t)t->max_pages * p->page_tokens;
+  if (t->n_seqs && k->max_len > cap) return fail(NNC_E_ARG, "pick: max_len %u, the table holds %llu positions", k->max_len, (unsigned long long)cap);
+  if (k->keep == 0 || k->keep > 65536) return fail(NNC_E_ARG, "pick: keep %u (1 .. 65536)", k->keep);
+  if (k->last == 0 || (uint64_t)k->first + k->last > k->keep)
+    return fail(NNC_E_ARG, "pick: the first %u and the last %u pages of %u (the last one at least, and no more than keep)", k->first, k->last, k->keep);
+  const size_t e = k->dtype == NNC_F32 ? 4 : 2;
+  if (bad_align(k->q, e) || bad_align(k->lens, 4) || bad_align(k->tables_out, 4) || bad_align(k->lens_out, 4))
+    return fail(NNC_E_ARG, "pick: not aligned to its elements");
+  o = PagePick{};
+  o.t = {t->entries, t->n_seqs, t->max_pages};
+  o.q = k->q; o.q_dtype = (int)k->dtype; o.q_row = k->q_row_stride; o.q_head = k->q_head_stride;
+  const int64_t per16 = k->dtype == NNC_F32 ? 4 : 8;
+  o.q_wide = !bad_align(k->q, 16) && k->q_row_stride % per16 == 0 && k->q_head_stride % per16 == 0;
+  o.n_q_heads = k->n_q_heads; o.lens = k->lens; o.max_len = k->max_len ? k->max_len : (uint32_t)cap;
+  o.blocks = (uint32_t)(((uint64_t)o.max_len + p->page_tokens - 1) / p->page_tokens);
+  o.keep = k->keep; o.first = k->first; o.last = k->last; o.tables_out = k->tables_out; o.lens_out = k->lens_out;
+  return NNC_OK;
+}
+
+nnc_status check_drafts(const nnc_drafts* d) {
+  if (!d) return fail(NNC_E_ARG, "drafts is NULL");
+  if (d->dtype > NNC_F16) return fail(NNC_E_ARG, "drafts: dtype %u is not one of fp32, bf16, binary16", d->dtype);
+  if (d->vocab == 0 || d->vocab > 0x7fffffffu) return fail(NNC_E_ARG, "drafts: vocab %u", d->vocab);
+  if (d->k > 0xffff || (uint64_t)d->n * (2ull * d->k + 1) > 65535) return fail(NNC_E_ARG, "drafts: %u sequences of %u drafts (n (2 k + 1) up to 65535)", d->n, d->k);
+  return NNC_OK;
+}
+
 nnc_status check_select(const nnc_beam* b) {
   if (!b) return fail(NNC_E_ARG, "beam is NULL");
   if (nnc_status st = check_beams(b->n_groups, b->width)) return st;
@@ -181,6 +248,139 @@ nnc_status nnc_page_attention(const nnc_pages* pages, uint32_t layer, const nnc_
   if (plan.floats && (!workspace || workspace_bytes < plan.floats * 4 || bad_align(workspace, 16)))
     return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, plan.floats * 4);
   OPS_TRY(launch_page_attention(static_cast<hipStream_t>(stream), p, table_of(table), a, plan, static_cast<float*>(workspace)));
+  return NNC_OK;
+}
+
+nnc_status nnc_page_attention_shared_workspace(const nnc_pages* pages, const nnc_page_table* table, const nnc_page_query* query,
+                                               const nnc_page_share* share, size_t* bytes) {
+  if (!bytes) return fail(NNC_E_ARG, "bytes is NULL");
+  PageAttn a;
+  PageShare s;
+  if (nnc_status st = check_query(pages, table, query, a)) return st;
+  if (nnc_status st = check_share(table, query, share, s)) return st;
+  *bytes = plan_page_share(pool_layer(pages, 0), a, s).floats * 4;
+  return NNC_OK;
+}
+
+nnc_status nnc_page_attention_shared(const nnc_pages* pages, uint32_t layer, const nnc_page_table* table, const nnc_page_query* query,
+                                     const nnc_page_share* share, void* workspace, size_t workspace_bytes, void* stream) {
+  PageAttn a;
+  PageShare s;
+  if (nnc_status st = check_query(pages, table, query, a)) return st;
+  if (nnc_status st = check_share(table, query, share, s)) return st;
+  if (layer >= pages->n_layers) return fail(NNC_E_ARG, "layer %u of %u", layer, pages->n_layers);
+  if (table->n_seqs == 0) return NNC_OK;
+  if (!query->q || !query->out || !query->lens) return fail(NNC_E_ARG, "query: q, out or lens is NULL");
+  const PagePool p = pool_layer(pages, layer);
+  const PageSharePlan plan = plan_page_share(p, a, s);
+  if (plan.floats && (!workspace || workspace_bytes < plan.floats * 4 || bad_align(workspace, 16)))
+    return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, plan.floats * 4);
+  OPS_TRY(launch_page_share(static_cast<hipStream_t>(stream), p, table_of(table), a, s, plan, static_cast<float*>(workspace)));
+  return NNC_OK;
+}
+
+nnc_status nnc_page_attention_picked_workspace(const nnc_pages* pages, const nnc_page_table* table, const nnc_page_query* query, size_t* bytes) {
+  if (!bytes) return fail(NNC_E_ARG, "bytes is NULL");
+  PageAttn a;
+  if (nnc_status st = check_picked(pages, table, query, a)) return st;
+  *bytes = plan_page_attention(pool_layer(pages, 0), table->n_seqs / pages->n_kv_heads, a).floats * 4;
+  return NNC_OK;
+}
+
+nnc_status nnc_page_attention_picked(const nnc_pages* pages, uint32_t layer, const nnc_page_table* table, const nnc_page_query* query,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  PageAttn a;
+  if (nnc_status st = check_picked(pages, table, query, a)) return st;
+  if (layer >= pages->n_layers) return fail(NNC_E_ARG, "layer %u of %u", layer, pages->n_layers);
+  if (table->n_seqs == 0) return NNC_OK;
+  if (!query->q || !query->out || !query->lens) return fail(NNC_E_ARG, "query: q, out or lens is NULL");
+  const PagePool p = pool_layer(pages, layer);
+  const PageAttnPlan plan = plan_page_attention(p, table->n_seqs / p.n_kv_heads, a);
+  if (plan.floats && (!workspace || workspace_bytes < plan.floats * 4 || bad_align(workspace, 16)))
+    return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, plan.floats * 4);
+  OPS_TRY(launch_page_attention(static_cast<hipStream_t>(stream), p, table_of(table), a, plan, static_cast<float*>(workspace)));
+  return NNC_OK;
+}
+
+nnc_status nnc_page_bound(const nnc_pages* pages, uint32_t layer, const nnc_page_bounds* bounds, const nnc_page_table* table,
+                          const int32_t* lens, const int32_t* since, int32_t since0, uint32_t max_new, void* stream) {
+  if (nnc_status st = check_pages(pages)) return st;
+  if (layer >= pages->n_layers) return fail(NNC_E_ARG, "layer %u of %u", layer, pages->n_layers);
+  if (nnc_status st = check_table(pages, table)) return st;
+  if (nnc_status st = check_bounds(bounds)) return st;
+  const uint64_t cap = (uint64_t)table->max_pages * pages->page_tokens;
+  if (!since && since0 < 0) return fail(NNC_E_ARG, "bounds since position %d", since0);
+  if (table->n_seqs == 0) return NNC_OK;
+  if (max_new > cap) return fail(NNC_E_ARG, "max_new %u, the table holds %llu positions", max_new, (unsigned long long)cap);
+  if (!lens || bad_align(lens, 4) || bad_align(since, 4)) return fail(NNC_E_ARG, "lens and since must be device memory on a multiple of 4 bytes");
+  PageBound b;
+  b.p = pool_layer(pages, layer);
+  b.t = table_of(table);
+  const size_t at = (size_t)layer * pages->n_pages * pages->n_kv_heads * pages->head_dim * bound_bytes(pages);
+  b.lo = static_cast<char*>(bounds->lo) + at;
+  b.hi = static_cast<char*>(bounds->hi) + at;
+  b.lens = lens; b.since = since; b.since0 = since0;
+  // (max_new neighbours lie in one page more than they fill, at most)
+  b.slots = max_new ? (uint32_t)std::min<uint64_t>(((uint64_t)max_new + pages->page_tokens - 2) / pages->page_tokens + 1, table->max_pages) : table->max_pages;
+  b.by_head = fast_div(pages->n_kv_heads);
+  if ((uint64_t)b.slots * pages->n_kv_heads > 0x3ffffffull) return fail(NNC_E_ARG, "%u pages x %u kv heads are too many for one call", b.slots, pages->n_kv_heads);
+  OPS_TRY(launch_page_bound(static_cast<hipStream_t>(stream), b));
+  return NNC_OK;
+}
+
+nnc_status nnc_page_pick_workspace(const nnc_pages* pages, const nnc_page_table* table, const nnc_pick* pick, size_t* bytes) {
+  if (!bytes) return fail(NNC_E_ARG, "bytes is NULL");
+  PagePick k;
+  if (nnc_status st = check_pick(pages, table, pick, k)) return st;
+  *bytes = k.blocks > k.keep ? page_pick_bytes(pool_layer(pages, 0), table->n_seqs, k.blocks) : 0;
+  return NNC_OK;
+}
+
+nnc_status nnc_page_pick(const nnc_pages* pages, uint32_t layer, const nnc_page_bounds* bounds, const nnc_page_table* table,
+                         const nnc_pick* pick, void* workspace, size_t workspace_bytes, void* stream) {
+  PagePick k;
+  if (nnc_status st = check_pick(pages, table, pick, k)) return st;
+  if (layer >= pages->n_layers) return fail(NNC_E_ARG, "layer %u of %u", layer, pages->n_layers);
+  if (nnc_status st = check_bounds(bounds)) return st;
+  if (table->n_seqs == 0) return NNC_OK;
+  if (!pick->q || !pick->lens || !pick->tables_out || !pick->lens_out) return fail(NNC_E_ARG, "pick: q, lens or an output is NULL");
+  k.p = pool_layer(pages, layer);
+  const size_t at = (size_t)layer * pages->n_pages * pages->n_kv_heads * pages->head_dim * bound_bytes(pages);
+  k.lo = static_cast<const char*>(bounds->lo) + at;
+  k.hi = static_cast<const char*>(bounds->hi) + at;
+  const size_t need = k.blocks > k.keep ? page_pick_bytes(k.p, table->n_seqs, k.blocks) : 0;
+  if (need && (!workspace || workspace_bytes < need || bad_align(workspace, 16)))
+    return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, need);
+  OPS_TRY(launch_page_pick(static_cast<hipStream_t>(stream), k, workspace));
+  return NNC_OK;
+}
+
+nnc_status nnc_draft_verify_workspace(const nnc_drafts* drafts, size_t* bytes) {
+  if (!bytes) return fail(NNC_E_ARG, "bytes is NULL");
+  if (nnc_status st = check_drafts(drafts)) return st;
+  *bytes = draft_verify_bytes(drafts->n, drafts->k, drafts->vocab, drafts->draft_logits != nullptr);
+  return NNC_OK;
+}
+
+nnc_status nnc_draft_verify(const nnc_drafts* drafts, void* workspace, size_t workspace_bytes, void* stream) {
+  if (nnc_status st = check_drafts(drafts)) return st;
+  const nnc_drafts& d = *drafts;
+  if (d.n == 0) return NNC_OK;
+  if (!d.logits || !d.uniforms || !d.tokens_out || !d.accepted_out || (d.k && !d.drafts))
+    return fail(NNC_E_ARG, "drafts: logits, drafts, uniforms or an output is NULL");
+  const size_t e = d.dtype == NNC_F32 ? 4 : 2;
+  if (bad_align(d.logits, e) || bad_align(d.draft_logits, e) || bad_align(d.drafts, 4) || bad_align(d.counts, 4) || bad_align(d.uniforms, 4) ||
+      bad_align(d.temperatures, 4) || bad_align(d.tokens_out, 4) || bad_align(d.accepted_out, 4))
+    return fail(NNC_E_ARG, "drafts: not aligned to its elements");
+  if (!d.temperatures && !(d.temperature >= 0.f && d.temperature - d.temperature == 0.f)) return fail(NNC_E_ARG, "drafts: temperature %g", (double)d.temperature);
+  DraftVerify v;
+  v.logits = d.logits; v.draft_logits = d.k ? d.draft_logits : nullptr; v.dtype = (int)d.dtype; v.row = d.row_stride; v.draft_row = d.draft_row_stride;
+  v.n = d.n; v.k = d.k; v.vocab = d.vocab; v.drafts = d.drafts; v.counts = d.counts; v.uniforms = d.uniforms;
+  v.temperatures = d.temperatures; v.temperature = d.temperature; v.tokens = d.tokens_out; v.accepted = d.accepted_out;
+  const size_t need = draft_verify_bytes(d.n, d.k, d.vocab, d.draft_logits != nullptr);
+  if (!workspace || workspace_bytes < need || bad_align(workspace, 16))
+    return fail(NNC_E_ARG, "workspace of %zu bytes on a multiple of 16; this call needs %zu", workspace ? workspace_bytes : 0, need);
+  OPS_TRY(launch_draft_verify(static_cast<hipStream_t>(stream), v, workspace));
   return NNC_OK;
 }
 

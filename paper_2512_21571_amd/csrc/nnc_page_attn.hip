@@ -1,56 +1,9 @@
-// Attention of one new token per sequence over a paged KV cache, split over the cache's length and joined.
-//   s_p = scale <q, k_p> over the positions p in reach,  o = sum_p e^(s_p - m) v_p / sum_p e^(s_p - m)
-// Each workgroup walks `chunk` positions of one sequence with a running maximum m, sum l and weighted sum; where a
-// sequence has several workgroups, k_page_attn_join merges their (m, l, sum) records.  Bound: the cache's bytes.
-#include <type_traits>
-#include <algorithm>
-
-#include "nnc_internal.h"
-#include "nnc_pages.h"
+// Attention of one new token per sequence over a paged KV cache: the kernels, their join and how a call is split.
+#include "nnc_page_attn.h"
 
 namespace nnc {
 
 namespace {
-
-struct AttnArgs {
-  PagePool p;
-  PageTable t;
-  PageAttn a;
-  PageAttnPlan plan;
-  float* part;  // [seq][head][split][head_dim] weighted sums, then [seq][head][split][2] maxima and sums
-  bool q_wide;  // query rows can be read sixteen bytes at a time
-};
-
-// Positions of a sequence that are attended to: lo .. hi - 1; bad: the length is no length of this cache.
-struct Reach {
-  uint32_t lo, hi;
-  bool bad;
-};
-__device__ __forceinline__ Reach reach(const AttnArgs& a, uint32_t seq) {
-  const int64_t len = (int64_t)a.a.lens[seq] + a.a.len_add;
-  if (len < 0 || len > a.a.max_len) return {0, 0, true};
-  const uint32_t hi = (uint32_t)len;
-  return {a.a.window && hi > a.a.window ? hi - a.a.window : 0u, hi, false};
-}
-
-__device__ __forceinline__ void store_out(const AttnArgs& a, uint32_t seq, uint32_t head, int dim, float v) {
-  if (a.a.packed) {  // k index of the projection = head * head_dim + dim
-    const size_t k = (size_t)head * a.p.head_dim + dim;
-    if (a.a.pk_dt == DT_F32) {
-      static_cast<float*>(a.a.packed)[((k >> 2) * a.a.NC + seq) * 4 + (k & 3)] = v;
-    } else {
-      uint32_t piece[3];
-      if (a.a.pk_dt == DT_BF16) split_pieces<Bf16>(v, a.a.nsplit, piece);
-      else split_pieces<Fp16>(v, a.a.nsplit, piece);
-      uint16_t* o = static_cast<uint16_t*>(a.a.packed) + ((k >> 3) * a.a.NC + (size_t)seq * a.a.nsplit) * 8 + (k & 7);
-      for (int s = 0; s < a.a.nsplit; ++s) o[s * 8] = (uint16_t)piece[s];
-    }
-    return;
-  }
-  const int64_t o = (int64_t)seq * a.a.o_row + (int64_t)head * a.a.o_head + dim;
-  if (a.a.q_dtype == DT_F32) static_cast<float*>(a.a.out)[o] = v;
-  else static_cast<uint16_t*>(a.a.out)[o] = (uint16_t)(a.a.q_dtype == DT_BF16 ? Bf16::bits(v) : Fp16::bits(v));
-}
 
 // A workgroup's heads: head0 .. + nh - 1 of one kv head.
 struct Heads {
@@ -74,77 +27,12 @@ __device__ __forceinline__ Part part_of(const AttnArgs& a, const Heads& h) {
   static_cast<Heads&>(w) = h;
   w.split = blockIdx.z;
   w.seq = blockIdx.y;
-  const Reach r = reach(a, w.seq);
+  const Reach r = reach(a, w.seq, h.kvh);
   w.begin = r.lo + w.split * a.plan.chunk;
   w.end = min(r.hi, w.begin + a.plan.chunk);
   w.bad = r.bad;
-  w.idle = w.split && w.begin >= w.end;  // (the first workgroup answers for an empty row)
+  w.idle = (w.split || a.slot) && w.begin >= w.end;  // (the first workgroup answers for an empty row)
   return w;
-}
-
-// The pages of a tile's rows, from the table.
-struct Finder {
-  const int32_t* entries;
-  FastDiv by_page;
-  uint32_t n_pages, page_tokens, page_rows, first_row, last;
-  __device__ __forceinline__ Finder(const AttnArgs& a, uint32_t seq, uint32_t kvh)
-      : entries(a.t.entries + (size_t)seq * a.t.max_pages), by_page(a.p.by_page), n_pages(a.p.n_pages), page_tokens(a.p.page_tokens),
-        page_rows(a.p.n_kv_heads * a.p.page_tokens), first_row(kvh * a.p.page_tokens), last(a.a.max_len ? a.a.max_len - 1 : 0) {}
-  // The entry of a position, and its row within that page's rows.  A position behind the sequence's end may be asked for too (up to
-  // max_len, which the table holds): its entry is a number that nothing is known about.
-  __device__ __forceinline__ void look(uint32_t pos, int32_t& page, uint32_t& row) const {
-    pos = min(pos, last);
-    const uint32_t e = fdiv(pos, by_page);
-    page = entries[e];
-    row = first_row + (pos - e * page_tokens);
-  }
-  // The row in the pool; `in`: the position is one of the sequence's, whose page has to exist.
-  __device__ __forceinline__ uint64_t at(int32_t page, uint32_t row, bool in, bool& missing) const {
-    const bool ok = (uint32_t)page < n_pages;
-    missing |= in && !ok;
-    return (uint64_t)(ok ? (uint32_t)page : 0u) * page_rows + row;
-  }
-};
-__device__ __forceinline__ uint64_t first_lane(uint64_t v) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) |
-         ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32);
-}
-
-// Eight query values at element o.
-__device__ __forceinline__ void load_query8(const AttnArgs& a, int64_t o, bool wide, float (&x)[8]) {
-  if (a.a.q_dtype == DT_F32) load8<DT_F32>(a.a.q, o, wide, x);
-  else if (a.a.q_dtype == DT_BF16) load8<DT_BF16>(a.a.q, o, wide, x);
-  else load8<DT_F16>(a.a.q, o, wide, x);
-}
-
-// The four waves' maxima and sums (smax, ssum [wave][head]) and weighted sums (out[wave * stride + head * pitch + dim], already
-// brought to the common maximum) -> output, or the workgroup's record.
-template <int D>
-__device__ __forceinline__ void finish(const AttnArgs& a, const Part& w, const float (&smax)[4][16], const float (&ssum)[4][16],
-                                       const float* out, int stride, int pitch) {
-  for (uint32_t e = threadIdx.x; e < w.nh * D; e += 256) {
-    const uint32_t h = e / D, d = e % D;
-    float L = 0.f, v = 0.f, M = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) M = fmaxf(M, smax[i][h]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float l = ssum[i][h];
-      L += l != l ? l : smax[i][h] == -INFINITY ? 0.f : l * __builtin_amdgcn_exp2f(smax[i][h] - M);
-      v += out[i * stride + h * pitch + d];
-    }
-    if (a.plan.splits == 1) {
-      store_out(a, w.seq, w.head0 + h, (int)d, L == 0.f ? 0.f : v / L);
-    } else {
-      const size_t rec = ((size_t)w.seq * a.a.n_q_heads + w.head0 + h) * a.plan.splits + w.split;
-      a.part[rec * D + d] = v;
-      if (d == 0) {
-        float* ml = a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D + rec * 2;
-        ml[0] = M;
-        ml[1] = L;
-      }
-    }
-  }
 }
 
 // fp32 pages, on the fp32 matrix instruction (16 x 16 x 4), tiles of 16 positions.  Its operands are one value per lane, so
@@ -165,22 +53,23 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
     int32_t page[5];
     uint32_t row[5];
   };
-  const Finder find(a, blockIdx.y, blockIdx.x / head_tiles);
+  const Finder find(a, table_row(a, blockIdx.y, blockIdx.x / head_tiles), blockIdx.x / head_tiles);
   bool missing = false;
   auto look = [&](Where& t, uint32_t p0) __attribute__((always_inline)) {
     find.look(p0 + c, t.page[4], t.row[4]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) find.look(p0 + g * 4 + i, t.page[i], t.row[i]);
   };
+  const bool moved = a.a.window || a.s.prefix;  // (the first position depends on the length)
   Where here, next;
-  if (!a.a.window) {
+  if (!moved) {
     look(here, blockIdx.z * a.plan.chunk + wave * 16);
     look(next, blockIdx.z * a.plan.chunk + wave * 16 + 64);
   }
   const Part w = part_of(a, heads_of(a, head_tiles));
   if (w.idle) return;
   uint32_t p0 = w.begin + wave * 16;
-  if (a.a.window) {
+  if (moved) {
     look(here, p0);
     look(next, p0 + 64);
   }
@@ -295,32 +184,11 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
             f32x4_t{acc[b][0][e], acc[b][1][e], acc[b][2][e], acc[b][3][e]} * r;
   }
   __syncthreads();
-  finish<D>(a, w, smax, ssum, out[0], 16 * OPITCH, OPITCH);
-}
-
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_v __attribute__((ext_vector_type(2)));
-
-// Eight 16-bit elements of the matrix cores' type out of what was cached.
-template <int STORE>
-__device__ __forceinline__ u32x4_v widen8_bf16(uint32_t lo, uint32_t hi) {
-  if constexpr (STORE == PS_I8) {
-    return Bf16W8::widen8(lo, hi);
-  } else {
-    auto two = [](uint32_t w, auto high) __attribute__((always_inline)) {
-      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, decltype(high)::value));
-    };
-    const std::false_type l{};
-    const std::true_type h{};
-    return u32x4_v{two(lo, l), two(lo, h), two(hi, l), two(hi, h)};
-  }
-}
-
-// 4 x 16 elements of 16 bits, the four rows `pitch` apart: lane c of a group of sixteen gets column c.  (Lane c asks for the
-// eight bytes of row c / 4 at column 4 (c % 4).)
-__device__ __forceinline__ u32x2_v lds_column4(const char* p) {
-  typedef __attribute__((address_space(3))) i16x4 lds_t;
-  return __builtin_bit_cast(u32x2_v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)p));
+  const auto row = [&](uint32_t h, uint32_t& seq, uint32_t& head) __attribute__((always_inline)) {
+    seq = w.seq;
+    head = w.head0 + h;
+  };
+  finish<D>(a, w.nh, w.split, row, smax, ssum, out[0], 16 * OPITCH, OPITCH);
 }
 
 // Up to sixteen query heads of one kv head per workgroup, a wave walking tiles of 32 positions, both products on the matrix cores.
@@ -367,7 +235,7 @@ __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_a
     int32_t page[2];
     uint32_t row[2];
   };
-  const Finder find(a, blockIdx.y, blockIdx.x / head_tiles);
+  const Finder find(a, table_row(a, blockIdx.y, blockIdx.x / head_tiles), blockIdx.x / head_tiles);
   bool missing = false;
   auto look = [&](Where& p, uint32_t p0) __attribute__((always_inline)) {
 #pragma unroll
@@ -394,8 +262,9 @@ __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_a
       }
     }
   }
+  const bool moved = a.a.window || a.s.prefix;  // (the first position depends on the length)
   Where here, next;
-  if (!a.a.window) {
+  if (!moved) {
     look(here, blockIdx.z * a.plan.chunk + wave * 32);
     look(next, blockIdx.z * a.plan.chunk + wave * 32 + 128);
   }
@@ -403,7 +272,7 @@ __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_a
   if (w.idle) return;
   const uint32_t end = w.end;
   uint32_t p0 = w.begin + wave * 32;
-  if (a.a.window) {
+  if (moved) {
     look(here, p0);
     look(next, p0 + 128);
   }
@@ -595,7 +464,11 @@ __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_a
     for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o + c * OPITCH + dt * 16 + g * 4) = acc[dt] * f;
   }
   __syncthreads();
-  finish<D>(a, w, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
+  const auto row = [&](uint32_t h, uint32_t& seq, uint32_t& head) __attribute__((always_inline)) {
+    seq = w.seq;
+    head = w.head0 + h;
+  };
+  finish<D>(a, w.nh, w.split, row, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
 }
 
 // Merge of a sequence's records for one query head: eight groups of threads take the splits in turn, four dims a thread (64 splits
@@ -608,13 +481,21 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
   __shared__ float total[8];
   const uint32_t head = blockIdx.x, seq = blockIdx.y;
   const int tid = threadIdx.x, grp = tid / LANES, lane = tid % LANES;
-  const Reach r = reach(a, seq);
-  const uint32_t used = r.hi == r.lo ? 1u : (r.hi - r.lo + a.plan.chunk - 1) / a.plan.chunk;
-  const size_t rec0 = ((size_t)seq * a.a.n_q_heads + head) * a.plan.splits;
-  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.t.n_seqs * a.a.n_q_heads * a.plan.splits * D) + rec0;
+  const Reach r = reach(a, seq, head / a.by_heads.d);
+  // records: of the prefix (first ones, and as many as `gap` before the others), then of the sequence's own positions
+  uint32_t used, first = 0xffffffffu, gap = 0;
+  if (a.slot) {
+    first = ((a.s.prefix ? r.lo : r.hi) + a.s.chunk - 1) / a.s.chunk;
+    gap = a.slot - first;
+    used = first + (a.s.prefix ? (r.hi - r.lo + a.plan.chunk - 1) / a.plan.chunk : 0u);
+  } else {
+    used = r.hi == r.lo ? 1u : (r.hi - r.lo + a.plan.chunk - 1) / a.plan.chunk;
+  }
+  const size_t rec0 = ((size_t)seq * a.a.n_q_heads + head) * a.slots;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)a.s.n_rows * a.a.n_q_heads * a.slots * D) + rec0;
   const float4* acc = reinterpret_cast<const float4*>(a.part + rec0 * D) + lane;
   float m = -INFINITY;
-  for (uint32_t i = tid; i < used; i += NT) m = fmaxf(m, ml[i].x);
+  for (uint32_t i = tid; i < used; i += NT) m = fmaxf(m, ml[i < first ? i : i + gap].x);
   m = wave_max(m);
   if ((tid & 63) == 0) top[tid >> 6] = m;
   __syncthreads();
@@ -626,8 +507,9 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (uint32_t i = grp; i < used; i += 8) {
-    const float2 v = ml[i];
-    const float4 x = acc[(size_t)i * LANES];
+    const uint32_t j = i < first ? i : i + gap;
+    const float2 v = ml[j];
+    const float4 x = acc[(size_t)j * LANES];
     const float f = __builtin_amdgcn_exp2f(v.x - Ms);
     L += v.y == v.y ? v.y * f : v.y;
     o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
@@ -636,7 +518,7 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
   if (lane == 0) total[grp] = L;
   __syncthreads();
   if (tid >= D) return;
-  L = 0.f;
+  L = r.bad ? NAN : 0.f;
   float v = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -674,19 +556,17 @@ PageAttnPlan plan_page_attention(const PagePool& p, uint32_t n_seqs, const PageA
   return pl;
 }
 
-hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTable& t, const PageAttn& a, const PageAttnPlan& plan,
-                                 float* workspace) {
-  if (t.n_seqs == 0) return hipSuccess;
-  if (t.n_seqs > 65535 || a.n_q_heads > 65535 || (p.head_dim != 64 && p.head_dim != 128) || (plan.splits > 1 && !workspace)) return hipErrorInvalidValue;
-  const int64_t per16 = a.q_dtype == DT_F32 ? 4 : 8;
-  const AttnArgs g{p, t, a, plan, workspace, reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_row % per16 == 0 && a.q_head % per16 == 0};
+hipError_t launch_page_walk(hipStream_t s, const AttnArgs& g, uint32_t n_seqs) {
+  const PagePool& p = g.p;
+  const PageAttn& a = g.a;
+  if (n_seqs > 65535 || a.n_q_heads > 65535 || (p.head_dim != 64 && p.head_dim != 128)) return hipErrorInvalidValue;
   // queries that enter the product as they are (with a binary16 output, whose rounding hides two-piece weights)
   const bool lite = !a.packed && a.q_dtype != DT_F32 && a.q_dtype == (p.store == PS_F16 ? DT_F16 : DT_BF16);
   const int ht = (a.n_q_heads / (int)p.n_kv_heads + 15) / 16;
   // Heads, sequences, splits, so that the workgroups of one split go to all XCDs in turn (with the splits innermost, four of them and
   // eight heads, a split stays on two of the eight XCDs, and where most sequences have no fourth one those two idle: 48 sequences
   // of 1 .. 6000 positions as 2 splits 81 -> 68 us), and the splits that few sequences reach come last.
-  const dim3 mc(p.n_kv_heads * ht, t.n_seqs, plan.splits);
+  const dim3 mc(p.n_kv_heads * ht, n_seqs, g.plan.splits);
 #define NNC_ATTN_CASE(ST)                                                                  \
   case ST:                                                                                 \
     if (p.head_dim == 128) {                                                               \
@@ -708,12 +588,25 @@ hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTab
     NNC_ATTN_CASE(PS_E4M3);
     default: return hipErrorInvalidValue;
   }
-  if (plan.splits > 1) {
-    const dim3 jg(a.n_q_heads, t.n_seqs);
-    if (p.head_dim == 128) k_page_attn_join<128><<<jg, 256, 0, s>>>(g);
-    else k_page_attn_join<64><<<jg, 128, 0, s>>>(g);
-  }
   return hipGetLastError();
+}
+
+hipError_t launch_page_join(hipStream_t s, const AttnArgs& g, uint32_t n_rows) {
+  const dim3 jg(g.a.n_q_heads, n_rows);
+  if (g.p.head_dim == 128) k_page_attn_join<128><<<jg, 256, 0, s>>>(g);
+  else k_page_attn_join<64><<<jg, 128, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTable& t, const PageAttn& a, const PageAttnPlan& plan,
+                                 float* workspace) {
+  const uint32_t n_seqs = a.per_head ? t.n_seqs / p.n_kv_heads : t.n_seqs;
+  if (n_seqs == 0) return hipSuccess;
+  if (plan.splits > 1 && !workspace) return hipErrorInvalidValue;
+  AttnArgs g{p, t, a, plan, workspace, query_wide(a), plan.splits, 0, PageShare{}, fast_div(1), fast_div(a.n_q_heads / p.n_kv_heads)};
+  g.s.n_rows = n_seqs;
+  if (hipError_t e = launch_page_walk(s, g, n_seqs)) return e;
+  return plan.splits > 1 ? launch_page_join(s, g, n_seqs) : hipSuccess;
 }
 
 }  // namespace nnc

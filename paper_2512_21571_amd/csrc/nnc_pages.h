@@ -261,6 +261,7 @@ struct PageAttn {
   // instead of `out`: the operand of the output projection in the decode GEMMs' layout, element type pk_dt, nsplit pieces
   void* packed = nullptr;
   int pk_dt = 0, NC = 0, nsplit = 1;
+  bool per_head = false;  // every kv head of a sequence has its own row of the table and its own length: [seq][kv head]
 };
 struct PageAttnPlan {
   uint32_t splits, chunk;  // workgroups along a sequence, positions of each
@@ -269,6 +270,67 @@ struct PageAttnPlan {
 PageAttnPlan plan_page_attention(const PagePool& p, uint32_t n_seqs, const PageAttn& a, uint32_t max_splits = 0xffffffffu);
 hipError_t launch_page_attention(hipStream_t s, const PagePool& p, const PageTable& t, const PageAttn& a, const PageAttnPlan& plan,
                                  float* workspace);
+
+// Rows of a group that share the first positions of their contexts (see nnc_page_attention_shared): row g * width + w of group g.
+struct PageShare {
+  uint32_t width = 1, n_rows = 0;
+  bool per_group = false;           // one row of the table for each group; else one for each row
+  const int32_t* prefix = nullptr;  // [groups] shared positions; NULL: all are
+  uint32_t max_own = 0;             // no row has more behind them
+  uint32_t chunk = 0;               // positions of a workgroup along the prefix (of the plan)
+};
+struct PageSharePlan {
+  uint32_t splits, chunk, tiles;  // workgroups along a prefix, positions of each, tiles of sixteen rows of each
+  PageAttnPlan own;               // of the positions behind it; splits 0: there are none
+  size_t floats;
+};
+PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageShare& s, uint32_t max_slots = 0xffffffffu);
+hipError_t launch_page_share(hipStream_t st, const PagePool& p, const PageTable& t, const PageAttn& a, const PageShare& s,
+                             const PageSharePlan& plan, float* workspace);
+
+// Bounds of the keys of pages (see nnc_page_bound).
+struct PageBound {
+  PagePool p;
+  PageTable t;
+  void *lo, *hi;  // of the layer: [page][kv head][head_dim]
+  const int32_t *lens, *since;  // since NULL: since0
+  int32_t since0;
+  uint32_t slots;  // pages of a sequence that are looked at
+  FastDiv by_head;
+};
+hipError_t launch_page_bound(hipStream_t s, const PageBound& b);
+
+// The pages that a query picks by their bounds (see nnc_page_pick).
+struct PagePick {
+  PagePool p;
+  PageTable t;
+  const void *lo, *hi;  // of the layer
+  const void* q;
+  int q_dtype;
+  int64_t q_row, q_head;
+  bool q_wide;
+  uint32_t n_q_heads;
+  const int32_t* lens;
+  uint32_t max_len, blocks;  // blocks: pages of max_len positions
+  uint32_t keep, first, last;
+  int32_t *tables_out, *lens_out;
+};
+size_t page_pick_bytes(const PagePool& p, uint32_t n_seqs, uint32_t blocks);
+hipError_t launch_page_pick(hipStream_t s, const PagePick& a, void* workspace);
+
+// Verification of drafted tokens (see nnc_draft_verify).
+struct DraftVerify {
+  const void *logits, *draft_logits;
+  int dtype;
+  int64_t row, draft_row;  // elements between rows; sequence i has rows (k + 1) i .. and k i ..
+  uint32_t n, k, vocab;
+  const int32_t *drafts, *counts;
+  const float *uniforms, *temperatures;
+  float temperature;
+  int32_t *tokens, *accepted;
+};
+size_t draft_verify_bytes(uint32_t n, uint32_t k, uint32_t vocab, bool drafter);
+hipError_t launch_draft_verify(hipStream_t s, const DraftVerify& v, void* workspace);
 
 // Beam selection (see nnc_beam_select).
 struct BeamSelect {
@@ -292,6 +354,9 @@ struct ColState;
 // Columns' tokens, positions and table rows from device memory; lens advance.  A column whose token is no token of the
 // vocabulary or whose position is outside 0 .. max_pos gets position -2: it is not cached, and its outputs become NaN.
 hipError_t launch_paged_state(hipStream_t s, ColState* st, int ncols, const int32_t* tok, int32_t* lens, uint32_t vocab, uint32_t max_pos);
+// The same for `width` tokens of each sequence, one behind another (counts: those behind the first, or NULL: all); lens stay.
+hipError_t launch_paged_state_drafts(hipStream_t s, ColState* st, int ncols, int width, const int32_t* tok, const int32_t* counts,
+                                     const int32_t* lens, uint32_t vocab, uint32_t max_len);
 // k_qknorm_rope_append with the K and V rows going into pages
 hipError_t launch_qknorm_rope_page(hipStream_t s, float* qkv, int nq, int nkv, const float* gq, const float* gk, float eps,
                                    const float2* rope, const ColState* st, int ncols, const PagePool& p, const PageTable& t);
