@@ -8,11 +8,11 @@ namespace nnc {
 
 namespace {
 
-// Rows of a group that a workgroup takes for one kv head: row0 .. + n - 1 of its width x heads, RT tiles of sixteen.  Lane c of
-// tile t has one row: its sequence, its query head and its limit, the positions that it sees.
+// Rows of a group that a workgroup takes for one kv head: row0 .. + n - 1 of its width x heads.  A wave has RT tiles of sixteen of
+// them, and lane c of tile t one row: its sequence, its query head and its limit, the positions that it sees.
 template <int RT>
 struct Block {
-  uint32_t kvh, group, row0, n, split, begin, end, least;  // least: the smallest limit (up to there no score is masked)
+  uint32_t kvh, group, row0, n, split, begin, end, least, most;  // least, most: of the limits (up to the least no score is masked)
   uint32_t seq[RT], head[RT], limit[RT];
   bool bad[RT], idle;
 };
@@ -21,17 +21,17 @@ __device__ __forceinline__ void row_at(const AttnArgs& a, uint32_t group, uint32
   seq = group * a.s.width + s;
   head = kvh * a.by_heads.d + (r - s * a.by_heads.d);
 }
-template <int RT>
-__device__ __forceinline__ void rows_of(const AttnArgs& a, int c, Block<RT>& w) {
+template <int RT, int WR = 1>
+__device__ __forceinline__ void rows_of(const AttnArgs& a, int c, Block<RT>& w, int wr = 0) {
   // (blocks of one kv head lie a multiple of the kv heads apart: on one XCD where those are eight)
   const uint32_t block = blockIdx.x / a.p.n_kv_heads;
   w.kvh = blockIdx.x - block * a.p.n_kv_heads;
   w.group = blockIdx.y;
   w.split = blockIdx.z;
-  w.row0 = block * 16 * RT;
-  w.n = min(16u * RT, a.s.width * a.by_heads.d - w.row0);
+  w.row0 = block * 16 * RT * WR;
+  w.n = min(16u * RT * WR, a.s.width * a.by_heads.d - w.row0);
 #pragma unroll
-  for (int t = 0; t < RT; ++t) row_at(a, w.group, w.kvh, w.row0 + min(t * 16u + c, w.n - 1), w.seq[t], w.head[t]);
+  for (int t = 0; t < RT; ++t) row_at(a, w.group, w.kvh, w.row0 + min((wr * RT + t) * 16u + c, w.n - 1), w.seq[t], w.head[t]);
 }
 // Largest of a number in every lane.
 __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
@@ -53,8 +53,9 @@ __device__ __forceinline__ void limits_of(const AttnArgs& a, Block<RT>& w) {
     least = min(least, w.limit[t]);
   }
   w.least = ~wave_most(~least);
+  w.most = wave_most(most);
   w.begin = w.split * a.s.chunk;
-  w.end = min(wave_most(most), w.begin + a.s.chunk);
+  w.end = min(w.most, w.begin + a.s.chunk);
   w.idle = w.split && w.begin >= w.end;  // (the first workgroup answers for empty rows)
 }
 
@@ -70,54 +71,37 @@ __device__ __forceinline__ uint32_t rows_flagged(bool x) {
   return (uint32_t)(b | (b >> 16) | (b >> 32) | (b >> 48)) & 0xffffu;
 }
 
-// Up to 16 RT rows per workgroup, a wave walking tiles of 32 positions as in k_page_attn_mc, whose products, pieces and layouts these
-// are: S^T = K Q^T for RT tiles of queries against one fragment of K, O^T = V^T P^T for RT tiles of weights against one of V.
-// Rows end at different positions: in tiles behind the smallest limit, scores behind a row's own are -infinity.  Weight zero does not
-// hide an infinity or a NaN in V, so that values there that are not finite are taken as zeros, and rows that do see them
-// become NaN; the same for pages that do not exist.
-template <int STORE, int D, bool FULL, int RT>
-__global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs a) {
-  using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
-  constexpr bool B8 = page_scaled(STORE);
-  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16;
-  constexpr int LD = B8 ? D / 64 : D / 32;   // 16-byte loads of a lane per row: bytes i * 64 + g * 16
-  constexpr int PITCH = D * 2 + 32, OPITCH = D + 4;
-  __shared__ __attribute__((aligned(16))) char vbuf[4][32 * PITCH];
-  __shared__ __attribute__((aligned(16))) float sc[4][64];
-  __shared__ float smax[4][16], ssum[4][16];
-  static_assert(16 * OPITCH * 4 <= 32 * PITCH, "the waves' results fit where V was");
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
-  char* vb = vbuf[wave];
-
-  struct Tile {
-    u32x4_v k[2][LD], v[2][LD];
-    float scale;
-  };
-  struct Where {
-    int32_t page[2];
-    uint32_t row[2];
-  };
-  Block<RT> w;
-  rows_of<RT>(a, c, w);
-  const Finder find(a, a.s.per_group ? w.group : w.group * a.s.width, w.kvh);
-  auto look = [&](Where& p, uint32_t p0) __attribute__((always_inline)) {
+// split_pair3 of weights.  The remainder behind a bf16 value is one product of pairs, v - (0 a + 1 b), exact like the subtraction
+// (a weight that is no number spoils its neighbour, which is of the same row).  The pairs (-1, 0) and (0, -1) are kept from the
+// compiler, which takes the first for the inline constant -1, to the instruction a pair (0, -1).
+template <class HF>
+__device__ __forceinline__ void split_weights3(float u, float v, uint32_t (&piece)[3]) {
+  if constexpr (HF::kNarrowRange) {
+    split_pair3<HF>(u, v, piece);
+  } else {
+    typedef typename HF::vec2 pair_t;
+    uint32_t low = 0x0000bf80u, high = 0xbf800000u;
+    asm("" : "+s"(low), "+s"(high));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) find.look(p0 + h * 16 + c, p.page[h], p.row[h]);
-  };
-  auto dim_of = [&](int kt) { return B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8; };
-  Where here, next;
-  uint32_t p0 = w.split * a.s.chunk + wave * 32;
-  look(here, p0);
-  look(next, p0 + 128);
-  limits_of<RT>(a, w);
-  if (w.idle) return;
-  const uint32_t end = w.end;
+    for (int s = 0; s < 3; ++s) {
+      piece[s] = HF::pack2(u, v);
+      if (s < 2) {
+        u = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, piece[s]), __builtin_bit_cast(pair_t, low), u, false);
+        v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, piece[s]), __builtin_bit_cast(pair_t, high), v, false);
+      }
+    }
+  }
+}
 
-  // Queries: of the product's own type as they are, others in three pieces.  A negative scale's sign goes into the query, so that the
-  // largest product is the largest score, and so does a scale of zero, which would make a masked score, -infinity, a NaN.
+// Queries of a wave's rows as operands of the product: of its own type as they are, others in three pieces.  A negative scale's sign
+// goes into the query, so that the largest product is the largest score, and so does a scale of zero, which would make a
+// masked score, -infinity, a NaN.  fac: what a product is multiplied by for an exponent of 2.
+template <int STORE, int D, bool FULL, int RT, class Dim>
+__device__ __forceinline__ void load_queries(const AttnArgs& a, const Block<RT>& w, const Dim& dim_of, u32x4_v (&qf)[RT][D / 32][FULL ? 3 : 1],
+                                             float (&fac)[RT]) {
+  using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
+  constexpr int KT = D / 32;
   const bool none = a.a.scale == 0.f;
-  float fac[RT];
-  u32x4_v qf[RT][KT][NQ];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     fac[t] = none ? 1.f : fabsf(a.a.scale) * 1.44269504088896341f;
@@ -167,6 +151,54 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
       }
     }
   }
+}
+
+// Up to 16 RT rows per workgroup, a wave walking tiles of 32 positions as in k_page_attn_mc, whose products, pieces and layouts these
+// are: S^T = K Q^T for RT tiles of queries against one fragment of K, O^T = V^T P^T for RT tiles of weights against one of V.
+// Rows end at different positions: in tiles behind the smallest limit, scores behind a row's own are -infinity.  Weight zero does not
+// hide an infinity or a NaN in V, so that values there that are not finite are taken as zeros, and rows that do see them
+// become NaN; the same for pages that do not exist.
+template <int STORE, int D, bool FULL, int RT>
+__global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs a) {
+  using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
+  constexpr bool B8 = page_scaled(STORE);
+  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16;
+  constexpr int LD = B8 ? D / 64 : D / 32;   // 16-byte loads of a lane per row: bytes i * 64 + g * 16
+  constexpr int PITCH = D * 2 + 32, OPITCH = D + 4;
+  __shared__ __attribute__((aligned(16))) char vbuf[4][32 * PITCH];
+  __shared__ __attribute__((aligned(16))) float sc[4][64];
+  __shared__ float smax[4][16], ssum[4][16];
+  static_assert(16 * OPITCH * 4 <= 32 * PITCH, "the waves' results fit where V was");
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  char* vb = vbuf[wave];
+
+  struct Tile {
+    u32x4_v k[2][LD], v[2][LD];
+    float scale;
+  };
+  struct Where {
+    int32_t page[2];
+    uint32_t row[2];
+  };
+  Block<RT> w;
+  rows_of<RT>(a, c, w);
+  const Finder find(a, a.s.per_group ? w.group : w.group * a.s.width, w.kvh);
+  auto look = [&](Where& p, uint32_t p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) find.look(p0 + h * 16 + c, p.page[h], p.row[h]);
+  };
+  auto dim_of = [&](int kt) { return B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8; };
+  Where here, next;
+  uint32_t p0 = w.split * a.s.chunk + wave * 32;
+  look(here, p0);
+  look(next, p0 + 128);
+  limits_of<RT>(a, w);
+  if (w.idle) return;
+  const uint32_t end = w.end;
+
+  float fac[RT];
+  u32x4_v qf[RT][KT][NQ];
+  load_queries<STORE, D, FULL, RT>(a, w, dim_of, qf, fac);
 
   uint32_t gone = 0xffffffffu;  // first position without a page
   auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
@@ -388,6 +420,297 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
   }
 }
 
+// More rows: the NW waves of a workgroup share tiles of 64 positions in LDS, WR of them with sixteen rows of their own,
+// NW / WR with positions of their own.  The next tile is on its way to registers during the work on this one and is laid
+// down, widened, in a second buffer.  Products, pieces, layouts and masks as above; what a position spoils (`spoilt`: the first one
+// without a page, or with a value in V that is no number and has been taken out) is looked at in the end.
+template <int STORE, int D, bool FULL, int NW, int WR>
+__global__ __launch_bounds__(64 * NW, NW / 2) void k_page_attn_block(AttnArgs a) {
+  using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
+  constexpr bool B8 = page_scaled(STORE);
+  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16, WP = NW / WR, TILE = 64;
+  constexpr int CHUNKS = D * (B8 ? 1 : 2) / 16, ROWS = 64 * NW / CHUNKS, LD = TILE / ROWS;  // sixteen bytes of a row; rows of a load; loads
+  constexpr int KP = D * 2 + 16, VP = D * 2 + 32, OPITCH = D + 4;                       // bytes from row to row, without bank conflicts
+  constexpr int BUFFER = TILE * (KP + VP);
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
+  __shared__ __attribute__((aligned(16))) float sc[2][B8 ? 2 * TILE : 4];
+  __shared__ float smax[NW][16], ssum[NW][16];
+  __shared__ uint32_t spoilt;
+  static_assert(NW * 16 * OPITCH * 4 <= 2 * BUFFER, "the waves' results fit where the tiles were");
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4, wr = wave % WR, wp = wave / WR;
+  const int row_l = tid / CHUNKS, chunk_l = tid % CHUNKS;
+
+  Block<1> w;
+  rows_of<1, WR>(a, c, w, wr);
+  const Finder find(a, a.s.per_group ? w.group : w.group * a.s.width, w.kvh);
+  int32_t page[LD + 1];
+  uint32_t row[LD + 1];
+  auto look = [&](uint32_t p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i) find.look(p0 + i * ROWS + row_l, page[i], row[i]);
+    if constexpr (B8) find.look(p0 + lane, page[LD], row[LD]);
+  };
+  const uint32_t first = w.split * a.s.chunk;
+  look(first);
+  if (tid == 0) spoilt = 0xffffffffu;
+  limits_of<1>(a, w);
+  // (limits and ends are those of all waves' rows)
+  if constexpr (WR > 1) {
+    uint32_t* share = reinterpret_cast<uint32_t*>(smax);
+    if (lane == 0) {
+      share[wave] = w.least;
+      share[NW + wave] = w.most;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      w.least = min(w.least, share[i]);
+      w.most = max(w.most, share[NW + i]);
+    }
+    w.end = min(w.most, w.begin + a.s.chunk);
+    w.idle = w.split && w.begin >= w.end;
+  }
+  if (w.idle) return;
+  const uint32_t end = w.end;
+  const uint32_t limit = min(w.limit[0], end);
+  float facs[1];
+  u32x4_v qs[1][KT][NQ];
+  load_queries<STORE, D, FULL, 1>(a, w, [&](int kt) { return kt * 32 + g * 8; }, qs, facs);
+  const float fac = facs[0];
+
+  u32x4_v tk[LD], tv[LD];
+  float ts = 0.f;
+  auto load = [&](uint32_t p0) __attribute__((always_inline)) {
+    uint32_t gone = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const uint32_t pos = p0 + i * ROWS + row_l;
+      bool missing = false;
+      // (behind the end: whatever row is there to be read)
+      const uint64_t at = find.at(pos < end ? page[i] : -1, pos < end ? row[i] : find.first_row, pos < end, missing);
+      if (missing) gone = min(gone, pos);
+      const uint64_t o = at * (D * (B8 ? 1 : 2)) + chunk_l * 16;
+      tk[i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.k) + o);
+      tv[i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.v) + o);
+    }
+    if constexpr (B8) {
+      const uint32_t pos = p0 + lane;
+      bool missing = false;
+      const uint64_t at = find.at(pos < end ? page[LD] : -1, pos < end ? row[LD] : find.first_row, pos < end, missing);
+      if (wave < 2) ts = (wave == 0 ? a.p.k_scale : a.p.v_scale)[at];
+    }
+    if (gone != 0xffffffffu) atomicMin(&spoilt, gone);
+  };
+  auto store = [&](uint32_t p0, int buf) __attribute__((always_inline)) {
+    char *kb = lds + buf * BUFFER, *vb = kb + TILE * KP;
+    const bool ragged = p0 + TILE > w.least;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int r = i * ROWS + row_l;
+      constexpr int W = B8 ? 2 : 1;
+      u32x4_v k[W], v[W];
+      if constexpr (B8) {
+        k[0] = widen8_bf16<STORE>(tk[i][0], tk[i][1]);
+        k[1] = widen8_bf16<STORE>(tk[i][2], tk[i][3]);
+        v[0] = widen8_bf16<STORE>(tv[i][0], tv[i][1]);
+        v[1] = widen8_bf16<STORE>(tv[i][2], tv[i][3]);
+      } else {
+        k[0] = tk[i];
+        v[0] = tv[i];
+      }
+      if (ragged) {
+        const uint32_t pos = p0 + r;
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (pos >= end) v[j][e] = 0;
+            if (pos >= w.least && not_finite2<HF>(v[j][e])) {
+              bad = true;
+              v[j][e] = 0;
+            }
+          }
+        if (bad) atomicMin(&spoilt, pos);
+      }
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        *reinterpret_cast<u32x4_v*>(kb + r * KP + (chunk_l * W + j) * 16) = k[j];
+        *reinterpret_cast<u32x4_v*>(vb + r * VP + (chunk_l * W + j) * 16) = v[j];
+      }
+    }
+    if constexpr (B8) {
+      if (wave < 2) {
+        const uint32_t pos = p0 + lane;
+        if (pos >= end) ts = 0.f;
+        if (wave == 1 && pos >= w.least && !(fabsf(ts) < INFINITY)) {  // (a scale that is no number belongs to a row of no numbers)
+          ts = 0.f;
+          atomicMin(&spoilt, pos);
+        }
+        sc[buf][wave * TILE + lane] = ts;
+      }
+    }
+  };
+
+  // A weight is 2^(score - m + LIFT); m follows the largest score only where that is 2^SLACK beyond it, so that sums are seldom
+  // brought to another m.  (Binary16 weights end at 2^16; their second piece is a normal number down to 2^-3.)
+  constexpr float LIFT = HF::kNarrowRange ? 10.f : 0.f, SLACK = HF::kNarrowRange ? 5.f : 20.f;
+  float m = -INFINITY, bar = -INFINITY, base = 0.f, l = 0.f;
+  f32x4_t acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  auto step = [&](uint32_t p0, int buf, int sub) __attribute__((always_inline)) {
+    const char *kb = lds + buf * BUFFER + sub * 32 * KP, *vb = lds + buf * BUFFER + TILE * KP + sub * 32 * VP;
+    float x[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const u32x4_v kf = *reinterpret_cast<const u32x4_v*>(kb + (h * 16 + c) * KP + kt * 64 + g * 16);
+#pragma unroll
+        for (int pc = 0; pc < NQ; ++pc) s = HF::mfma(kf, qs[0][kt][pc], s);
+      }
+      if constexpr (B8) s *= *reinterpret_cast<const f32x4_t*>(&sc[buf][sub * 32 + h * 16 + g * 4]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[h * 4 + i] = s[i];
+    }
+    if (p0 + 32 > w.least) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (p0 + (e >> 2) * 16 + g * 4 + (e & 3) >= limit) x[e] = -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+    top *= fac;
+    if (__any(top > bar)) {
+      const float mn = fmaxf(m, col4_max(top)), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      bar = mn + SLACK;
+      base = mn == -INFINITY ? 0.f : mn - LIFT;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[i] *= f;
+    }
+    uint32_t pw[NP][4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], fac, -base)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e + 1], fac, -base));
+      l += u + v;
+      if constexpr (B8) {
+        const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&sc[buf][TILE + sub * 32 + (e >> 2) * 16 + g * 4]);
+        u *= vs[e & 3];
+        v *= vs[(e & 3) + 1];
+      }
+      if constexpr (NP == 3) {
+        uint32_t pc[3];
+        split_weights3<HF>(u, v, pc);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) pw[k][e >> 1] = pc[k];
+      } else {
+#pragma clang fp contract(off)
+        pw[0][e >> 1] = HF::pack2(u, v);
+        u -= HF::lo(pw[0][e >> 1]);
+        v -= HF::hi(pw[0][e >> 1]);
+        pw[1][e >> 1] = HF::pack2(u, v);
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; dt += 2) {
+      u32x4_v vf[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const char* p = vb + (g * 4 + (c >> 2)) * VP + (dt + j) * 32 + (c & 3) * 8;
+        const u32x2_v lo = lds_column4(p), hi = lds_column4(p + 16 * VP);
+        vf[j] = u32x4_v{lo[0], lo[1], hi[0], hi[1]};
+      }
+#pragma unroll
+      for (int k = 0; k < NP; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[dt + j] = HF::mfma(vf[j], u32x4_v{pw[k][0], pw[k][1], pw[k][2], pw[k][3]}, acc[dt + j]);
+    }
+  };
+
+  // (one copy of each part of the loop: a kernel's code is fetched once, and that takes a while)
+  int buf = 0;
+  bool work = false;
+#pragma unroll 1
+  for (uint32_t p0 = w.begin;; p0 += TILE) {
+    const bool more = p0 < end;
+    if (more) {
+      load(p0);
+      look(p0 + TILE);
+    }
+    if (work) {
+#pragma unroll 1
+      for (int i = 0; i < (WP == 1 ? 2 : 1); ++i) {
+        const int sub = WP == 1 ? i : wp;
+        if (p0 - TILE + sub * 32 < end) step(p0 - TILE + sub * 32, buf, sub);
+      }
+    }
+    if (!more) break;
+    buf ^= 1;
+    store(p0, buf);
+    __syncthreads();
+    work = true;
+  }
+
+  // Results.  Waves with rows of their own (WP 1) put them where they belong, the others merge them first.
+  float* ml = a.part + (size_t)a.s.n_rows * a.a.n_q_heads * a.slots * D;
+  auto put = [&](uint32_t seq, uint32_t head, uint32_t dim, f32x4_t v, float top, float L) __attribute__((always_inline)) {
+    if (a.slots == 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) store_out(a, seq, head, (int)dim + e, L == 0.f ? 0.f : v[e] / L);
+    } else {
+      const size_t rec = ((size_t)seq * a.a.n_q_heads + head) * a.slots + a.slot + w.split;
+      *reinterpret_cast<f32x4_t*>(a.part + rec * D + dim) = v;
+      if (dim == 0) *reinterpret_cast<float2*>(ml + rec * 2) = make_float2(top, L);
+    }
+  };
+  __syncthreads();
+  l = col4_sum(l);
+  if (w.limit[0] > spoilt || w.bad[0]) l = NAN;
+  if constexpr (WP == 1) {
+    if (wr * 16u + c < w.n) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) put(w.seq[0], w.head[0], dt * 16 + g * 4, acc[dt], m, l);
+    }
+  } else {
+    float* out = reinterpret_cast<float*>(lds);
+    if (g == 0) {
+      smax[wave][c] = m;
+      ssum[wave][c] = l;
+    }
+    __syncthreads();
+    float M = m;
+#pragma unroll
+    for (int i = 0; i < WP; ++i) M = fmaxf(M, smax[i * WR + wr][c]);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+    float* o = out + wave * 16 * OPITCH;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o + c * OPITCH + dt * 16 + g * 4) = acc[dt] * f;
+    __syncthreads();
+    for (uint32_t e = tid; e < WR * 16 * (D / 4); e += 64 * NW) {
+      const uint32_t h = e / (D / 4), d = e % (D / 4) * 4, j = h / 16;
+      if (h >= w.n) continue;
+      float L = 0.f, top = -INFINITY;
+      f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < WP; ++i) top = fmaxf(top, smax[i * WR + j][h % 16]);
+#pragma unroll
+      for (int i = 0; i < WP; ++i) {
+        const float x = ssum[i * WR + j][h % 16], mx = smax[i * WR + j][h % 16];
+        L += x != x ? x : mx == -INFINITY ? 0.f : x * __builtin_amdgcn_exp2f(mx - top);
+        v += *reinterpret_cast<const f32x4_t*>(out + ((i * WR + j) * 16 + h % 16) * OPITCH + d);
+      }
+      uint32_t seq, head;
+      row_at(a, w.group, w.kvh, w.row0 + h, seq, head);
+      put(seq, head, d, v, top, L);
+    }
+  }
+}
+
 // fp32 pages, as k_page_attn_f32: sixteen rows per workgroup, on the fp32 matrix instruction, tiles of 16 positions.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
@@ -549,10 +872,14 @@ static bool own_type(const PagePool& p, const PageAttn& a) {
   return !a.packed && a.q_dtype != DT_F32 && a.q_dtype == (p.store == PS_F16 ? DT_F16 : DT_BF16);
 }
 
+// Tiles of sixteen rows of the largest workgroup.  (Queries in three pieces take the registers of eight waves; 8-bit rows of
+// 64 values fill a tile of 64 positions with the loads of four.)
+static constexpr int most_tiles(int store, int dim, bool full) { return full || (page_scaled(store) && dim == 64) ? 4 : 8; }
+
 PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageShare& s, uint32_t max_slots) {
   const uint32_t G = a.n_q_heads / p.n_kv_heads, groups = s.width ? s.n_rows / s.width : 0, rows = s.width * G;
   PageSharePlan pl{};
-  pl.tiles = p.store == PS_F32 || rows <= 16 ? 1 : 2;
+  pl.tiles = p.store == PS_F32 || rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : most_tiles(p.store, p.head_dim, !own_type(p, a));
   const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)groups * p.n_kv_heads * ((rows + 16 * pl.tiles - 1) / (16 * pl.tiles)));
   const uint32_t span = a.max_len;
   uint64_t splits = (512 + wgs - 1) / wgs;
@@ -584,10 +911,13 @@ hipError_t launch_page_share(hipStream_t st, const PagePool& p, const PageTable&
   AttnArgs g{p, t, a, plan.own, workspace, query_wide(a), slots, 0, s, fast_div(s.width), fast_div(G)};
   g.s.chunk = plan.chunk;
   const dim3 grid((uint32_t)blocks, groups, plan.splits);
-#define NNC_ROWS_TILES(ST, D, FULL)                                            \
-  do {                                                                         \
-    if (plan.tiles == 1) k_page_attn_rows<ST, D, FULL, 1><<<grid, 256, 0, st>>>(g); \
-    else k_page_attn_rows<ST, D, FULL, 2><<<grid, 256, 0, st>>>(g);            \
+#define NNC_ROWS_TILES(ST, D, FULL)                                                                                        \
+  do {                                                                                                                     \
+    constexpr int MOST = most_tiles(ST, D, FULL);                                                                          \
+    if (plan.tiles == 1) k_page_attn_rows<ST, D, FULL, 1><<<grid, 256, 0, st>>>(g);                                        \
+    else if (plan.tiles == 2) k_page_attn_block<ST, D, FULL, 4, 2><<<grid, 256, 0, st>>>(g);                               \
+    else if (plan.tiles == 4) k_page_attn_block<ST, D, FULL, 4, 4><<<grid, 256, 0, st>>>(g);                               \
+    else k_page_attn_block<ST, D, FULL, MOST, MOST><<<grid, 64 * MOST, 0, st>>>(g);                                        \
   } while (0)
 #define NNC_ROWS_CASE(ST)                                \
   case ST:                                               \
