@@ -35,12 +35,22 @@ __device__ __forceinline__ T lane_xor(T v, int mask) {
   return __shfl_xor(v, mask, 64);
 }
 
-// A wave per page and kv head: 64 / LPR rows at a time, a lane 16 bytes of one (EPL values).  A NaN shows in its column's bounds.
+// Pairs of sixteen-bit floats as integers that order like them (and back: the map is its own inverse), and their minima and maxima.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ i16x2 ordered(uint32_t w) {
+  const i16x2 v = __builtin_bit_cast(i16x2, w);
+  return v ^ ((v >> (short)15) & (short)0x7fff);
+}
+__device__ __forceinline__ uint32_t word_of(i16x2 v) { return __builtin_bit_cast(uint32_t, v ^ ((v >> (short)15) & (short)0x7fff)); }
+
+// A wave per page and kv head: 64 / LPR rows at a time, a lane 16 bytes of one (EPL values), four such loads on their way at once.
+// Sixteen-bit keys are compared as integers, two at a time.  A value of 8 bits times its scale is exact in 64 bits; rounding outwards
+// does not change an order, so lanes round their own before they compare.  A NaN shows in both bounds of its dimension.
+// Bound: the keys' bytes; a step's few pages: the loads that wait for each other (length -> table -> row).
 template <int STORE, int D>
 __global__ __launch_bounds__(256) void k_page_bound(PageBound b) {
   constexpr bool B8 = page_scaled(STORE);
-  constexpr int EPL = 16 / page_elem_bytes(STORE), LPR = D / EPL, ROWS = 64 / LPR;
-  using V = std::conditional_t<B8, double, float>;
+  constexpr int EPL = 16 / page_elem_bytes(STORE), LPR = D / EPL, ROWS = 64 / LPR, LOADS = 4, WORDS = B8 ? EPL / 2 : 4;
   const uint32_t seq = blockIdx.y, id = blockIdx.x * 4 + (threadIdx.x >> 6), slot = fdiv(id, b.by_head), head = id - slot * b.p.n_kv_heads;
   const int lane = threadIdx.x & 63, row0 = lane / LPR, at = lane % LPR * EPL;
   const int32_t len = b.lens[seq], since = b.since ? b.since[seq] : b.since0;
@@ -50,69 +60,141 @@ __global__ __launch_bounds__(256) void k_page_bound(PageBound b) {
   const int32_t page = b.t.entries[(size_t)seq * b.t.max_pages + block];
   if ((uint32_t)page >= b.p.n_pages) return;
   const uint32_t n = min(T, (uint32_t)len - block * T);
-  const uint64_t first = ((uint64_t)page * b.p.n_kv_heads + head) * T;
-  V lo[EPL], hi[EPL];
-  uint32_t nan = 0;
+  const uint64_t first = ((uint64_t)page * b.p.n_kv_heads + head) * T, to = ((uint64_t)page * b.p.n_kv_heads + head) * D + at;
+  const char* keys = static_cast<const char*>(b.p.k) + (first * D + at) * page_elem_bytes(STORE);
+  // (rows behind the last one: the last one again)
+  auto load = [&](uint32_t r0, u32x4_v (&w)[LOADS], float (&scale)[LOADS]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) {
-    lo[e] = INFINITY;
-    hi[e] = -INFINITY;
-  }
-  for (uint32_t r0 = 0; r0 < n; r0 += ROWS) {
-    const uint32_t r = r0 + row0;
-    if (r < n) {
-      const u32x4_v w = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(b.p.k) + ((first + r) * D + at) * page_elem_bytes(STORE));
-      V x[EPL];
-      if constexpr (B8) {
-        const double s = (double)b.p.k_scale[first + r];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float f[4];
-          page_widen4<STORE>(w[i], f);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[i * 4 + e] = (double)f[e] * s;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-          if constexpr (STORE == PS_F32) x[e] = __uint_as_float(w[e]);
-          else if constexpr (STORE == PS_BF16) x[e] = Bf16::widen((w[e / 2] >> (16 * (e & 1))) & 0xffffu);
-          else x[e] = Fp16::widen((w[e / 2] >> (16 * (e & 1))) & 0xffffu);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        nan |= x[e] != x[e] ? 1u << e : 0u;
-        lo[e] = x[e] < lo[e] ? x[e] : lo[e];
-        hi[e] = x[e] > hi[e] ? x[e] : hi[e];
-      }
+    for (int j = 0; j < LOADS; ++j) {
+      const uint32_t r = min(r0 + j * ROWS + row0, n - 1);
+      w[j] = *reinterpret_cast<const u32x4_v*>(keys + (uint64_t)r * (D * page_elem_bytes(STORE)));
+      if constexpr (B8) scale[j] = b.p.k_scale[first + r];
     }
-  }
-#pragma unroll
-  for (int o = LPR; o < 64; o <<= 1) {
-    nan |= lane_xor(nan, o);
+  };
+  u32x4_v w[LOADS];
+  float scale[LOADS];
+  if constexpr (STORE == PS_F32) {
+    float lo[EPL], hi[EPL];
+    uint32_t nan = 0;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) {
-      const V u = lane_xor(lo[e], o), v = lane_xor(hi[e], o);
-      lo[e] = u < lo[e] ? u : lo[e];
-      hi[e] = v > hi[e] ? v : hi[e];
+      lo[e] = INFINITY;
+      hi[e] = -INFINITY;
     }
-  }
-  if (row0) return;
-  const uint64_t to = ((uint64_t)page * b.p.n_kv_heads + head) * D + at;
+    for (uint32_t r0 = 0; r0 < n; r0 += LOADS * ROWS) {
+      load(r0, w, scale);
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) {
-    if ((nan >> e) & 1) lo[e] = hi[e] = NAN;
-    if constexpr (STORE == PS_F32) {
-      static_cast<float*>(b.lo)[to + e] = lo[e];
-      static_cast<float*>(b.hi)[to + e] = hi[e];
-    } else if constexpr (B8) {
-      static_cast<uint16_t*>(b.lo)[to + e] = (uint16_t)bf16_outwards(lo[e], false);
-      static_cast<uint16_t*>(b.hi)[to + e] = (uint16_t)bf16_outwards(hi[e], true);
+      for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) {
+          const float x = __uint_as_float(w[j][e]);
+          nan |= x != x ? 1u << e : 0u;
+          lo[e] = fminf(lo[e], x);
+          hi[e] = fmaxf(hi[e], x);
+        }
+    }
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+      nan |= lane_xor(nan, o);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) {
+        lo[e] = fminf(lo[e], lane_xor(lo[e], o));
+        hi[e] = fmaxf(hi[e], lane_xor(hi[e], o));
+      }
+    }
+    if (row0) return;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e)
+      if ((nan >> e) & 1) lo[e] = hi[e] = NAN;
+    *reinterpret_cast<float4*>(static_cast<float*>(b.lo) + to) = make_float4(lo[0], lo[1], lo[2], lo[3]);
+    *reinterpret_cast<float4*>(static_cast<float*>(b.hi) + to) = make_float4(hi[0], hi[1], hi[2], hi[3]);
+  } else {
+    i16x2 lo[WORDS], hi[WORDS];
+    constexpr uint32_t INF = STORE == PS_F16 ? 0x7c00u : 0x7f80u, QUIET = STORE == PS_F16 ? 0x7e00u : 0x7fc0u;
+    if constexpr (!B8) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        lo[i] = i16x2{0x7fff, 0x7fff};
+        hi[i] = i16x2{(short)0x8000, (short)0x8000};
+      }
+      for (uint32_t r0 = 0; r0 < n; r0 += LOADS * ROWS) {
+        load(r0, w, scale);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+          for (int i = 0; i < WORDS; ++i) {
+            const i16x2 k = ordered(w[j][i]);
+            lo[i] = __builtin_elementwise_min(lo[i], k);
+            hi[i] = __builtin_elementwise_max(hi[i], k);
+          }
+      }
     } else {
-      using HF = std::conditional_t<STORE == PS_BF16, Bf16, Fp16>;
-      static_cast<uint16_t*>(b.lo)[to + e] = (uint16_t)HF::bits(lo[e]);
-      static_cast<uint16_t*>(b.hi)[to + e] = (uint16_t)HF::bits(hi[e]);
+      double low[EPL], high[EPL];
+      uint32_t nan = 0;
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) {
+        low[e] = INFINITY;
+        high[e] = -INFINITY;
+      }
+      for (uint32_t r0 = 0; r0 < n; r0 += LOADS * ROWS) {
+        load(r0, w, scale);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const double s = (double)scale[j];
+          if (!(scale[j] == scale[j])) nan = 0xffffu;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[4];
+            page_widen4<STORE>(w[j][i], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const double x = (double)f[e] * s;
+              if constexpr (STORE == PS_E4M3) nan |= f[e] != f[e] ? 1u << (i * 4 + e) : 0u;
+              low[i * 4 + e] = fmin(low[i * 4 + e], x);
+              high[i * 4 + e] = fmax(high[i * 4 + e], x);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        uint32_t l[2], h[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bool bad = (nan >> (i * 2 + e)) & 1;
+          l[e] = bad ? QUIET | 0x8000u : bf16_outwards(low[i * 2 + e], false);  // (below every number)
+          h[e] = bad ? QUIET : bf16_outwards(high[i * 2 + e], true);
+        }
+        lo[i] = ordered(l[0] | (l[1] << 16));
+        hi[i] = ordered(h[0] | (h[1] << 16));
+      }
+    }
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        lo[i] = __builtin_elementwise_min(lo[i], __builtin_bit_cast(i16x2, lane_xor(__builtin_bit_cast(int, lo[i]), o)));
+        hi[i] = __builtin_elementwise_max(hi[i], __builtin_bit_cast(i16x2, lane_xor(__builtin_bit_cast(int, hi[i]), o)));
+      }
+    if (row0) return;
+    uint32_t ol[WORDS], oh[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      ol[i] = word_of(lo[i]);
+      oh[i] = word_of(hi[i]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {  // a NaN lies beyond the infinity of its sign, at one end or the other
+        const int sh = 16 * e;
+        if (((oh[i] >> sh) & 0x7fffu) > INF || ((ol[i] >> sh) & 0x7fffu) > INF) {
+          ol[i] = (ol[i] & ~(0xffffu << sh)) | (QUIET << sh);
+          oh[i] = (oh[i] & ~(0xffffu << sh)) | (QUIET << sh);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
+      *reinterpret_cast<u32x4_v*>(static_cast<uint16_t*>(b.lo) + to + i * 2) = u32x4_v{ol[i], ol[i + 1], ol[i + 2], ol[i + 3]};
+      *reinterpret_cast<u32x4_v*>(static_cast<uint16_t*>(b.hi) + to + i * 2) = u32x4_v{oh[i], oh[i + 1], oh[i + 2], oh[i + 3]};
     }
   }
 }
@@ -127,64 +209,120 @@ __device__ __forceinline__ uint64_t order_of(double x) {
   return (b >> 63) ? ~b : b | (1ull << 63);
 }
 
+// Sum over the LPR (8 or 16) neighbouring lanes of a page, in all of them: the same additions for every page.
+template <int LPR>
+__device__ __forceinline__ double lanes_sum(double v) {
+  auto get = [](double x, auto ctrl) __attribute__((always_inline)) {
+    const uint64_t b = (uint64_t)__double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, decltype(ctrl)::value, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), decltype(ctrl)::value, 0xf, 0xf, true);
+    return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+  };
+  v += get(v, std::integral_constant<int, DPP_QUAD_XOR1>{});
+  v += get(v, std::integral_constant<int, DPP_QUAD_XOR2>{});
+  v += get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{});
+  if constexpr (LPR == 16) v += get(v, std::integral_constant<int, DPP_ROW_MIRROR>{});
+  return v;
+}
+
 // Scores of the pages of a sequence for one kv head, in 64 bits: pages whose scores lie close are told apart as the definition does
 // (a sum of 128 products of fp32 is off by 2^-20 of its terms, and of 8192 pages several lie closer than that to the last one picked).
-// LPR lanes a page, eight dims each; a page's products are added in the same order wherever it lies, so equal pages tie.
-template <int DT, int D>
-__global__ __launch_bounds__(256) void k_page_score(PagePick a, uint64_t* keys) {
-  constexpr int LPR = D / 8, PER = 64 / LPR;
+// LPR lanes a page, eight dims each, LOADS pages of them on their way at once; max(q lo, q hi) is q hi for a positive and q lo for a
+// negative q, so that a product with both parts of q is all there is to do, HG query heads at a time.
+// Bound: the bounds' bytes, and nearly as long the 64-bit products.
+template <int DT, int D, int HG>
+__global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* keys) {
+  constexpr int LPR = D / 8, PER = 64 / LPR, LOADS = 4, WORDS = DT == DT_F32 ? 2 : 1;
   const uint32_t seq = blockIdx.y, kvh = blockIdx.z, G = a.n_q_heads / a.p.n_kv_heads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = lane % LPR * 8;
   const int32_t len = a.lens[seq];
   if (len <= 0 || (uint32_t)len > a.max_len) return;
-  const uint32_t blocks = fdiv((uint32_t)len - 1, a.p.by_page) + 1, block = (blockIdx.x * 4 + wave) * PER + lane / LPR;
-  if ((blockIdx.x * 4 + wave) * PER >= blocks) return;
-  double lo[8], hi[8];
-  bool there = false;
-  {
-    const int32_t page = block < blocks ? a.t.entries[(size_t)seq * a.t.max_pages + block] : -1;
-    there = (uint32_t)page < a.p.n_pages;
-    const uint64_t at = ((uint64_t)(there ? (uint32_t)page : 0u) * a.p.n_kv_heads + kvh) * D + dim;
-    float x[8];
-    load8<DT>(a.lo, (int64_t)at, true, x);
+  const uint32_t blocks = fdiv((uint32_t)len - 1, a.p.by_page) + 1, first = (blockIdx.x * 4 + wave) * PER * LOADS;
+  if (first >= blocks) return;
+  int32_t page[LOADS];
+  const int32_t* entries = a.t.entries + (size_t)seq * a.t.max_pages;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lo[i] = x[i];
-    load8<DT>(a.hi, (int64_t)at, true, x);
+  for (int j = 0; j < LOADS; ++j) page[j] = entries[min(first + j * PER + lane / LPR, blocks - 1)];
+  u32x4_v wl[LOADS][WORDS], wh[LOADS][WORDS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) hi[i] = x[i];
+  for (int j = 0; j < LOADS; ++j) {
+    const uint64_t at = (((uint64_t)((uint32_t)page[j] < a.p.n_pages ? page[j] : 0) * a.p.n_kv_heads + kvh) * D + dim) * (DT == DT_F32 ? 4 : 2);
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      wl[j][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.lo) + at + i * 16);
+      wh[j][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.hi) + at + i * 16);
+    }
   }
-  double best = -INFINITY;
-  bool nan = !there;
-  for (uint32_t h = 0; h < G; ++h) {
-    const int64_t o = (int64_t)seq * a.q_row + (int64_t)(kvh * G + h) * a.q_head + dim;
-    float q[8];
-    if (a.q_dtype == DT_F32) load8<DT_F32>(a.q, o, a.q_wide, q);
-    else if (a.q_dtype == DT_BF16) load8<DT_BF16>(a.q, o, a.q_wide, q);
-    else load8<DT_F16>(a.q, o, a.q_wide, q);
-    double s = 0.;
+  double best[LOADS];
+  bool nan[LOADS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s = __builtin_fma((double)fmaxf(q[i], 0.f), hi[i], s);
-      s = __builtin_fma((double)fminf(q[i], 0.f), lo[i], s);
-      nan |= q[i] != q[i];
+  for (int j = 0; j < LOADS; ++j) {
+    best[j] = -INFINITY;
+    nan[j] = (uint32_t)page[j] >= a.p.n_pages;
+  }
+  auto value = [](const u32x4_v (&w)[WORDS], int i) __attribute__((always_inline)) {
+    if constexpr (DT == DT_F32) return __uint_as_float(w[i / 4][i % 4]);
+    else if constexpr (DT == DT_BF16) return i & 1 ? Bf16::hi(w[0][i / 2]) : Bf16::lo(w[0][i / 2]);
+    else return i & 1 ? Fp16::hi(w[0][i / 2]) : Fp16::lo(w[0][i / 2]);
+  };
+#pragma unroll 1
+  for (uint32_t h0 = 0; h0 < G; h0 += HG) {
+    double up[HG][8], down[HG][8];
+#pragma unroll
+    for (int h = 0; h < HG; ++h) {
+      const int64_t o = (int64_t)seq * a.q_row + (int64_t)(kvh * G + min(h0 + h, G - 1)) * a.q_head + dim;
+      float q[8];
+      if (a.q_dtype == DT_F32) load8<DT_F32>(a.q, o, a.q_wide, q);
+      else if (a.q_dtype == DT_BF16) load8<DT_BF16>(a.q, o, a.q_wide, q);
+      else load8<DT_F16>(a.q, o, a.q_wide, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // (a NaN in q is one in both parts)
+        up[h][i] = q[i] < 0.f ? 0. : (double)q[i];
+        down[h][i] = q[i] > 0.f ? 0. : (double)q[i];
+      }
     }
 #pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) s += lane_xor(s, o);
-    nan |= s != s;
-    best = s > best ? s : best;
+    for (int j = 0; j < LOADS; ++j) {
+      // (converted anew for every group of heads: as 64-bit numbers the bounds would take all registers)
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm("" : "+v"(wl[j][i][e]), "+v"(wh[j][i][e]));
+      double s[HG];
+#pragma unroll
+      for (int h = 0; h < HG; ++h) s[h] = 0.;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double lo = value(wl[j], i), hi = value(wh[j], i);
+#pragma unroll
+        for (int h = 0; h < HG; ++h) s[h] = __builtin_fma(down[h][i], lo, __builtin_fma(up[h][i], hi, s[h]));
+      }
+#pragma unroll
+      for (int h = 0; h < HG; ++h) {
+        s[h] = lanes_sum<LPR>(s[h]);
+        nan[j] |= s[h] != s[h];
+        best[j] = s[h] > best[j] ? s[h] : best[j];
+      }
+    }
   }
 #pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) nan |= (bool)lane_xor((int)nan, o);
-  if (lane % LPR == 0 && block < blocks) keys[((size_t)seq * a.p.n_kv_heads + kvh) * a.blocks + block] = nan ? ORDER_NAN : order_of(best);
+  for (int j = 0; j < LOADS; ++j) {
+    const uint32_t block = first + j * PER + lane / LPR;
+    if (lane % LPR == 0 && block < blocks) keys[((size_t)seq * a.p.n_kv_heads + kvh) * a.blocks + block] = nan[j] ? ORDER_NAN : order_of(best[j]);
+  }
 }
 
 // ---- the best --------------------------------------------------------------------------------------------------
 
-// A workgroup per sequence and kv head.  The key of the last page that is picked is found digit by digit (eight bits at a time,
-// from the highest bit in which two keys differ), then the pages above it and, lowest first, as many equal to it as fit, in order.
+// A workgroup per sequence and kv head.  The key of the last page that is picked is found digit by digit (eight bits at a time, from the
+// highest bit in which two keys differ) until few keys are left, which are ranked; then the pages above it and, lowest
+// first, as many equal to it as fit, in order.  R: keys that a thread keeps in registers, key i of it page 1024 i + thread; 0: more
+// pages, which are read again for every digit.  Bound: latency, of the passes and of the barriers between them.
+template <int R>
 __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* all) {
-  __shared__ uint32_t count[256], total[16], left;
-  __shared__ uint64_t limit, ors[16], ands[16];
+  constexpr uint32_t FEW = 64;
+  __shared__ uint32_t count[256], left, n_open, n_few, total[16], cell[R ? 16 * R : 1];
+  __shared__ uint64_t limit, ors[16], ands[16], few[FEW];
   const uint32_t seq = blockIdx.y, kvh = blockIdx.x, hk = a.p.n_kv_heads, T = a.p.page_tokens, tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
   const size_t row = (size_t)seq * hk + kvh;
@@ -198,14 +336,26 @@ __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* 
   if (tid == 0) a.lens_out[row] = bad ? -1 : blocks == 0 ? 0 : (int32_t)((n - 1) * T + (uint32_t)len - (blocks - 1) * T);
   if (blocks <= a.keep) return;
   const uint64_t* keys = all + row * a.blocks;
-  auto key = [&](uint32_t b) { return b < a.first || b + a.last >= blocks ? ORDER_ALWAYS : keys[b]; };
-  // bits in which keys differ
+  // pages that are picked in any case are above all others
+  auto read = [&](uint32_t b) { return b < a.first || b + a.last >= blocks ? ORDER_ALWAYS : keys[b]; };
+  uint64_t held[R ? R : 1];
+#pragma unroll
+  for (int i = 0; i < R; ++i) held[i] = i * 1024 + tid < blocks ? read(i * 1024 + tid) : 0;  // (0: below every key)
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (held[i]) f(held[i]);
+    } else {
+      for (uint32_t b = tid; b < blocks; b += 1024) f(read(b));
+    }
+  };
+  // bits in which the keys of other pages differ
   uint64_t any = 0, every = ~0ull;
-  for (uint32_t b = tid; b < blocks; b += 1024) {
-    const uint64_t k = key(b);
-    any |= k;
+  each([&](uint64_t k) {
+    any |= k == ORDER_ALWAYS ? 0ull : k;
     every &= k;
-  }
+  });
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     any |= (uint64_t)lane_xor((unsigned long long)any, o);
@@ -215,7 +365,7 @@ __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* 
     ors[wave] = any;
     ands[wave] = every;
   }
-  if (tid == 0) left = a.keep;
+  if (tid == 0) n_few = 0;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -225,15 +375,14 @@ __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* 
   const uint64_t differ = any & ~every;
   int top = differ ? 64 - __clzll((long long)differ) : 0;  // bits below this one are still open
   uint64_t mask = top >= 64 ? 0ull : ~0ull << top, want = every & mask;
-  uint32_t need = a.keep;
-  while (top > 0) {
+  uint32_t need = a.keep - min(a.first + a.last, blocks), open = FEW + 1;  // of the keys that agree with `want` so far: how many are picked, how many there are
+  while (need && top > 0) {
     const int bits = min(top, 8), shift = top - bits;
     if (tid < 256) count[tid] = 0;
     __syncthreads();
-    for (uint32_t b = tid; b < blocks; b += 1024) {
-      const uint64_t k = key(b);
-      if ((k & mask) == want) atomicAdd(&count[(uint32_t)(k >> shift) & ((1u << bits) - 1)], 1u);
-    }
+    each([&](uint64_t k) {
+      if ((k & mask) == want && k != ORDER_ALWAYS) atomicAdd(&count[(uint32_t)(k >> shift) & ((1u << bits) - 1)], 1u);
+    });
     __syncthreads();
     if (wave == 0) {  // lane i: digits 255 - 4 i .. 252 - 4 i, the larger ones first
       uint32_t c[4], mine = 0;
@@ -254,6 +403,7 @@ __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* 
         if (before < need && need <= before + c[j]) {
           limit = want | ((uint64_t)(255 - 4 * lane - j) << shift);
           left = need - before;
+          n_open = c[j];
         }
         before += c[j];
       }
@@ -261,37 +411,101 @@ __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* 
     __syncthreads();
     want = limit;
     need = left;
+    open = n_open;
     top = shift;
     mask = ~0ull << top;
+    if (top > 0 && open <= FEW) {  // rank what is left
+      each([&](uint64_t k) {
+        if ((k & mask) == want && k != ORDER_ALWAYS) few[atomicAdd(&n_few, 1u)] = k;
+      });
+      __syncthreads();
+      if (tid < open) {
+        const uint64_t k = few[tid];
+        uint32_t above = 0, equal = 0;
+        for (uint32_t i = 0; i < open; ++i) {
+          above += few[i] > k;
+          equal += few[i] == k;
+        }
+        if (above < need && need <= above + equal) {  // (equal keys write the same)
+          limit = k;
+          left = need - above;
+        }
+      }
+      __syncthreads();
+      want = limit;
+      need = left;
+      top = 0;
+    }
   }
-  // in order: each thread takes neighbouring pages
-  const uint32_t per = (blocks + 1023) / 1024, b0 = min(tid * per, blocks), b1 = min(b0 + per, blocks);
-  uint32_t above = 0, equal = 0;
-  for (uint32_t b = b0; b < b1; ++b) {
-    const uint64_t k = key(b);
-    above += k > want;
-    equal += k == want;
-  }
-  auto scan = [&](uint32_t v) __attribute__((always_inline)) {  // sum of v over the threads in front of this one
-    uint32_t s = v;
+  if (!need) want = ORDER_ALWAYS - 1;  // (nothing but the pages that are picked in any case)
+  // Where they go.  above: keys that are picked whatever else is; equal: those at the limit, of which the first `need` are.
+  if constexpr (R > 0) {
+    // (counts of a wave's 64 pages of round i: above in the lower sixteen bits, equal in the upper; then their running sums)
+    uint64_t above[R], equal[R];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t u = __shfl_up(s, o, 64);
-      if (lane >= o) s += u;
+    for (int i = 0; i < R; ++i) {
+      above[i] = __ballot(held[i] > want);
+      equal[i] = __ballot(held[i] == want && need);
+      if (lane == 0) cell[i * 16 + wave] = __popcll(above[i]) | (__popcll(equal[i]) << 16);
     }
     __syncthreads();
-    if (lane == 63) total[wave] = s;
+    if (wave == 0) {
+      constexpr int PER = R >= 4 ? R / 4 : 1;
+      uint32_t c[PER], mine = 0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        c[j] = lane * PER + j < 16 * R ? cell[lane * PER + j] : 0;
+        mine += c[j];
+      }
+      uint32_t before = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(before, o, 64);
+        if (lane >= o) before += v;
+      }
+      before -= mine;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (lane * PER + j < 16 * R) cell[lane * PER + j] = before;
+        before += c[j];
+      }
+    }
     __syncthreads();
-    uint32_t before = s - v;
-    for (int i = 0; i < wave; ++i) before += total[i];
-    return before;
-  };
-  uint32_t equal_before = scan(equal);
-  const uint32_t take = equal_before >= need ? 0u : min(equal, need - equal_before);
-  uint32_t to = scan(above + take), taken = 0;
-  for (uint32_t b = b0; b < b1; ++b) {
-    const uint64_t k = key(b);
-    if (k > want || (k == want && taken++ < take)) out[to++] = table[b];
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const uint32_t c = cell[i * 16 + wave], eq = (c >> 16) + __popcll(equal[i] & below);
+      if (held[i] > want || (held[i] == want && eq < need)) out[(c & 0xffffu) + __popcll(above[i] & below) + min(eq, need)] = table[i * 1024 + tid];
+    }
+  } else {  // each thread takes neighbouring pages
+    const uint32_t per = (blocks + 1023) / 1024, b0 = min(tid * per, blocks), b1 = min(b0 + per, blocks);
+    uint32_t above = 0, equal = 0;
+    for (uint32_t b = b0; b < b1; ++b) {
+      const uint64_t k = read(b);
+      above += k > want;
+      equal += need && k == want;
+    }
+    auto scan = [&](uint32_t v) __attribute__((always_inline)) {  // sum of v over the threads in front of this one
+      uint32_t s = v;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(s, o, 64);
+        if (lane >= o) s += u;
+      }
+      __syncthreads();
+      if (lane == 63) total[wave] = s;
+      __syncthreads();
+      uint32_t before = s - v;
+      for (int i = 0; i < wave; ++i) before += total[i];
+      return before;
+    };
+    const uint32_t equal_before = scan(equal);
+    const uint32_t take = equal_before >= need ? 0u : min(equal, need - equal_before);
+    uint32_t to = scan(above + take), taken = 0;
+    for (uint32_t b = b0; b < b1; ++b) {
+      const uint64_t k = read(b);
+      if (k > want || (need && k == want && taken++ < take)) out[to++] = table[b];
+    }
   }
 }
 
@@ -326,12 +540,18 @@ hipError_t launch_page_pick(hipStream_t s, const PagePick& a, void* workspace) {
   uint64_t* keys = static_cast<uint64_t*>(workspace);
   const int bound = a.p.store == PS_F32 ? DT_F32 : a.p.store == PS_F16 ? DT_F16 : DT_BF16;
   if (a.blocks > a.keep) {  // (else every page is picked)
-    const uint32_t per = 4 * (a.p.head_dim == 128 ? 4 : 8);
+    const uint32_t per = 4 * 4 * (a.p.head_dim == 128 ? 4 : 8), G = a.n_q_heads / a.p.n_kv_heads;
     const dim3 grid((a.blocks + per - 1) / per, a.t.n_seqs, a.p.n_kv_heads);
-#define NNC_SCORE_CASE(DT)                                                         \
-  case DT:                                                                         \
-    if (a.p.head_dim == 128) k_page_score<DT, 128><<<grid, 256, 0, s>>>(a, keys);  \
-    else k_page_score<DT, 64><<<grid, 256, 0, s>>>(a, keys);                       \
+#define NNC_SCORE(DT, D)                                                      \
+  do {                                                                        \
+    if (G == 1) k_page_score<DT, D, 1><<<grid, 256, 0, s>>>(a, keys);         \
+    else if (G == 2) k_page_score<DT, D, 2><<<grid, 256, 0, s>>>(a, keys);    \
+    else k_page_score<DT, D, 4><<<grid, 256, 0, s>>>(a, keys);                \
+  } while (0)
+#define NNC_SCORE_CASE(DT)                            \
+  case DT:                                            \
+    if (a.p.head_dim == 128) NNC_SCORE(DT, 128);      \
+    else NNC_SCORE(DT, 64);                           \
     break
     switch (bound) {
       NNC_SCORE_CASE(DT_F32);
@@ -339,7 +559,11 @@ hipError_t launch_page_pick(hipStream_t s, const PagePick& a, void* workspace) {
       NNC_SCORE_CASE(DT_F16);
     }
   }
-  k_page_best<<<dim3(a.p.n_kv_heads, a.t.n_seqs), 1024, 0, s>>>(a, keys);
+  const dim3 best(a.p.n_kv_heads, a.t.n_seqs);
+  if (a.blocks <= 2048) k_page_best<2><<<best, 1024, 0, s>>>(a, keys);
+  else if (a.blocks <= 8192) k_page_best<8><<<best, 1024, 0, s>>>(a, keys);
+  else if (a.blocks <= 16384) k_page_best<16><<<best, 1024, 0, s>>>(a, keys);
+  else k_page_best<0><<<best, 1024, 0, s>>>(a, keys);
   return hipGetLastError();
 }
 
