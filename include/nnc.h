@@ -619,7 +619,7 @@ typedef struct {
  *   then one token more: the first v for which  sum_{w <= v} r(w) > u_k sum_w r(w),  where r = max(p_j - q_j, 0) behind a draft that
  *   was not kept (p_j itself if that is zero everywhere), and r = p_j of the row behind the last draft
  * tokens_out: the kept drafts, that token, and -1 behind it; accepted_out: how many were kept.  Sums, exponentials and comparisons are in
- * 64 bits (exponentials to 2^-47), and sums are taken in a fixed order: the same call gives the same tokens.  Rows behind a sequence's count are not looked at.
+ * 64 bits (exponentials to 2^-42), and sums are taken in a fixed order: the same call gives the same tokens.  Rows behind a sequence's count are not looked at.
  * A sequence whose count is none of 0 .. k or whose temperature is negative or not finite gives the token -1 and
  * keeps nothing; where a row that has to be looked at has no distribution (a NaN, a +infinity, only -infinities), a draft is
  * no token or a random number is NaN, the token there is -1, behind the drafts kept before.
