@@ -110,20 +110,20 @@ __device__ __forceinline__ uint32_t table_row(const AttnArgs& a, uint32_t seq, u
   return a.a.per_head ? seq * a.p.n_kv_heads + kvh : seq;
 }
 
-// The four waves' maxima and sums (smax, ssum [wave][row]) and weighted sums (out[wave * stride + row * pitch + dim], already
+// The NW waves' maxima and sums (smax, ssum [wave][row]) and weighted sums (out[wave * stride + row * pitch + dim], already
 // brought to the common maximum) of n rows -> output, or the workgroup's record.  at(row): its sequence and query head.
-template <int D, class At>
-__device__ __forceinline__ void finish(const AttnArgs& a, uint32_t n, uint32_t split, const At& at, const float (&smax)[4][16],
-                                       const float (&ssum)[4][16], const float* out, int stride, int pitch) {
-  for (uint32_t e = threadIdx.x; e < n * D; e += 256) {
+template <int D, int NW, class At>
+__device__ __forceinline__ void finish(const AttnArgs& a, uint32_t n, uint32_t split, const At& at, const float (&smax)[NW][16],
+                                       const float (&ssum)[NW][16], const float* out, int stride, int pitch) {
+  for (uint32_t e = threadIdx.x; e < n * D; e += 64 * NW) {
     const uint32_t h = e / D, d = e % D;
     uint32_t seq, head;
     at(h, seq, head);
     float L = 0.f, v = 0.f, M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) M = fmaxf(M, smax[i][h]);
+    for (int i = 0; i < NW; ++i) M = fmaxf(M, smax[i][h]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NW; ++i) {
       const float l = ssum[i][h];
       L += l != l ? l : smax[i][h] == -INFINITY ? 0.f : l * __builtin_amdgcn_exp2f(smax[i][h] - M);
       v += out[i * stride + h * pitch + d];

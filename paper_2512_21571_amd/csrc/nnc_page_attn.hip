@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_f32(AttnArgs a, int head_t
     seq = w.seq;
     head = w.head0 + h;
   };
-  finish<D>(a, w.nh, w.split, row, smax, ssum, out[0], 16 * OPITCH, OPITCH);
+  finish<D, 4>(a, w.nh, w.split, row, smax, ssum, out[0], 16 * OPITCH, OPITCH);
 }
 
 // Up to sixteen query heads of one kv head per workgroup, a wave walking tiles of 32 positions, both products on the matrix cores.
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(256, STORE == PS_I8 && !FULL ? 3 : 2) void k_page_a
     seq = w.seq;
     head = w.head0 + h;
   };
-  finish<D>(a, w.nh, w.split, row, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
+  finish<D, 4>(a, w.nh, w.split, row, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
 }
 
 // Merge of a sequence's records for one query head: eight groups of threads take the splits in turn, four dims a thread (64 splits
@@ -484,7 +484,9 @@ __global__ __launch_bounds__(2 * D) void k_page_attn_join(AttnArgs a) {
   const Reach r = reach(a, seq, head / a.by_heads.d);
   // records: of the prefix (first ones, and as many as `gap` before the others), then of the sequence's own positions
   uint32_t used, first = 0xffffffffu, gap = 0;
-  if (a.slot) {
+  if (a.s.whole) {
+    used = a.slots;
+  } else if (a.slot) {
     first = ((a.s.prefix ? r.lo : r.hi) + a.s.chunk - 1) / a.s.chunk;
     gap = a.slot - first;
     used = first + (a.s.prefix ? (r.hi - r.lo + a.plan.chunk - 1) / a.plan.chunk : 0u);

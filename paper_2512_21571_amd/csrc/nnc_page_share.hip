@@ -1,7 +1,7 @@
 // Attention of rows that share the first positions of their contexts: a batch behind one prompt, the beams of a search, the new
-// tokens of one sequence.  The shared positions are read once for up to 64 rows (sequences x query heads of a kv head), whose
-// scores and weighted sums are matrix products with all of them; what a row has behind the prefix is a walk of its own, and
-// the records of both are joined.  Bound: few rows the cache's bytes, many rows the vector instructions of the softmax.
+// tokens of one sequence.  The shared positions are read once for up to 128 rows (sequences x query heads of a kv head), whose
+// scores and weighted sums are matrix products with all of them; what a row has behind the prefix follows in the same walk (up to
+// sixteen rows) or is a walk of its own, and the records are joined.  Bound: few rows the cache's bytes, many rows the vector instructions of the softmax.
 #include "nnc_page_attn.h"
 
 namespace nnc {
@@ -57,6 +57,59 @@ __device__ __forceinline__ void limits_of(const AttnArgs& a, Block<RT>& w) {
   w.begin = w.split * a.s.chunk;
   w.end = min(w.most, w.begin + a.s.chunk);
   w.idle = w.split && w.begin >= w.end;  // (the first workgroup answers for empty rows)
+}
+
+// What the sixteen rows of a workgroup see, in tiles: first the positions that they share, then, sequence by sequence, those behind the
+// prefix.  Lane 0 holds the shared positions, lane j (up to 16) those of the block's j-th sequence; a tile belongs to one of them.
+struct Tiles {
+  uint32_t first_seq, upto, pos0, end;  // of this lane's segment: its last tile + 1, its first and last position + 1
+  uint32_t begin, stop;                 // tiles of this workgroup
+};
+struct TileAt {
+  uint32_t p0, end, seq;  // positions p0 .. < end of sequence seq (~0: shared)
+};
+template <int TILE, int NW>
+__device__ __forceinline__ Tiles tiles_of(const AttnArgs& a, const Block<1>& w, int lane) {
+  Tiles t;
+  t.first_seq = w.group * a.s.width + fdiv(w.row0, a.by_heads);
+  const uint32_t seqs = fdiv(w.row0 + w.n - 1, a.by_heads) - fdiv(w.row0, a.by_heads) + 1;
+  const uint32_t prefix = a.s.prefix ? (uint32_t)max(a.s.prefix[w.group], 0) : 0u;
+  t.pos0 = t.end = 0;
+  if (lane == 0) {
+    t.end = w.most;
+  } else if (a.s.prefix && lane <= (int)seqs) {
+    const int64_t len = (int64_t)a.a.lens[t.first_seq + lane - 1] + a.a.len_add;
+    if (len > prefix && len <= a.a.max_len && len - prefix <= a.s.max_own) {
+      t.pos0 = prefix;
+      t.end = (uint32_t)len;
+    }
+  }
+  t.upto = (t.end - t.pos0 + TILE - 1) / TILE;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up(t.upto, o, 64);
+    if (lane >= o) t.upto += v;
+  }
+  const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)t.upto, 16);
+  // (evenly among the workgroups, a tile at least for each of the waves)
+  const uint32_t each = max((total + gridDim.z - 1) / gridDim.z, (uint32_t)NW);
+  t.begin = w.split * each;
+  t.stop = min(total, t.begin + each);
+  return t;
+}
+template <int TILE>
+__device__ __forceinline__ TileAt tile_at(const Tiles& t, uint32_t tile, int lane) {
+  const int s = __popcll(__ballot(lane <= 16 && t.upto <= tile));
+  const uint32_t before = s ? (uint32_t)__builtin_amdgcn_readlane((int)t.upto, s - 1) : 0u;
+  TileAt r;
+  r.p0 = (uint32_t)__builtin_amdgcn_readlane((int)t.pos0, s) + (tile - before) * TILE;
+  r.end = (uint32_t)__builtin_amdgcn_readlane((int)t.end, s);
+  r.seq = s ? t.first_seq + s - 1 : 0xffffffffu;
+  return r;
+}
+// Table row that a tile's positions are looked up in.
+__device__ __forceinline__ uint32_t row_of_tile(const AttnArgs& a, uint32_t group, const TileAt& t) {
+  return t.seq != 0xffffffffu ? t.seq : a.s.per_group ? group : group * a.s.width;
 }
 
 // Bits of a word of two 16-bit values of which one is not finite.
@@ -153,66 +206,68 @@ __device__ __forceinline__ void load_queries(const AttnArgs& a, const Block<RT>&
   }
 }
 
-// Up to 16 RT rows per workgroup, a wave walking tiles of 32 positions as in k_page_attn_mc, whose products, pieces and layouts these
-// are: S^T = K Q^T for RT tiles of queries against one fragment of K, O^T = V^T P^T for RT tiles of weights against one of V.
-// Rows end at different positions: in tiles behind the smallest limit, scores behind a row's own are -infinity.  Weight zero does not
-// hide an infinity or a NaN in V, so that values there that are not finite are taken as zeros, and rows that do see them
-// become NaN; the same for pages that do not exist.
-template <int STORE, int D, bool FULL, int RT>
-__global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs a) {
+// Up to sixteen rows per workgroup, a wave walking tiles of 32 positions as in k_page_attn_mc, whose products, pieces and layouts these are.
+// Rows see different positions: scores of others are -infinity.  Weight zero does not hide an infinity or a NaN in V, so values that are not finite are
+// taken as zeros where not every row sees them, and rows that do become NaN; the same for pages that do not exist.
+template <int STORE, int D, bool FULL, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
   constexpr bool B8 = page_scaled(STORE);
   constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16;
   constexpr int LD = B8 ? D / 64 : D / 32;   // 16-byte loads of a lane per row: bytes i * 64 + g * 16
   constexpr int PITCH = D * 2 + 32, OPITCH = D + 4;
-  __shared__ __attribute__((aligned(16))) char vbuf[4][32 * PITCH];
-  __shared__ __attribute__((aligned(16))) float sc[4][64];
-  __shared__ float smax[4][16], ssum[4][16];
+  __shared__ __attribute__((aligned(16))) char vbuf[NW][32 * PITCH];
+  __shared__ __attribute__((aligned(16))) float sc[NW][64];
+  __shared__ float smax[NW][16], ssum[NW][16];
   static_assert(16 * OPITCH * 4 <= 32 * PITCH, "the waves' results fit where V was");
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   char* vb = vbuf[wave];
 
   struct Tile {
     u32x4_v k[2][LD], v[2][LD];
     float scale;
+    uint32_t gone;  // first position without a page
   };
   struct Where {
+    TileAt t;
     int32_t page[2];
     uint32_t row[2];
   };
-  Block<RT> w;
-  rows_of<RT>(a, c, w);
-  const Finder find(a, a.s.per_group ? w.group : w.group * a.s.width, w.kvh);
-  auto look = [&](Where& p, uint32_t p0) __attribute__((always_inline)) {
+  Block<1> w;
+  rows_of<1>(a, c, w);
+  limits_of<1>(a, w);
+  const Tiles tiles = tiles_of<32, NW>(a, w, lane);
+  Finder find(a, 0, w.kvh);
+  auto look = [&](Where& p, uint32_t tile) __attribute__((always_inline)) {
+    p.t = tile_at<32>(tiles, tile, lane);
+    find.entries = a.t.entries + (size_t)row_of_tile(a, w.group, p.t) * a.t.max_pages;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) find.look(p0 + h * 16 + c, p.page[h], p.row[h]);
+    for (int h = 0; h < 2; ++h) find.look(p.t.p0 + h * 16 + c, p.page[h], p.row[h]);
   };
+  uint32_t tile = tiles.begin + wave;
+  Where next;
+  if (tile < tiles.stop) look(next, tile);
   auto dim_of = [&](int kt) { return B8 ? (kt >> 1) * 64 + g * 16 + (kt & 1) * 8 : kt * 32 + g * 8; };
-  Where here, next;
-  uint32_t p0 = w.split * a.s.chunk + wave * 32;
-  look(here, p0);
-  look(next, p0 + 128);
-  limits_of<RT>(a, w);
-  if (w.idle) return;
-  const uint32_t end = w.end;
+  float facs[1];
+  u32x4_v qs[1][KT][NQ];
+  load_queries<STORE, D, FULL, 1>(a, w, dim_of, qs, facs);
+  const float fac = facs[0];
 
-  float fac[RT];
-  u32x4_v qf[RT][KT][NQ];
-  load_queries<STORE, D, FULL, RT>(a, w, dim_of, qf, fac);
-
-  uint32_t gone = 0xffffffffu;  // first position without a page
-  auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
+  auto load = [&](Tile& t, const Where& p) __attribute__((always_inline)) {
     uint64_t at[2];
+    uint32_t flagged[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       bool missing = false;
-      at[h] = find.at(p.page[h], p.row[h], p0 + h * 16 + c < end, missing);
-      if (missing) gone = min(gone, p0 + h * 16 + c);
+      at[h] = find.at(p.page[h], p.row[h], p.t.p0 + h * 16 + c < p.t.end, missing);
+      flagged[h] = rows_flagged(missing);
     }
+    const uint32_t f = flagged[0] | (flagged[1] << 16);
+    t.gone = f ? p.t.p0 + __ffs(f) - 1 : 0xffffffffu;
     const uint64_t first = first_lane(at[0]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (p0 + h * 16 + c >= end) at[h] = first;
+      if (p.t.p0 + h * 16 + c >= p.t.end) at[h] = first;
       const uint64_t o = at[h] * (D * (B8 ? 1 : 2)) + g * 16;
 #pragma unroll
       for (int i = 0; i < LD; ++i) t.k[h][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.p.k) + o + i * 64);
@@ -224,31 +279,21 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
   };
 
   constexpr float LIFT = HF::kNarrowRange ? 10.f : 0.f;
-  float m[RT], l[RT];
-  f32x4_t acc[RT][DT];
+  float m = -INFINITY, l = 0.f;
+  f32x4_t acc[DT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-#pragma unroll
-    for (int i = 0; i < DT; ++i) acc[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int i = 0; i < DT; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  auto step = [&](Tile& t, uint32_t p0) __attribute__((always_inline)) {
-    const bool ragged = p0 + 32 > w.least;
-    uint32_t odd = 0xffffffffu;  // first position with a value that is not finite
-    u32x4_v vw[2][B8 ? 2 * LD : LD];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < LD; ++i) {
-        if constexpr (B8) {
-          vw[h][2 * i] = widen8_bf16<STORE>(t.v[h][i][0], t.v[h][i][1]);
-          vw[h][2 * i + 1] = widen8_bf16<STORE>(t.v[h][i][2], t.v[h][i][3]);
-        } else {
-          vw[h][i] = t.v[h][i];
-        }
-      }
+  // V to LDS and the scores, behind which a tile's registers are free for the next one, on its way while this one's weights are formed
+  // and multiplied.  (Two tiles in registers spill, at 16 bits and 128 values.)
+  float x[8], vs[8];
+  auto scores = [&](Tile& t, const TileAt& ta) __attribute__((always_inline)) {
+    const uint32_t p0 = ta.p0, end = ta.end;
+    const bool shared = ta.seq == 0xffffffffu;
+    // from `least` on not every row sees what is there; this lane's row sees what lies before `limit`
+    const uint32_t least = shared ? w.least : 0u, limit = shared ? w.limit[0] : w.seq[0] == ta.seq ? end : 0u;
+    const bool ragged = p0 + 32 > min(least, end);
+    if (limit > t.gone) l = NAN;
     if (ragged) {
       uint32_t flagged[2];
 #pragma unroll
@@ -256,27 +301,36 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
         const uint32_t pos = p0 + h * 16 + c;
         bool bad = false;
 #pragma unroll
-        for (int i = 0; i < (B8 ? 2 * LD : LD); ++i)
+        for (int i = 0; i < LD; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if (pos >= w.least && not_finite2<HF>(vw[h][i][e])) {
-              bad = true;
-              vw[h][i][e] = 0;
+            uint32_t v = t.v[h][i][e];
+            bool odd = false;
+            if constexpr (STORE == PS_E4M3) {  // (NaN is seven ones behind the sign)
+#pragma unroll
+              for (int k = 0; k < 32; k += 8) odd |= ((v >> k) & 0x7fu) == 0x7fu;
+            } else if constexpr (STORE != PS_I8) {
+              odd = not_finite2<HF>(v);
             }
-            if (pos >= end) vw[h][i][e] = 0;
+            if (pos >= least && odd) {
+              bad = true;
+              v = 0;
+            }
+            t.v[h][i][e] = pos >= end ? 0u : v;
           }
         flagged[h] = rows_flagged(bad && pos < end);
       }
       const uint32_t f = flagged[0] | (flagged[1] << 16);
-      if (f) odd = p0 + __ffs(f) - 1;
+      uint32_t odd = f ? p0 + __ffs(f) - 1 : 0xffffffffu;
       if constexpr (B8) {
         // (a scale that is no number belongs to a row of no numbers)
         const uint32_t pos = p0 + (g & 1) * 16 + c;
-        const bool bad = g >= 2 && pos >= w.least && !(fabsf(t.scale) < INFINITY);
+        const bool bad = g >= 2 && pos >= least && !(fabsf(t.scale) < INFINITY);
         const uint64_t b = __ballot(bad && pos < end) >> 32;
         if (b) odd = min(odd, p0 + (uint32_t)__ffsll((unsigned long long)b) - 1);
         if (bad || pos >= end) t.scale = 0.f;
       }
+      if (limit > odd) l = NAN;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -284,83 +338,74 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
       for (int i = 0; i < LD; ++i) {
         char* d = vb + (h * 16 + c) * PITCH;
         if constexpr (B8) {
-          *reinterpret_cast<u32x4_v*>(d + (i * 64 + g * 16) * 2) = vw[h][2 * i];
-          *reinterpret_cast<u32x4_v*>(d + (i * 64 + g * 16) * 2 + 16) = vw[h][2 * i + 1];
+          *reinterpret_cast<u32x4_v*>(d + (i * 64 + g * 16) * 2) = widen8_bf16<STORE>(t.v[h][i][0], t.v[h][i][1]);
+          *reinterpret_cast<u32x4_v*>(d + (i * 64 + g * 16) * 2 + 16) = widen8_bf16<STORE>(t.v[h][i][2], t.v[h][i][3]);
         } else {
-          *reinterpret_cast<u32x4_v*>(d + i * 64 + g * 16) = vw[h][i];
+          *reinterpret_cast<u32x4_v*>(d + i * 64 + g * 16) = t.v[h][i];
         }
       }
     if constexpr (B8) sc[wave][lane] = t.scale;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    f32x4_t ks[2], vs[2];
-    if constexpr (B8) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        ks[h] = *reinterpret_cast<const f32x4_t*>(&sc[wave][h * 16 + g * 4]);
-        vs[h] = *reinterpret_cast<const f32x4_t*>(&sc[wave][32 + h * 16 + g * 4]);
-      }
-    }
-    u32x4_v kf[2][KT];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
-        if constexpr (B8) kf[h][kt] = widen8_bf16<STORE>(t.k[h][kt >> 1][(kt & 1) * 2], t.k[h][kt >> 1][(kt & 1) * 2 + 1]);
-        else kf[h][kt] = t.k[h][kt];
+        u32x4_v kf;
+        if constexpr (B8) kf = widen8_bf16<STORE>(t.k[h][kt >> 1][(kt & 1) * 2], t.k[h][kt >> 1][(kt & 1) * 2 + 1]);
+        else kf = t.k[h][kt];
+#pragma unroll
+        for (int pc = 0; pc < NQ; ++pc) s = HF::mfma(kf, qs[0][kt][pc], s);
       }
-    uint32_t pw[RT][NP][4];
+      if constexpr (B8) {
+        s *= *reinterpret_cast<const f32x4_t*>(&sc[wave][h * 16 + g * 4]);
+        const f32x4_t vv = *reinterpret_cast<const f32x4_t*>(&sc[wave][32 + h * 16 + g * 4]);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      float x[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int pc = 0; pc < NQ; ++pc) s = HF::mfma(kf[h][kt], qf[r][kt][pc], s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[h * 4 + i] = B8 ? s[i] * ks[h][i] : s[i];
+        for (int i = 0; i < 4; ++i) vs[h * 4 + i] = vv[i];
       }
-      if (ragged) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (p0 + (e >> 2) * 16 + g * 4 + (e & 3) >= min(w.limit[r], end)) x[e] = -INFINITY;
-        if (w.limit[r] > odd) l[r] = NAN;
+      for (int i = 0; i < 4; ++i) x[h * 4 + i] = s[i];
+    }
+    if (ragged) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (p0 + (e >> 2) * 16 + g * 4 + (e & 3) >= min(limit, end)) x[e] = -INFINITY;
+    }
+  };
+  auto weigh = [&]() __attribute__((always_inline)) {
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+    top = col4_max(top * fac);
+    if (__any(top > m)) {
+      const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[i] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m - LIFT;
+    uint32_t pw[NP][4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], fac, -base)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e + 1], fac, -base));
+      l += u + v;
+      if constexpr (B8) {
+        u *= vs[e];
+        v *= vs[e + 1];
       }
-      float top = x[0];
+      if constexpr (NP == 3) {
+        uint32_t pc[3];
+        split_weights3<HF>(u, v, pc);
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-      top = col4_max(top * fac[r]);
-      if (__any(top > m[r])) {
-        const float mn = fmaxf(m[r], top), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - mn);
-        m[r] = mn;
-        l[r] *= f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) acc[r][i] *= f;
-      }
-      const float base = m[r] == -INFINITY ? 0.f : m[r] - LIFT;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], fac[r], -base)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e + 1], fac[r], -base));
-        l[r] += u + v;
-        if constexpr (B8) {
-          u *= vs[e >> 2][e & 3];
-          v *= vs[e >> 2][(e & 3) + 1];
-        }
-        if constexpr (NP == 3) {
-          uint32_t pc[3];
-          split_pair3<HF>(u, v, pc);
-#pragma unroll
-          for (int k = 0; k < 3; ++k) pw[r][k][e >> 1] = pc[k];
-        } else {
+        for (int k = 0; k < 3; ++k) pw[k][e >> 1] = pc[k];
+      } else {
 #pragma clang fp contract(off)
-          pw[r][0][e >> 1] = HF::pack2(u, v);
-          u -= HF::lo(pw[r][0][e >> 1]);
-          v -= HF::hi(pw[r][0][e >> 1]);
-          pw[r][1][e >> 1] = HF::pack2(u, v);
-        }
+        pw[0][e >> 1] = HF::pack2(u, v);
+        u -= HF::lo(pw[0][e >> 1]);
+        v -= HF::hi(pw[0][e >> 1]);
+        pw[1][e >> 1] = HF::pack2(u, v);
       }
     }
 #pragma unroll
@@ -369,55 +414,46 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void k_page_attn_rows(AttnArgs
       const u32x2_v lo = lds_column4(p), hi = lds_column4(p + 16 * PITCH);
       const u32x4_v vf = u32x4_v{lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int k = 0; k < NP; ++k) acc[r][dt] = HF::mfma(vf, u32x4_v{pw[r][k][0], pw[r][k][1], pw[r][k][2], pw[r][k][3]}, acc[r][dt]);
+      for (int k = 0; k < NP; ++k) acc[dt] = HF::mfma(vf, u32x4_v{pw[k][0], pw[k][1], pw[k][2], pw[k][3]}, acc[dt]);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
 
-  if (p0 < end) {
-    Tile t0, t1;
-    load(t0, here, p0);
+  if (tile < tiles.stop) {
+    Tile t;
+    load(t, next);
+#pragma unroll 1
     while (true) {
-      if (p0 + 128 < end) load(t1, next, p0 + 128);
-      if (p0 + 256 < end) look(next, p0 + 256);
-      step(t0, p0);
-      p0 += 128;
-      if (p0 >= end) break;
-      if (p0 + 128 < end) load(t0, next, p0 + 128);
-      if (p0 + 256 < end) look(next, p0 + 256);
-      step(t1, p0);
-      p0 += 128;
-      if (p0 >= end) break;
+      const TileAt at = next.t;
+      const bool more = tile + NW < tiles.stop;
+      if (more) look(next, tile + NW);
+      scores(t, at);
+      if (more) load(t, next);
+      weigh();
+      if (!more) break;
+      tile += NW;
     }
   }
-  gone = ~wave_most(~gone);
 
-  // the four waves' results, sixteen rows at a time
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    if (t * 16u >= w.n) break;
-    l[t] = col4_sum(l[t]);
-    if (w.limit[t] > gone || w.bad[t]) l[t] = NAN;
-    __syncthreads();
-    if (g == 0) {
-      smax[wave][c] = m[t];
-      ssum[wave][c] = l[t];
-    }
-    __syncthreads();
-    const float M = fmaxf(fmaxf(smax[0][c], smax[1][c]), fmaxf(smax[2][c], smax[3][c]));
-    const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - M);
-    float* o = reinterpret_cast<float*>(vb);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o + c * OPITCH + dt * 16 + g * 4) = acc[t][dt] * f;
-    __syncthreads();
-    const auto row = [&](uint32_t h, uint32_t& seq, uint32_t& head) __attribute__((always_inline)) {
-      row_at(a, w.group, w.kvh, w.row0 + t * 16 + h, seq, head);
-    };
-    finish<D>(a, min(16u, w.n - t * 16), w.split, row, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
+  // the waves' results
+  l = col4_sum(l);
+  if (w.bad[0]) l = NAN;
+  if (g == 0) {
+    smax[wave][c] = m;
+    ssum[wave][c] = l;
   }
+  __syncthreads();
+  float M = smax[0][c];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) M = fmaxf(M, smax[i][c]);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  float* o = reinterpret_cast<float*>(vb);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o + c * OPITCH + dt * 16 + g * 4) = acc[dt] * f;
+  __syncthreads();
+  const auto row = [&](uint32_t h, uint32_t& seq, uint32_t& head) __attribute__((always_inline)) { row_at(a, w.group, w.kvh, w.row0 + h, seq, head); };
+  finish<D, NW>(a, w.n, w.split, row, smax, ssum, reinterpret_cast<const float*>(vbuf[0]), 32 * PITCH / 4, OPITCH);
 }
 
 // More rows: the NW waves of a workgroup share tiles of 64 positions in LDS, WR of them with sixteen rows of their own,
@@ -437,7 +473,7 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void k_page_attn_block(AttnArgs a)
   __shared__ float smax[NW][16], ssum[NW][16];
   __shared__ uint32_t spoilt;
   static_assert(NW * 16 * OPITCH * 4 <= 2 * BUFFER, "the waves' results fit where the tiles were");
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4, wr = wave % WR, wp = wave / WR;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4, wr = wave % WR, wp = wave / WR;
   const int row_l = tid / CHUNKS, chunk_l = tid % CHUNKS;
 
   Block<1> w;
@@ -712,47 +748,54 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void k_page_attn_block(AttnArgs a)
 }
 
 // fp32 pages, as k_page_attn_f32: sixteen rows per workgroup, on the fp32 matrix instruction, tiles of 16 positions.
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows_f32(AttnArgs a) {
   constexpr int LD = D / 16, NB = D / 64, OPITCH = D + 4;
-  __shared__ __attribute__((aligned(16))) float out[4][16 * OPITCH];
-  __shared__ float smax[4][16], ssum[4][16];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  __shared__ __attribute__((aligned(16))) float out[NW][16 * OPITCH];
+  __shared__ float smax[NW][16], ssum[NW][16];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   struct Tile {
     f32x4_t k[LD], v[4][NB];
+    uint32_t gone;  // first position without a page
   };
   struct Where {
+    TileAt t;
     int32_t page[5];
     uint32_t row[5];
   };
   Block<1> w;
   rows_of<1>(a, c, w);
-  const Finder find(a, a.s.per_group ? w.group : w.group * a.s.width, w.kvh);
-  uint32_t gone = 0xffffffffu;
-  auto look = [&](Where& t, uint32_t p0) __attribute__((always_inline)) {
-    find.look(p0 + c, t.page[4], t.row[4]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) find.look(p0 + g * 4 + i, t.page[i], t.row[i]);
-  };
-  Where here, next;
-  uint32_t p0 = w.split * a.s.chunk + wave * 16;
-  look(here, p0);
-  look(next, p0 + 64);
   limits_of<1>(a, w);
-  if (w.idle) return;
-  const uint32_t end = w.end, limit = w.limit[0];
-  auto load = [&](Tile& t, const Where& p, uint32_t p0) __attribute__((always_inline)) {
+  const Tiles tiles = tiles_of<16, NW>(a, w, lane);
+  Finder find(a, 0, w.kvh);
+  auto look = [&](Where& p, uint32_t tile) __attribute__((always_inline)) {
+    p.t = tile_at<16>(tiles, tile, lane);
+    find.entries = a.t.entries + (size_t)row_of_tile(a, w.group, p.t) * a.t.max_pages;
+    find.look(p.t.p0 + c, p.page[4], p.row[4]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) find.look(p.t.p0 + g * 4 + i, p.page[i], p.row[i]);
+  };
+  uint32_t tile = tiles.begin + wave;
+  Where next;
+  if (tile < tiles.stop) look(next, tile);
+  uint64_t first = 0;
+  auto load_k = [&](Tile& t, const Where& p) __attribute__((always_inline)) {
+    const uint32_t p0 = p.t.p0, end = p.t.end;
     bool missing = false;
-    uint64_t at = find.at(p.page[4], p.row[4], p0 + c < end, missing);
-    if (missing) gone = min(gone, p0 + c);
-    const uint64_t first = first_lane(at);
+    const uint64_t at = find.at(p.page[4], p.row[4], p0 + c < end, missing);
+    const uint32_t f = rows_flagged(missing);
+    t.gone = f ? p0 + __ffs(f) - 1 : 0xffffffffu;
+    first = first_lane(at);
     const float* k = static_cast<const float*>(a.p.k) + (p0 + c < end ? at : first) * D + g * 4;
 #pragma unroll
     for (int i = 0; i < LD; ++i) t.k[i] = *reinterpret_cast<const f32x4_t*>(k + i * 16);
+  };
+  auto load_v = [&](Tile& t, const Where& p) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool in = p0 + g * 4 + i < end;
-      at = find.at(p.page[i], p.row[i], in, missing);
+      const bool in = p.t.p0 + g * 4 + i < p.t.end;
+      bool missing = false;
+      const uint64_t at = find.at(p.page[i], p.row[i], in, missing);
       const float* v = static_cast<const float*>(a.p.v) + (in ? at : first) * D + c * 4;
 #pragma unroll
       for (int b = 0; b < NB; ++b) t.v[i][b] = *reinterpret_cast<const f32x4_t*>(v + b * 64);
@@ -777,16 +820,20 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  auto step = [&](Tile& t, uint32_t p0) __attribute__((always_inline)) {
+  float x[4];
+  auto scores = [&](Tile& t, const TileAt& ta) __attribute__((always_inline)) {
+    const uint32_t p0 = ta.p0, end = ta.end;
+    const bool shared = ta.seq == 0xffffffffu;
+    const uint32_t least = shared ? w.least : 0u, limit = shared ? w.limit[0] : w.seq[0] == ta.seq ? end : 0u;
+    if (limit > t.gone) l = NAN;
     f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < LD; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[i][j], q[i][j], s, 0, 0, 0);
-    float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = s[i] * fac;
-    if (p0 + 16 > w.least) {
+    if (p0 + 16 > min(least, end)) {
       uint32_t odd = 0xffffffffu;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -796,8 +843,8 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if (pos >= w.least && !(fabsf(t.v[i][b][j]) < INFINITY)) bad = true;
-            if (pos >= end || (pos >= w.least && !(fabsf(t.v[i][b][j]) < INFINITY))) t.v[i][b][j] = 0.f;
+            if (pos >= least && !(fabsf(t.v[i][b][j]) < INFINITY)) bad = true;
+            if (pos >= end || (pos >= least && !(fabsf(t.v[i][b][j]) < INFINITY))) t.v[i][b][j] = 0.f;
           }
         // (lanes of one g hold one row)
         const uint64_t f = __ballot(bad && pos < end);
@@ -806,6 +853,8 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
       }
       if (limit > odd) l = NAN;
     }
+  };
+  auto weigh = [&](Tile& t) __attribute__((always_inline)) {
     const float top = col4_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
     if (__any(top > m)) {
       const float mn = fmaxf(m, top), r = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
@@ -827,31 +876,33 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
         for (int j = 0; j < 4; ++j) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[i][b][j], p, acc[b][j], 0, 0, 0);
     }
   };
-  if (p0 < end) {
-    Tile t0, t1;
-    load(t0, here, p0);
+  if (tile < tiles.stop) {
+    Tile t;
+    load_k(t, next);
+    load_v(t, next);
+#pragma unroll 1
     while (true) {
-      if (p0 + 64 < end) load(t1, next, p0 + 64);
-      if (p0 + 128 < end) look(next, p0 + 128);
-      step(t0, p0);
-      p0 += 64;
-      if (p0 >= end) break;
-      if (p0 + 64 < end) load(t0, next, p0 + 64);
-      if (p0 + 128 < end) look(next, p0 + 128);
-      step(t1, p0);
-      p0 += 64;
-      if (p0 >= end) break;
+      const TileAt at = next.t;
+      const bool more = tile + NW < tiles.stop;
+      if (more) look(next, tile + NW);
+      scores(t, at);
+      if (more) load_k(t, next);
+      weigh(t);
+      if (!more) break;
+      load_v(t, next);
+      tile += NW;
     }
   }
-  gone = ~wave_most(~gone);
   l = col4_sum(l);
-  if (limit > gone || w.bad[0]) l = NAN;
+  if (w.bad[0]) l = NAN;
   if (g == 0) {
     smax[wave][c] = m;
     ssum[wave][c] = l;
   }
   __syncthreads();
-  const float M = fmaxf(fmaxf(smax[0][c], smax[1][c]), fmaxf(smax[2][c], smax[3][c]));
+  float M = smax[0][c];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) M = fmaxf(M, smax[i][c]);
   const float r = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -862,10 +913,13 @@ __global__ __launch_bounds__(256, 2) void k_page_attn_rows_f32(AttnArgs a) {
   const auto row = [&](uint32_t h, uint32_t& seq, uint32_t& head) __attribute__((always_inline)) {
     row_at(a, w.group, w.kvh, w.row0 + h, seq, head);
   };
-  finish<D>(a, w.n, w.split, row, smax, ssum, out[0], 16 * OPITCH, OPITCH);
+  finish<D, NW>(a, w.n, w.split, row, smax, ssum, out[0], 16 * OPITCH, OPITCH);
 }
 
 }  // namespace
+
+// Waves of a workgroup of up to sixteen rows.  (Eight: 13.9 us in place of 14.8 at 4 rows of 304 positions, 23.5 in place of 19.6 at 16384.)
+static constexpr int ROWS_WAVES = 4;
 
 // (see launch_page_share: queries that enter the product as they are)
 static bool own_type(const PagePool& p, const PageAttn& a) {
@@ -876,26 +930,36 @@ static bool own_type(const PagePool& p, const PageAttn& a) {
 // 64 values fill a tile of 64 positions with the loads of four.)
 static constexpr int most_tiles(int store, int dim, bool full) { return full || (page_scaled(store) && dim == 64) ? 4 : 8; }
 
+// Workgroups along the positions: as many as fill the chip (two on a CU).  Up to sixteen rows (sequences x query heads of a kv head), and fp32,
+// walk what is behind the prefix in the same launch, evenly shared out whatever the lengths are, and up to 512 positions one workgroup
+// takes them all, which saves the join (8 kv heads of two query heads, four rows, 304 positions and up to 16 of their own, bf16: 14.8 us by one
+// workgroup, 10.6 + 3.8 us and a second launch by four; 600 positions 20 and 9.0 + 3.9; fp32 304 18.4 and 12.2 + 3.9).
 PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageShare& s, uint32_t max_slots) {
   const uint32_t G = a.n_q_heads / p.n_kv_heads, groups = s.width ? s.n_rows / s.width : 0, rows = s.width * G;
   PageSharePlan pl{};
   pl.tiles = p.store == PS_F32 || rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : most_tiles(p.store, p.head_dim, !own_type(p, a));
   const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)groups * p.n_kv_heads * ((rows + 16 * pl.tiles - 1) / (16 * pl.tiles)));
-  const uint32_t span = a.max_len;
-  uint64_t splits = (512 + wgs - 1) / wgs;
-  splits = std::min<uint64_t>(splits, span <= 256 ? 1 : (span + 127) / 128);
   const bool own = s.prefix && s.max_own;
   pl.own.chunk = 1;  // (the join divides by it)
-  if (own) {
+  uint64_t span = a.max_len;
+  if (own && pl.tiles == 1) {
+    span += (uint64_t)std::min(s.width, (16 + G - 1) / G) * std::min(s.max_own, a.max_len);
+  } else if (own) {
     PageAttn o = a;
     o.max_len = std::min(s.max_own, a.max_len);
     o.window = 0;
     pl.own = plan_page_attention(p, s.n_rows, o, std::max(1u, max_slots / 2));
   }
+  uint64_t splits = (512 + wgs - 1) / wgs;
+  splits = std::min<uint64_t>(splits, span <= (pl.tiles == 1 ? 512 : 256) ? 1 : (span + 127) / 128);
   splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, max_slots - pl.own.splits));
-  pl.chunk = (uint32_t)(((span + splits - 1) / splits + 127) / 128 * 128);
-  if (pl.chunk == 0) pl.chunk = 1;
-  pl.splits = span ? (span + pl.chunk - 1) / pl.chunk : 1;
+  if (pl.tiles == 1) {
+    pl.chunk = 1;
+    pl.splits = (uint32_t)splits;
+  } else {
+    pl.chunk = (uint32_t)std::max<uint64_t>(1, ((span + splits - 1) / splits + 127) / 128 * 128);
+    pl.splits = span ? (uint32_t)((span + pl.chunk - 1) / pl.chunk) : 1;
+  }
   const uint32_t slots = pl.splits + pl.own.splits;
   pl.floats = slots > 1 ? (size_t)s.n_rows * a.n_q_heads * slots * (p.head_dim + 2) : 0;
   return pl;
@@ -910,11 +974,12 @@ hipError_t launch_page_share(hipStream_t st, const PagePool& p, const PageTable&
     return hipErrorInvalidValue;
   AttnArgs g{p, t, a, plan.own, workspace, query_wide(a), slots, 0, s, fast_div(s.width), fast_div(G)};
   g.s.chunk = plan.chunk;
+  g.s.whole = plan.tiles == 1;
   const dim3 grid((uint32_t)blocks, groups, plan.splits);
 #define NNC_ROWS_TILES(ST, D, FULL)                                                                                        \
   do {                                                                                                                     \
     constexpr int MOST = most_tiles(ST, D, FULL);                                                                          \
-    if (plan.tiles == 1) k_page_attn_rows<ST, D, FULL, 1><<<grid, 256, 0, st>>>(g);                                        \
+    if (plan.tiles == 1) k_page_attn_rows<ST, D, FULL, ROWS_WAVES><<<grid, 64 * ROWS_WAVES, 0, st>>>(g);                                           \
     else if (plan.tiles == 2) k_page_attn_block<ST, D, FULL, 4, 2><<<grid, 256, 0, st>>>(g);                               \
     else if (plan.tiles == 4) k_page_attn_block<ST, D, FULL, 4, 4><<<grid, 256, 0, st>>>(g);                               \
     else k_page_attn_block<ST, D, FULL, MOST, MOST><<<grid, 64 * MOST, 0, st>>>(g);                                        \
@@ -931,8 +996,8 @@ hipError_t launch_page_share(hipStream_t st, const PagePool& p, const PageTable&
     break
   switch (p.store) {
     case PS_F32:
-      if (p.head_dim == 128) k_page_attn_rows_f32<128><<<grid, 256, 0, st>>>(g);
-      else k_page_attn_rows_f32<64><<<grid, 256, 0, st>>>(g);
+      if (p.head_dim == 128) k_page_attn_rows_f32<128, ROWS_WAVES><<<grid, 64 * ROWS_WAVES, 0, st>>>(g);
+      else k_page_attn_rows_f32<64, ROWS_WAVES><<<grid, 64 * ROWS_WAVES, 0, st>>>(g);
       break;
     NNC_ROWS_CASE(PS_BF16);
     NNC_ROWS_CASE(PS_F16);
@@ -946,7 +1011,7 @@ hipError_t launch_page_share(hipStream_t st, const PagePool& p, const PageTable&
     if (hipError_t e = launch_page_walk(st, g, s.n_rows)) return e;
   }
   if (slots == 1) return hipSuccess;
-  g.slot = plan.splits;
+  g.slot = g.s.whole ? 0 : plan.splits;
   return launch_page_join(st, g, s.n_rows);
 }
 

@@ -278,6 +278,7 @@ struct PageShare {
   const int32_t* prefix = nullptr;  // [groups] shared positions; NULL: all are
   uint32_t max_own = 0;             // no row has more behind them
   uint32_t chunk = 0;               // positions of a workgroup along the prefix (of the plan)
+  bool whole = false;               // every workgroup leaves a record of every row, of the positions behind the prefix too
 };
 struct PageSharePlan {
   uint32_t splits, chunk, tiles;  // workgroups along a prefix, positions of each, tiles of sixteen rows of each

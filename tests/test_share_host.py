@@ -84,10 +84,11 @@ def test_bad_shared_rows(nnc):
     assert call(layer=2) == nnc.E_ARG
     for change in (dict(q=None), dict(out=None), dict(lens=None)):
         assert call(q=query(nnc, **change)) == nnc.E_ARG, change
-    # the prefix and what is behind it are joined, which needs a workspace of the size that is asked for
-    assert L.nnc_page_attention_shared_workspace(ref(pages(nnc)), ref(table(nnc)), ref(query(nnc)), ref(share(nnc)), ctypes.byref(n)) == nnc.OK and n.value > 0
+    # parts of a long context are joined, which needs a workspace of the size that is asked for
+    long_t, long_q = table(nnc, max_pages=1024), query(nnc, max_len=16000)
+    assert L.nnc_page_attention_shared_workspace(ref(pages(nnc)), ref(long_t), ref(long_q), ref(share(nnc)), ctypes.byref(n)) == nnc.OK and n.value > 0
     for ws, size in ((None, 1 << 30), (P, n.value - 1), (P + 4, 1 << 30)):
-        assert call(ws=ws, size=size) == nnc.E_ARG
+        assert call(t=long_t, q=long_q, ws=ws, size=size) == nnc.E_ARG
     assert "workspace" in nnc.last_error()
     assert call(t=table(nnc, n_seqs=0), ws=None, size=0) == nnc.OK                                                     # nobody there
     assert L.nnc_page_attention_shared_workspace(ref(pages(nnc)), ref(table(nnc)), ref(query(nnc)), ref(share(nnc, max_own=0)), ctypes.byref(n)) == nnc.OK and n.value == 0
