@@ -5,6 +5,7 @@ forward pass runs in the library's HIP kernels.  PyTorch supplies device memory
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 
@@ -322,11 +323,12 @@ class Pages:
         return cls(k, v, *scales)
 
     def _table(self, tables, name="tables", heads=False):
-        if heads and tables.dim() == 3 and tables.shape[1] == self.n_kv_heads:   # (a table for every kv head)
-            tables = tables.flatten(0, 1)
-        if tables.dtype != self._i32 or tables.dim() != 2 or tables.device != self.device or not tables.is_contiguous():
+        *of, m = tables.shape or (0,)
+        n = of[0] if of else 0
+        if heads and len(of) == 2 and of[1] == self.n_kv_heads:   # (a table for every kv head)
+            n, of = n * of[1], of[:1]
+        if tables.dtype != self._i32 or len(of) != 1 or tables.device != self.device or not tables.is_contiguous():
             _bad(f"{name}: contiguous int32 [sequences, pages] on {self.device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
-        n, m = tables.shape
         return NncPageTable(tables.data_ptr() or None, n, m)
 
     def _index(self, x, n, name):
@@ -468,36 +470,41 @@ class Pages:
         """(table, query, share) of a call of attention_shared."""
         if q.dim() != 4 or lens.shape != q.shape[:2] or q.shape[3] != self.head_dim:
             _bad(f"q [groups, width, heads, {self.head_dim}] and lens [groups, width] expected, not {list(q.shape)} and {list(lens.shape)}")
-        groups, width, heads, _ = q.shape
-        rows = []
-        for name, x in (("q", q), ("out", out)):
-            if x is not None:
-                if x.shape != q.shape or x.dtype != q.dtype:
-                    _bad(f"{name}: type and shape of q expected")
-                between, row = x.stride()[:2]
-                if width == 1:
-                    row = between   # (one row a group: no rows are `row` apart)
-                if groups > 1 and between != width * row and x.numel():
-                    _bad(f"{name}: one distance between all rows expected")
-                rows.append(x.as_strided((groups * width, heads, self.head_dim), (row, *x.stride()[2:])))
-        if max_own is not None and not 0 <= max_own <= 0x7fffffff:
-            _bad(f"max_own {max_own}: 0 .. 2^31 - 1 expected")
-        if prefix is None:
-            if tables.dim() != 2 or tables.shape[0] != groups:
-                _bad(f"tables: a row for each of {groups} groups expected, not {list(tables.shape)}")
-        else:
-            tables = tables.flatten(0, 1) if tables.dim() == 3 and tables.is_contiguous() else tables
-            if tables.dim() != 2 or tables.shape[0] != groups * width:
-                _bad(f"tables: a row for each of {groups} x {width} sequences expected, not {list(tables.shape)}")
-            if prefix.dtype != self._i32 or prefix.shape != (groups,) or prefix.device != self.device or not prefix.is_contiguous():
-                _bad(f"prefix: contiguous int32 [{groups}] on {self.device} expected, not {prefix.dtype} {list(prefix.shape)} on {prefix.device}")
-        table = self._table(tables)
-        if not lens.is_contiguous():
-            _bad("lens: contiguous int32 [groups, width] expected")
-        query = self._query(rows[0], groups * width, lens.view(-1), max_len, scale, 0, rows[1] if out is not None else None)
+        shape, i32, device = q.shape, self._i32, self.device
+        groups, width, heads, _ = shape
+        n = groups * width
+        row, head = self._apart(q, "q")
+        o_row = o_head = 0
+        if out is not None:
+            if out.shape != shape or out.dtype != q.dtype:
+                _bad("out: type and shape of q expected")
+            o_row, o_head = self._apart(out, "out")
+        if not 0 <= max_len <= 0x7fffffff or not (max_own is None or 0 <= max_own <= 0x7fffffff):
+            _bad(f"max_len {max_len}, max_own {max_own}: 0 .. 2^31 - 1 expected")
+        *of, pages = tables.shape
+        if math.prod(of) != (groups if prefix is None else n) or not 1 <= len(of) <= (1 if prefix is None else 2):
+            _bad(f"tables: a row for each of {groups} groups expected, not {list(tables.shape)}" if prefix is None else
+                 f"tables: a row for each of {groups} x {width} sequences expected, not {list(tables.shape)}")
+        if tables.dtype != i32 or tables.device != device or not tables.is_contiguous():
+            _bad(f"tables: contiguous int32 on {device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
+        if prefix is not None and (prefix.dtype != i32 or prefix.shape != (groups,) or prefix.device != device or not prefix.is_contiguous()):
+            _bad(f"prefix: contiguous int32 [{groups}] on {device} expected, not {prefix.dtype} {list(prefix.shape)} on {prefix.device}")
+        if lens.dtype != i32 or lens.device != device or not lens.is_contiguous():
+            _bad(f"lens: contiguous int32 [{groups}, {width}] on {device} expected, not {lens.dtype} {list(lens.shape)} on {lens.device}")
+        query = NncPageQuery(q.data_ptr(), _ptr(out), _dtype_of(q), heads, row, head, o_row, o_head, lens.data_ptr(), max_len, 0,
+                             self.head_dim ** -0.5 if scale is None else scale)
         if max_own is None:
-            max_own = max_len or table.max_pages * self.page_tokens
-        return table, query, NncPageShare(width, _ptr(prefix), max_own)
+            max_own = max_len or pages * self.page_tokens
+        return NncPageTable(tables.data_ptr() or None, math.prod(of), pages), query, NncPageShare(width, _ptr(prefix), max_own)
+
+    def _apart(self, x, name):
+        """(row stride, head stride) of a tensor [groups, width, heads, head_dim] whose rows are all one distance apart."""
+        (groups, width, _, _), (between, row, head, one) = x.shape, x.stride()
+        if width == 1:
+            row = between   # (one row a group: no rows are `row` apart)
+        if x.device != self.device or ((one != 1 or (groups > 1 and between != width * row)) and x.numel()):
+            _bad(f"{name}: on {self.device}, the elements of a head next to each other and one distance between all rows expected")
+        return row, head
 
     def attention_shared_workspace(self, q, tables, lens, prefix=None, max_len: int = 0, max_own: int | None = None) -> int:
         """Bytes of workspace of the same call of `attention_shared`."""
