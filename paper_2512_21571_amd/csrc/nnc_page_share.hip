@@ -124,21 +124,29 @@ __device__ __forceinline__ uint32_t rows_flagged(bool x) {
   return (uint32_t)(b | (b >> 16) | (b >> 32) | (b >> 48)) & 0xffffu;
 }
 
-// split_pair3 of weights.  The remainder behind a bf16 value is one product of pairs, v - (0 a + 1 b), exact like the subtraction
-// (a weight that is no number spoils its neighbour, which is of the same row).  The pairs (-1, 0) and (0, -1) are kept from the
-// compiler, which takes the first for the inline constant -1, to the instruction a pair (0, -1).
-template <class HF>
-__device__ __forceinline__ void split_weights3(float u, float v, uint32_t (&piece)[3]) {
-  if constexpr (HF::kNarrowRange) {
+// Weights in pieces of the matrix cores' type: three for an fp32 output, and two, where the queries and so the output have 16 bits: two
+// bf16 pieces leave out 2^-18 of a weight, which is 2^-9 of the output's own rounding, two binary16 pieces 2^-22.  (Two for three: the 256
+// rows of 16384 positions of launch_page_share's figures 50.9 -> 43.5 us.)  The remainder behind a bf16 value is one product of pairs, v - (0 a + 1 b),
+// exact like the subtraction (a weight that is no number spoils its neighbour, which is of the same row).  The pairs (-1, 0) and (0, -1) are kept
+// from the compiler, which takes the first for the inline constant -1, to the instruction a pair (0, -1).
+template <class HF, int NP>
+__device__ __forceinline__ void split_weights(float u, float v, uint32_t (&piece)[NP]) {
+  if constexpr (HF::kNarrowRange && NP == 3) {
     split_pair3<HF>(u, v, piece);
+  } else if constexpr (HF::kNarrowRange) {
+#pragma clang fp contract(off)
+    piece[0] = HF::pack2(u, v);
+    u -= HF::lo(piece[0]);
+    v -= HF::hi(piece[0]);
+    piece[1] = HF::pack2(u, v);
   } else {
     typedef typename HF::vec2 pair_t;
     uint32_t low = 0x0000bf80u, high = 0xbf800000u;
     asm("" : "+s"(low), "+s"(high));
 #pragma unroll
-    for (int s = 0; s < 3; ++s) {
+    for (int s = 0; s < NP; ++s) {
       piece[s] = HF::pack2(u, v);
-      if (s < 2) {
+      if (s + 1 < NP) {
         u = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, piece[s]), __builtin_bit_cast(pair_t, low), u, false);
         v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, piece[s]), __builtin_bit_cast(pair_t, high), v, false);
       }
@@ -213,7 +221,7 @@ template <int STORE, int D, bool FULL, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
   constexpr bool B8 = page_scaled(STORE);
-  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16;
+  constexpr int NQ = FULL ? 3 : 1, NP = FULL ? 3 : 2, KT = D / 32, DT = D / 16;
   constexpr int LD = B8 ? D / 64 : D / 32;   // 16-byte loads of a lane per row: bytes i * 64 + g * 16
   constexpr int PITCH = D * 2 + 32, OPITCH = D + 4;
   __shared__ __attribute__((aligned(16))) char vbuf[NW][32 * PITCH];
@@ -395,18 +403,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
         u *= vs[e];
         v *= vs[e + 1];
       }
-      if constexpr (NP == 3) {
-        uint32_t pc[3];
-        split_weights3<HF>(u, v, pc);
+      uint32_t pc[NP];
+      split_weights<HF, NP>(u, v, pc);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) pw[k][e >> 1] = pc[k];
-      } else {
-#pragma clang fp contract(off)
-        pw[0][e >> 1] = HF::pack2(u, v);
-        u -= HF::lo(pw[0][e >> 1]);
-        v -= HF::hi(pw[0][e >> 1]);
-        pw[1][e >> 1] = HF::pack2(u, v);
-      }
+      for (int k = 0; k < NP; ++k) pw[k][e >> 1] = pc[k];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -464,7 +464,7 @@ template <int STORE, int D, bool FULL, int NW, int WR>
 __global__ __launch_bounds__(64 * NW, NW / 2) void k_page_attn_block(AttnArgs a) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
   constexpr bool B8 = page_scaled(STORE);
-  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16, WP = NW / WR, TILE = 64;
+  constexpr int NQ = FULL ? 3 : 1, NP = FULL ? 3 : 2, KT = D / 32, DT = D / 16, WP = NW / WR, TILE = 64;
   constexpr int CHUNKS = D * (B8 ? 1 : 2) / 16, ROWS = 64 * NW / CHUNKS, LD = TILE / ROWS;  // sixteen bytes of a row; rows of a load; loads
   constexpr int KP = D * 2 + 16, VP = D * 2 + 32, OPITCH = D + 4;                       // bytes from row to row, without bank conflicts
   constexpr int BUFFER = TILE * (KP + VP);
@@ -639,18 +639,10 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void k_page_attn_block(AttnArgs a)
         u *= vs[e & 3];
         v *= vs[(e & 3) + 1];
       }
-      if constexpr (NP == 3) {
-        uint32_t pc[3];
-        split_weights3<HF>(u, v, pc);
+      uint32_t pc[NP];
+      split_weights<HF, NP>(u, v, pc);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) pw[k][e >> 1] = pc[k];
-      } else {
-#pragma clang fp contract(off)
-        pw[0][e >> 1] = HF::pack2(u, v);
-        u -= HF::lo(pw[0][e >> 1]);
-        v -= HF::hi(pw[0][e >> 1]);
-        pw[1][e >> 1] = HF::pack2(u, v);
-      }
+      for (int k = 0; k < NP; ++k) pw[k][e >> 1] = pc[k];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; dt += 2) {
