@@ -26,8 +26,10 @@ __device__ __forceinline__ void rows_of(const AttnArgs& a, int c, Block<RT>& w, 
   // (blocks of one kv head lie a multiple of the kv heads apart: on one XCD where those are eight)
   const uint32_t block = blockIdx.x / a.p.n_kv_heads;
   w.kvh = blockIdx.x - block * a.p.n_kv_heads;
-  w.group = blockIdx.y;
   w.split = blockIdx.z;
+  // (the groups turned by the split: a CU's workgroups, a multiple of 256 apart, are then not all of one long group; 16 groups of
+  // 20 .. 4100 positions 42.3 -> 33.3 us)
+  w.group = (blockIdx.y + w.split + (w.split >> 1) + (w.split >> 3)) % gridDim.y;
   w.row0 = block * 16 * RT * WR;
   w.n = min(16u * RT * WR, a.s.width * a.by_heads.d - w.row0);
 #pragma unroll
@@ -926,6 +928,10 @@ static constexpr int most_tiles(int store, int dim, bool full) { return full || 
 // walk what is behind the prefix in the same launch, evenly shared out whatever the lengths are, and up to 512 positions one workgroup
 // takes them all, which saves the join (8 kv heads of two query heads, four rows, 304 positions and up to 16 of their own, bf16: 14.8 us by one
 // workgroup, 10.6 + 3.8 us and a second launch by four; 600 positions 20 and 9.0 + 3.9; fp32 304 18.4 and 12.2 + 3.9).
+// More rows: tiles of 64 positions, and the lengths of several groups being unknown here, up to twice the workgroups, of 512 positions at least
+// (without / with that, five drafts of 32 query heads over int8, us of the walk: 32 groups of 20 .. 8000 positions 124.5 / 111.0, 8 of 333 ..
+// 16000 72.8 / 68.1; where all are equally long it costs: 16 of 4100 43.3 / 49.6.  Twice the workgroups for shorter chunks, too: 4 of 333 .. 4100
+// 18.7 / 21.4).
 PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageShare& s, uint32_t max_slots) {
   const uint32_t G = a.n_q_heads / p.n_kv_heads, groups = s.width ? s.n_rows / s.width : 0, rows = s.width * G;
   PageSharePlan pl{};
@@ -943,13 +949,14 @@ PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageSh
     pl.own = plan_page_attention(p, s.n_rows, o, std::max(1u, max_slots / 2));
   }
   uint64_t splits = (512 + wgs - 1) / wgs;
+  if (pl.tiles > 1 && groups > 1) splits = std::max<uint64_t>(splits, std::min<uint64_t>((1024 + wgs - 1) / wgs, span / 512));
   splits = std::min<uint64_t>(splits, span <= (pl.tiles == 1 ? 512 : 256) ? 1 : (span + 127) / 128);
   splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, max_slots - pl.own.splits));
   if (pl.tiles == 1) {
     pl.chunk = 1;
     pl.splits = (uint32_t)splits;
   } else {
-    pl.chunk = (uint32_t)std::max<uint64_t>(1, ((span + splits - 1) / splits + 127) / 128 * 128);
+    pl.chunk = (uint32_t)std::max<uint64_t>(1, ((span + splits - 1) / splits + 63) / 64 * 64);
     pl.splits = span ? (uint32_t)((span + pl.chunk - 1) / pl.chunk) : 1;
   }
   const uint32_t slots = pl.splits + pl.own.splits;
