@@ -44,14 +44,15 @@ struct VerifyArgs {
 
 constexpr double LOG2E = 1.4426950408889634;
 
-// e^((x - m) / T) in 64 bits, to 2^-42: with (x - m) / T log2 e = (n + r) / 256, |r| <= 1/2, it is 2^(n / 256) out of a table of 256 and an
-// exponent, times the series of e^(r ln2 / 256) up to r^3 (the next term is below 2^-42.7).  n is what a product and a sum with
-// 1.5 2^52 leave in the lowest bits: nine operations of 64 bits, which take twice the time of others here (with a series up
-// to r^11 and no table twenty, 160 us in place of 104 for 960 rows of 151936 bf16 logits).
+// e^((x - m) / T) in 64 bits, to 2^-42 and up to a factor near one that all x of one m share (exp_of(m), which is not quite one): with x / T
+// log2 e = (N + n + r) / 256, |r| <= 1/2, N a whole number near m / T 256 log2 e, it is 2^(n / 256) out of a table of 256 and an exponent, times
+// the series of e^(r ln2 / 256) up to r^3 (the next term is below 2^-42.7).  n is what a product and a sum with 1.5 2^52 - N leave in the
+// lowest bits, r is exact: eight operations of 64 bits, which issue like others, and four others (960 rows of 151936 bf16 logits: with a
+// series up to r^11 and no table, twenty operations, 160 us; with x - m formed first and the exponent cut out of n 104 to 112; so 91).
 constexpr int EXP_STEPS = 256;
 constexpr double FAR_STEPS = 400. * EXP_STEPS;
 struct ExpTable {
-  double v[EXP_STEPS];
+  double v[EXP_STEPS];  // 2^(i / 256), and i 2^12 off its upper half, where n 2^12 is added whose multiples of 256 are the exponent
   constexpr ExpTable() : v() {
     for (int i = 0; i < EXP_STEPS; ++i) {
       double x = 0.69314718055994531 * i / EXP_STEPS, term = 1., sum = 1.;
@@ -59,7 +60,7 @@ struct ExpTable {
         term = term * x / k;
         sum += term;
       }
-      v[i] = sum;
+      v[i] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, sum) - ((uint64_t)i << 44));
     }
   }
 };
@@ -67,29 +68,30 @@ __device__ constexpr ExpTable EXP_TABLE{};
 
 // What the logits of a row (or of a chunk) are measured by: a large one of them, m (finite), and the temperature.  Logits so far below it that
 // e^.. is below 2^-400 count as lying there; none is as far above it.  (Where the temperature is so low that the next smaller number than m does, it is taken to be as
-// high as that allows, which is the same.)
+// high as that allows, which is the same.  m / T 256 log2 e is below 2^41 by that.)
 __device__ __forceinline__ double steps_per(float T) { return EXP_STEPS * LOG2E / (double)T; }
 struct ExpBase {
-  double m, c;
+  double c, bias;
   float least;
-  __device__ __forceinline__ ExpBase(float top, float T, double steps) : m(top), c(steps) {
-    constexpr double FAR = FAR_STEPS;
+  __device__ __forceinline__ ExpBase(float top, float T, double steps) : c(steps) {
+    constexpr double FAR = FAR_STEPS, MAGIC = 6755399441055744.;
     least = fmaxf(top - T * (float)(FAR / (EXP_STEPS * LOG2E)), -3.4028234663852886e38f);
     if (!(least < top)) {
       const uint32_t b = __float_as_uint(top);
       least = __uint_as_float(top > 0.f ? b - 1 : top < 0.f ? b + 1 : 0x80000001u);
-      c = fmin(c, FAR / (m - (double)least));
+      c = fmin(c, FAR / ((double)top - (double)least));
     }
+    bias = MAGIC - rint((double)top * c);
   }
   __device__ __forceinline__ ExpBase(float top, float T) : ExpBase(top, T, steps_per(T)) {}
 };
 __device__ __forceinline__ void exp_parts(float x, const ExpBase& b, const double* table, double& power, double& series) {
-  constexpr double MAGIC = 6755399441055744., L = 0.69314718055994531 / EXP_STEPS;
-  x = !(x < b.least) ? x : b.least;  // (a NaN stays one)
-  const double d = (double)x - b.m, t = __builtin_fma(d, b.c, MAGIC), r = __builtin_fma(d, b.c, MAGIC - t);
-  const int n = (int)(uint32_t)(uint64_t)__double_as_longlong(t);
-  const double v = table[n & (EXP_STEPS - 1)];
-  power = __hiloint2double((int)((uint32_t)__double2hiint(v) + ((uint32_t)(n >> 8) << 20)), __double2loint(v));
+  constexpr double L = 0.69314718055994531 / EXP_STEPS;
+  x = __builtin_elementwise_maximum(x, b.least);  // (a NaN stays one)
+  const double t = __builtin_fma((double)x, b.c, b.bias), r = __builtin_fma((double)x, b.c, b.bias - t);
+  const uint32_t n = (uint32_t)(uint64_t)__double_as_longlong(t);
+  const double v = table[n % EXP_STEPS];
+  power = __hiloint2double((int)((uint32_t)__double2hiint(v) + (n << 12)), __double2loint(v));
   series = __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, L * L * L / 6., L * L / 2.), L), 1.);
 }
 __device__ __forceinline__ double exp_of(float x, const ExpBase& b, const double* table) {
@@ -166,8 +168,8 @@ __device__ __forceinline__ double wave_scan(double v, int lane) {
   return v;
 }
 
-// A wave per chunk, the next sixteen elements of a lane on their way during the work on these.  Bound: the logits' bytes where they are fp32, the
-// instructions (nine of 64 bits and six others for an exponential) where they have sixteen bits.
+// A wave per chunk, the next sixteen elements of a lane on their way during the work on these.  Bound: the logits' bytes where they are fp32 (176 rows
+// of 151936 17 us, 6.2 TB/s), the instructions where they have sixteen bits (960 rows 91 us: 17 of them for each 64 exponentials, 80% of the issue slots).
 template <int DT>
 __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   __shared__ double table[EXP_STEPS];
@@ -204,8 +206,9 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
       for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
       if (__any(top > m + far)) {  // (the first time, and where logits run away)
         const float mn = wave_max(top);
+        const ExpBase before = base;
         base = ExpBase(mn, T, steps);
-        if (m > -INFINITY) sum *= exp_of(m, base, table);
+        if (m > -INFINITY) sum *= exp_of(m, base, table) / exp_of(m, before, table);
         m = mn;
       }
       if (m > -INFINITY) {
@@ -230,6 +233,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
       if (piece + 2 >= pieces) break;
     }
     sum = wave_add(sum);
+    if (m > -INFINITY) sum /= exp_of(m, base, table);
   } else {
     while (true) {
       float top = x[0];
