@@ -322,14 +322,18 @@ class Pages:
         scales = [torch.empty(shape[:-1], dtype=torch.float32, device=device) if dtype in (torch.int8, torch.float8_e4m3fn) else None for _ in range(2)]
         return cls(k, v, *scales)
 
-    def _table(self, tables, name="tables", heads=False):
-        *of, m = tables.shape or (0,)
-        n = of[0] if of else 0
-        if heads and len(of) == 2 and of[1] == self.n_kv_heads:   # (a table for every kv head)
-            n, of = n * of[1], of[:1]
-        if tables.dtype != self._i32 or len(of) != 1 or tables.device != self.device or not tables.is_contiguous():
+    def _table(self, tables, name="tables"):
+        if tables.dtype != self._i32 or tables.dim() != 2 or tables.device != self.device or not tables.is_contiguous():
             _bad(f"{name}: contiguous int32 [sequences, pages] on {self.device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
+        n, m = tables.shape
         return NncPageTable(tables.data_ptr() or None, n, m)
+
+    def _tables_of_heads(self, tables):
+        if (tables.dtype != self._i32 or tables.dim() != 3 or tables.shape[1] != self.n_kv_heads or tables.device != self.device
+                or not tables.is_contiguous()):
+            _bad(f"tables: contiguous int32 [sequences, {self.n_kv_heads}, pages] on {self.device} expected, not {tables.dtype} {list(tables.shape)} on {tables.device}")
+        n, heads, m = tables.shape
+        return NncPageTable(tables.data_ptr() or None, n * heads, m)
 
     def _index(self, x, n, name):
         """seq or pos of n rows: (pointer, 0) of a tensor, (None, value) of a number."""
@@ -428,7 +432,8 @@ class Pages:
 
     def attention_workspace(self, q, tables, lens, max_len: int = 0, window: int = 0) -> int:
         """Bytes of workspace of the same call of `attention`."""
-        table, heads = self._table(tables, heads=True), tables.dim() == 3
+        heads = tables.dim() == 3
+        table = self._tables_of_heads(tables) if heads else self._table(tables)
         query = self._query(q, q.shape[0] if heads else table.n_seqs, lens, max_len, None, window, None, heads)
         if heads:
             n = ctypes.c_size_t()
@@ -458,9 +463,7 @@ class Pages:
         return out
 
     def _attention_picked(self, layer, q, tables, lens, max_len, scale, window, out, workspace):
-        if tables.shape[1] != self.n_kv_heads:
-            _bad(f"tables: [sequences, {self.n_kv_heads}, pages] expected, not {list(tables.shape)}")
-        L, table = lib(), self._table(tables, heads=True)
+        L, table = lib(), self._tables_of_heads(tables)
         query = self._query(q, tables.shape[0], lens, max_len, scale, window, out, True)
         kept, at, size = self._workspace(workspace, L.nnc_page_attention_picked_workspace, self._desc, ctypes.byref(table), ctypes.byref(query))
         _enqueue(self.device, L.nnc_page_attention_picked, self._desc, self._layer(layer), ctypes.byref(table), ctypes.byref(query), at, size)
