@@ -530,7 +530,7 @@ class Pages:
             out = self.torch.empty_like(q, memory_format=self.torch.contiguous_format)
         table, query, share = self._share(q, tables, lens, prefix, max_len, max_own, scale, out)
         layer = self._layer(layer)
-        if not table.n_seqs:
+        if not (table.n_seqs and share.width):
             return out
         kept, at, size = self._workspace(workspace, L.nnc_page_attention_shared_workspace, self._desc, ctypes.byref(table), ctypes.byref(query), ctypes.byref(share))
         _enqueue(self.device, L.nnc_page_attention_shared, self._desc, layer, ctypes.byref(table), ctypes.byref(query), ctypes.byref(share), at, size)

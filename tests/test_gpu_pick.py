@@ -275,6 +275,27 @@ def test_picked_attention_that_is_split(nnc):
             check_row(p, got[i, h * 4:h * 4 + 4], qq[i, h * 4:h * 4 + 4], k[tb[i, h][pos // 16], h, pos % 16], v[tb[i, h][pos // 16], h, pos % 16], "bf16", (i, h))
 
 
+def test_offsets_past_32_bits(nnc):
+    """A pool whose last pages and whose bounds of them start beyond 2^32 bytes."""
+    pages = 2200000
+    p = nnc.Pages.empty(1, pages, 1, 16, 64, torch.float16, DEV)
+    tables = ints(pages - 1 - np.arange(60).reshape(2, 30))
+    for i in range(2):
+        p.append(0, *[torch.randn((30, 16, 64), device=DEV) for _ in range(2)], tables, i, 0)
+    bounds, q, ln = p.empty_bounds(), queries((2, 32, 64), "f16"), ints([30, 27])
+    p.bound(0, bounds, tables, ln)
+    small = nnc.Pages(p.k[:, -60:].clone(), p.v[:, -60:].clone())
+    few, near = small.empty_bounds(), tables - (pages - 60)
+    small.bound(0, few, near, ln)
+    assert (pages - 60) * 16 * 64 * 2 > 2 ** 32
+    for b, want in zip(bounds, few):
+        assert torch.equal(b[0, pages - 60 + 3:], want[0, 3:])           # (the pages behind a sequence's end are left as they were)
+    t, n = p.pick(0, bounds, q, tables, ln, 9)
+    t2, n2 = small.pick(0, few, q, near, ln, 9)
+    assert torch.equal(t - (pages - 60), t2) and torch.equal(n, n2)
+    assert torch.equal(p.attention(0, q, t, n), small.attention(0, q, t2, n2))
+
+
 def test_a_run_of_steps_in_a_graph(nnc):
     """Append, bounds of the new row's page, picks and attention, captured once and replayed as the sequences grow."""
     lens = [100, 37]

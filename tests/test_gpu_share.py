@@ -127,12 +127,34 @@ def test_wrong_lengths_and_missing_pages_are_nan(nnc, store):
     assert torch.isfinite(out[0, 2]).all()
 
 
+@pytest.mark.parametrize("store,rows,heads,group,dim", [("bf16", "bf16", 2, 2, 128), ("f16", "f32", 1, 5, 64), ("e4m3", "bf16", 1, 3, 128), ("f32", "f32", 1, 12, 128), ("f32", "bf16", 3, 7, 64)])
+def test_few_rows_with_long_contexts_of_their_own(nnc, store, rows, heads, group, dim):
+    """Up to sixteen rows, and fp32: one walk over the shared positions and each sequence's, which a workgroup's share may begin or end in;
+    sequences whose heads lie in two workgroups; far fewer positions than the call allows, so that most workgroups have none."""
+    lens = [[700, 650, 1300], [3, 0, 640]]
+    s = Shared(nnc, store, lens, [650, 600], 16, heads, dim)
+    q = queries((2, 3, heads * group, dim), rows)
+    out = s.run(q)
+    s.check(q, out, rows)
+    assert torch.equal(out, s.run(q))
+    wide = torch.full((6, 4096), -1, dtype=torch.int32, device=DEV)
+    wide[:, :s.tables.shape[1]] = s.tables
+    assert s.p.attention_shared_workspace(q, wide, s.lens_t, s.prefix_t) > 0
+    s.check(q, s.p.attention_shared(1, q, wide, s.lens_t, s.prefix_t), rows)
+    assert s.p.attention_shared_workspace(q, s.tables, s.lens_t, s.prefix_t, max_len=1300, max_own=0) > 0
+    short = torch.minimum(s.lens_t, s.prefix_t[:, None]).contiguous()     # nobody behind the prefix
+    got = s.p.attention_shared(1, q, s.tables, short, s.prefix_t, max_own=0)
+    assert torch.isfinite(got).all() and not torch.equal(got[0, 2], out[0, 2])
+
+
 def test_no_rows_and_one_row(nnc):
     s = Shared(nnc, "bf16", [[20]], [20], 16, 2, 64)
     q = queries((1, 1, 4, 64), "bf16")
     s.check(q, s.run(q, max_own=0), "bf16")
     assert s.p.attention_shared(1, q[:0], s.tables[:0], s.lens_t[:0], s.prefix_t[:0]).shape == (0, 1, 4, 64)
     assert s.p.attention_shared_workspace(q, s.tables, s.lens_t, s.prefix_t, max_len=20, max_own=0) == 0
+    for tables, prefix in ((s.tables[:0], s.prefix_t), (s.tables, None)):                  # a group without rows
+        assert s.p.attention_shared(1, q[:, :0], tables, s.lens_t[:, :0].contiguous(), prefix).shape == (1, 0, 4, 64)
 
 
 @pytest.mark.parametrize("rows", list(pu.ROWS))

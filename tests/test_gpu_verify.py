@@ -118,6 +118,23 @@ def test_forbidden_tokens_and_far_logits(nnc, rows, v):
             check(nnc, ((target.float() / 8).clamp(-1, 1) * offset).to(target.dtype), drafts, u, draft, temperature=abs(offset) / 4)
 
 
+@pytest.mark.parametrize("top", [3.0, -7.5, 0.0, 1e-40, 3.4e38, -3.4e38, 65504.0])
+def test_temperatures_so_low_that_only_equals_are_left(nnc, top):
+    """Three equal largest logits in three chunks share the probability; the next smaller number has next to none, however near it
+    is (but e^-290 and less is more than u = 0 asks for, so that the first token is picked there)."""
+    top = np.float32(top)
+    x = np.full(5000, np.nextafter(top, np.float32(-np.inf)), np.float32)
+    x[1000:2000] = np.float32(-3.4028235e38)
+    x[[70, 2500, 4999]] = top
+    logits = torch.from_numpy(x).to(DEV).expand(6, 1, 5000).contiguous()
+    u = torch.tensor([0.0, 0.32, 0.35, 0.65, 0.68, 1 - 2.0 ** -24], device=DEV)[:, None].contiguous()
+    none = torch.empty((6, 0), dtype=torch.int32, device=DEV)
+    step = float(top) - float(np.nextafter(top, np.float32(-np.inf)))
+    for t in (step / 300, step / 1e6, 1e-45):
+        if 0 < np.float32(t) and step / float(np.float32(t)) > 290:       # e^-290 of 5000 others: nothing beside three ones
+            assert nnc.draft_verify(logits, none, u, temperature=float(np.float32(t)))[0][:, 0].tolist() == [0, 70, 2500, 2500, 4999, 4999], t
+
+
 def test_equal_distributions_and_edges_of_the_random_numbers(nnc):
     """p = q: every draft is kept, whatever u; u = 0 keeps whatever has any probability; equal logits; a residual of nothing."""
     target, drafts, u, draft = inputs(4, 3, 777, "f32")
