@@ -27,8 +27,10 @@ def ints(x):
 
 def row_bound(p, rows, size, n, top):
     """How far a row of attention over n positions may be off, per unit of the largest |v| (top): an fp32 score of head_dim products by (dim + 8)
-    2^-24 of the sum of their magnitudes, size (twice: weight and normaliser), exponentials 2^-22, weights in pieces 2^-22, sums of n terms n 2^-24."""
-    return 2 * (p.head_dim + 8) * 2.0 ** -24 * size + 2.0 ** -21 + (n + 64) * 2.0 ** -24
+    2^-24 of the sum of their magnitudes, size (twice: weight and normaliser), exponentials 2^-22, weights in pieces 2^-22, sums of n terms n 2^-24.
+    With bf16 rows a weight is two pieces of bf16: the first leaves 2^-9 of it at most, the second 2^-9 of that, so that a sum of weighted values
+    is off by 2^-18 of the largest (of this bound, which is taken twice, half)."""
+    return 2 * (p.head_dim + 8) * 2.0 ** -24 * size + 2.0 ** -21 + (n + 64) * 2.0 ** -24 + (2.0 ** -19 if rows == "bf16" else 0)
 
 
 def check_row(p, got, q, k, v, rows, what):

@@ -231,9 +231,10 @@ def test_in_a_graph_on_another_stream_and_with_shared_workspaces(nnc):
 
 @pytest.mark.parametrize("store,rows", [("bf16", "bf16"), ("i8", "bf16"), ("e4m3", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("dim", [128, 64])
-def test_weights_are_as_good_as_fp32(nnc, store, rows, dim):
+def test_weights_where_sums_cancel(nnc, store, rows, dim):
     """Sums that cancel to 2^-13 of their terms, as for the attention of one row: every row of a group sees the same six rows, its scores
-    exact products, and what is left must be right to 2^-20 of the terms (binary16 pieces leave 2^-22 more out)."""
+    exact products, and what is left must be right to 2^-20 of the terms.  Two binary16 pieces of a weight leave 2^-22 more out (half a step, 2^-11,
+    of half a step), two pieces of bf16, with bf16 rows over 16- and 8-bit pools, 2^-18 (2^-9 of 2^-9)."""
     from test_gpu_pages_precision import cancelling
     rng = np.random.default_rng(11)
     n, width = 6, 40
@@ -260,7 +261,7 @@ def test_weights_are_as_good_as_fp32(nnc, store, rows, dim):
     w = np.exp(s - s.max())
     x = v * scale[:, None]
     want, size = (w @ x) / w.sum(), (w @ np.abs(x)) / w.sum()
-    bound = 2.0 ** -20 + (2.0 ** -22 if store == "f16" and rows == "f16" else 0)
+    bound = 2.0 ** -20 + (2.0 ** -22 if store == "f16" and rows == "f16" else 2.0 ** -18 if store != "f32" and rows == "bf16" else 0)
     tol = bound * size + pu.HALF_ULP[rows] * (np.abs(want) + bound * size) + (2.0 ** -25 if rows == "f16" else 0)
     err = np.abs(pu.f64(out)[0, :, 0] - want)
     assert (err <= tol).all(), float((err - tol).max())
