@@ -457,7 +457,8 @@ __device__ __forceinline__ void answer(const VerifyArgs& a, uint32_t i, int32_t 
 
 // Every workgroup of a sequence decides for itself (a few dozen numbers a row), and each of its waves adds r up over a chunk where that
 // takes the draft's probabilities off the target's.  Otherwise the sequence has one workgroup, which picks its token too.
-// Bound: few sequences the loads that wait for each other, many the 64-bit exponentials.
+// Bound: few sequences the loads that wait for each other (one of four drafts 8.5 us), many the 64-bit exponentials of p and q where
+// q is taken off (16 sequences of 151936 tokens 14.5 us, 64 27).
 template <int DT>
 __global__ __launch_bounds__(64 * JUDGE_WAVES) void k_draft_judge(VerifyArgs a) {
   constexpr int ROWS = 32;  // drafts that are judged at once
