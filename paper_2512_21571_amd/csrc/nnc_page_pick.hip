@@ -210,29 +210,42 @@ __device__ __forceinline__ uint64_t order_of(double x) {
   return (b >> 63) ? ~b : b | (1ull << 63);
 }
 
-// Sum over the LPR (8 or 16) neighbouring lanes of a page, in all of them: the same additions for every page.
-template <int LPR>
-__device__ __forceinline__ double lanes_sum(double v) {
-  auto get = [](double x, auto ctrl) __attribute__((always_inline)) {
-    const uint64_t b = (uint64_t)__double_as_longlong(x);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, decltype(ctrl)::value, 0xf, 0xf, true);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), decltype(ctrl)::value, 0xf, 0xf, true);
-    return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp64(uint64_t b) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+  return ((uint64_t)hi << 32) | lo;
+}
+// Sums of N numbers over LPR (8 or 16) neighbouring lanes, BIT lanes apart first: of two numbers a lane keeps the one that its bit names and gives
+// the other away, so that in the end lane l has number l / (LPR / N) (N < LPR: so have its neighbours), or the 2 l'th and the next one.  The partner
+// that a mirror gives differs in the lower bits too, which say nothing yet.  The same additions for every number, but for their sides.
+template <int BIT, int N>
+__device__ __forceinline__ void lanes_sum(double (&v)[N], int lane) {
+  constexpr int CTRL = BIT == 8 ? DPP_ROW_MIRROR : BIT == 4 ? DPP_ROW_HALF_MIRROR : BIT == 2 ? DPP_QUAD_XOR2 : DPP_QUAD_XOR1;
+  auto get = [](double x) __attribute__((always_inline)) {
+    return __longlong_as_double((long long)dpp64<CTRL>((uint64_t)__double_as_longlong(x)));
   };
-  v += get(v, std::integral_constant<int, DPP_QUAD_XOR1>{});
-  v += get(v, std::integral_constant<int, DPP_QUAD_XOR2>{});
-  v += get(v, std::integral_constant<int, DPP_ROW_HALF_MIRROR>{});
-  if constexpr (LPR == 16) v += get(v, std::integral_constant<int, DPP_ROW_MIRROR>{});
-  return v;
+  if constexpr (N == 1) {
+    v[0] += get(v[0]);
+    if constexpr (BIT > 1) lanes_sum<BIT / 2>(v, lane);
+  } else {
+    double half[N / 2];
+    const bool upper = lane & BIT;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) half[i] = (upper ? v[i + N / 2] : v[i]) + get(upper ? v[i] : v[i + N / 2]);
+    if constexpr (BIT > 1) lanes_sum<BIT / 2>(half, lane);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = half[i];
+  }
 }
 
 // Scores of the pages of a sequence for one kv head, in 64 bits: pages whose scores lie close are told apart as the definition does
 // (a sum of 128 products of fp32 is off by 2^-20 of its terms, and of 8192 pages several lie closer than that to the last one picked).
 // LPR lanes a page, eight dims each, LOADS pages of them on their way at once; max(q lo, q hi) is q hi for a positive and q lo for a
 // negative q, so that a product with both parts of q is all there is to do, HG query heads at a time.
-// Bound: the 64-bit products and their sums over lanes, 1.8 us for each query head behind 5 us of launch and loads (8192 pages, 8 kv heads, bf16,
-// 33.5 MB: 7.0 us for one query head, 13.3 for four, 20.3 for eight).  Two or eight pages on their way 14.1 and 18.6 us, two heads at a time
-// in place of four 13.3 at half the registers.
+// Bound: loads that wait for each other (length, table, bounds) and then the 64-bit products, 1.7 us for each query head (8192 pages, 8 kv heads,
+// bf16, 33.5 MB: 7.1 us for one query head, 12.8 for four, 18.7 for eight; with every sum on its own through all lanes 7.6, 13.4, 20.3).  Two or
+// eight pages on their way 14.1 and 18.6 us for four heads, two heads at a time in place of four no less at two thirds of the registers.
 template <int DT, int D, int HG>
 __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* keys) {
   constexpr int LPR = D / 8, PER = 64 / LPR, LOADS = 4, WORDS = DT == DT_F32 ? 2 : 1;
@@ -256,13 +269,8 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
       wh[j][i] = *reinterpret_cast<const u32x4_v*>(static_cast<const char*>(a.hi) + at + i * 16);
     }
   }
-  double best[LOADS];
-  bool nan[LOADS];
-#pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    best[j] = -INFINITY;
-    nan[j] = (uint32_t)page[j] >= a.p.n_pages;
-  }
+  constexpr int N = LOADS * HG, LEFT = N > LPR ? N / LPR : 1;
+  uint64_t best = 0;  // of this lane's page, number lane % LPR / (LPR / LOADS) of the four
   auto value = [](const u32x4_v (&w)[WORDS], int i) __attribute__((always_inline)) {
     if constexpr (DT == DT_F32) return __uint_as_float(w[i / 4][i % 4]);
     else if constexpr (DT == DT_BF16) return i & 1 ? Bf16::hi(w[0][i / 2]) : Bf16::lo(w[0][i / 2]);
@@ -284,6 +292,7 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
         down[h][i] = q[i] > 0.f ? 0. : (double)q[i];
       }
     }
+    double sums[N];
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       // (converted anew for every group of heads: as 64-bit numbers the bounds would take all registers)
@@ -291,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
       for (int i = 0; i < WORDS; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) asm("" : "+v"(wl[j][i][e]), "+v"(wh[j][i][e]));
-      double s[HG];
+      double* s = sums + j * HG;
 #pragma unroll
       for (int h = 0; h < HG; ++h) s[h] = 0.;
 #pragma unroll
@@ -300,19 +309,20 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
 #pragma unroll
         for (int h = 0; h < HG; ++h) s[h] = __builtin_fma(down[h][i], lo, __builtin_fma(up[h][i], hi, s[h]));
       }
-#pragma unroll
-      for (int h = 0; h < HG; ++h) {
-        s[h] = lanes_sum<LPR>(s[h]);
-        nan[j] |= s[h] != s[h];
-        best[j] = s[h] > best[j] ? s[h] : best[j];
-      }
     }
-  }
+    lanes_sum<LPR / 2>(sums, lane);
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const uint32_t block = first + j * PER + lane / LPR;
-    if (lane % LPR == 0 && block < blocks) keys[((size_t)seq * a.p.n_kv_heads + kvh) * a.blocks + block] = nan[j] ? ORDER_NAN : order_of(best[j]);
+    for (int i = 0; i < LEFT; ++i) best = max(best, order_of(sums[i]));
   }
+  best = max(best, dpp64<DPP_QUAD_XOR1>(best));
+  if constexpr (LPR == 16) best = max(best, dpp64<DPP_QUAD_XOR2>(best));
+  const int mine = lane % LPR / (LPR / LOADS);
+  bool gone = false;
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j)
+    if (j == mine) gone = (uint32_t)page[j] >= a.p.n_pages;
+  const uint32_t block = first + mine * PER + lane / LPR;
+  if (lane % (LPR / LOADS) == 0 && block < blocks) keys[((size_t)seq * a.p.n_kv_heads + kvh) * a.blocks + block] = gone ? ORDER_NAN : best;
 }
 
 // ---- the best --------------------------------------------------------------------------------------------------
