@@ -153,7 +153,7 @@ def pool_for(nnc, store, pages, tokens, heads, dim):
 
 @pytest.mark.parametrize("store", list(pu.STORES))
 @pytest.mark.parametrize("rows", list(pu.ROWS))
-@pytest.mark.parametrize("heads,group,dim,tokens", [(2, 4, 128, 16), (3, 1, 64, 7), (1, 16, 128, 1), (2, 5, 64, 24)])
+@pytest.mark.parametrize("heads,group,dim,tokens", [(2, 4, 128, 16), (3, 1, 64, 7), (1, 16, 128, 1), (2, 5, 64, 24), (1, 2, 128, 16), (2, 2, 64, 24), (1, 1, 128, 5), (3, 3, 128, 16)])
 def test_pick(nnc, store, rows, heads, group, dim, tokens):
     lens = [0, 1, tokens, 3 * tokens, 7 * tokens - (tokens > 1), 40 * tokens, 41 * tokens - tokens // 2]
     p = pool_for(nnc, store, 300, tokens, heads, dim)
