@@ -331,7 +331,8 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
 // highest bit in which two keys differ) until few keys are left, which are ranked; then the pages above it and, lowest
 // first, as many equal to it as fit, in order.  R: keys that a thread keeps in registers, key i of it page 1024 i + thread; 0: more
 // pages, which are read again for every digit.  Bound: latency, of the passes and of the barriers between them
-// (8192 pages 10.5 us, 512 pages 5.5).
+// (8192 pages 10.5 us, 512 pages 5.5).  With 16 keys a thread 12.6 and 9.2, read again for every digit 18.9 and 7.3; 16384 pages with 16 keys
+// 16.2 and 41.9, 31250, which no registers hold, 65.5.
 template <int R>
 __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* all) {
   constexpr uint32_t FEW = 64;

@@ -1,7 +1,7 @@
 // Attention of rows that share the first positions of their contexts: a batch behind one prompt, the beams of a search, the new
 // tokens of one sequence.  The shared positions are read once for up to 128 rows (sequences x query heads of a kv head), whose
 // scores and weighted sums are matrix products with all of them; what a row has behind the prefix follows in the same walk (up to
-// sixteen rows) or is a walk of its own, and the records are joined.  Bound: few rows the cache's bytes, many rows the vector instructions of the softmax.
+// sixteen rows, and fp32) or is a walk of its own, and the records are joined.  Bound: few rows the cache's bytes, many rows the vector instructions of the softmax.
 #include "nnc_page_attn.h"
 
 namespace nnc {
@@ -931,6 +931,10 @@ static bool own_type(const PagePool& p, const PageAttn& a) {
 // 64 values fill a tile of 64 positions with the loads of four.)
 static constexpr int most_tiles(int store, int dim, bool full) { return full || (page_scaled(store) && dim == 64) ? 4 : 8; }
 
+// Rows of a workgroup: the fewest that all of a group's fit in, in 32, 64 or 128 (16384 positions of one group, 8 kv heads, bf16, us of the
+// walk with 32 / 64 / 128: 16 rows 16.3 / 18.0 / 21.8, 40 21.3 / 18.9 / 22.5, 64 21.7 / 20.0 / 23.2, 128 34.8 / 28.0 / 26.0, 256 61.0 / 47.1 / 38.1).
+// Sixteen rows with positions of their own keep to the other kernel, whose one launch takes those too (without any: 1024 positions 11.0 us
+// there and 7.4 here, 16384 20.5 and 16.3, int8 and fp32 queries 8192 14.3 and 13.0; but the walk of a few own positions is 4.8 us and a launch).
 // Workgroups along the positions: as many as fill the chip (two on a CU).  Up to sixteen rows (sequences x query heads of a kv head), and fp32,
 // walk what is behind the prefix in the same launch, evenly shared out whatever the lengths are, and up to 512 positions one workgroup
 // takes them all, which saves the join (8 kv heads of two query heads, four rows, 304 positions and up to 16 of their own, bf16: 14.8 us by one
@@ -942,9 +946,9 @@ static constexpr int most_tiles(int store, int dim, bool full) { return full || 
 PageSharePlan plan_page_share(const PagePool& p, const PageAttn& a, const PageShare& s, uint32_t max_slots) {
   const uint32_t G = a.n_q_heads / p.n_kv_heads, groups = s.width ? s.n_rows / s.width : 0, rows = s.width * G;
   PageSharePlan pl{};
-  pl.tiles = p.store == PS_F32 || rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : most_tiles(p.store, p.head_dim, !own_type(p, a));
-  const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)groups * p.n_kv_heads * ((rows + 16 * pl.tiles - 1) / (16 * pl.tiles)));
   const bool own = s.prefix && s.max_own;
+  pl.tiles = p.store == PS_F32 || (own && rows <= 16) ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : most_tiles(p.store, p.head_dim, !own_type(p, a));
+  const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)groups * p.n_kv_heads * ((rows + 16 * pl.tiles - 1) / (16 * pl.tiles)));
   pl.own.chunk = 1;  // (the join divides by it)
   uint64_t span = a.max_len;
   if (own && pl.tiles == 1) {
