@@ -23,7 +23,7 @@ constexpr int JUDGE_WAVES = 16;
 
 struct ChunkSum {
   double sum;     // of e^((x - top) / T)
-  float top;      // a large element (T = 0: the largest); NaN: the chunk holds one
+  float top;      // the largest element; NaN: the chunk holds one
   uint32_t best;  // T = 0: the first element that is `top`
 };
 struct Verdict {  // of a sequence
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
     __syncthreads();
   }
   if (!work) return;
-  float m = -INFINITY;
+  float m = -INFINITY, high = -INFINITY;  // what exponentials are measured by; the largest so far, by lane, which may be up to `far` beyond it
   uint32_t best = 0;
   double sum = 0.;
   bool nan = false;
@@ -208,9 +208,14 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
         const float mn = wave_max(top);
         const ExpBase before = base;
         base = ExpBase(mn, T, steps);
-        if (m > -INFINITY) sum *= exp_of(m, base, table) / exp_of(m, before, table);
+        // (by the largest so far, whose exponential is what the sum is about: by m, whose exponential ends at 2^-400, a sum of 2^400 would become 1)
+        if (m > -INFINITY) {
+          const float h = wave_max(high);
+          sum *= exp_of(h, base, table) / exp_of(h, before, table);
+        }
         m = mn;
       }
+      high = fmaxf(high, top);
       if (m > -INFINITY) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -233,7 +238,11 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
       if (piece + 2 >= pieces) break;
     }
     sum = wave_add(sum);
-    if (m > -INFINITY) sum /= exp_of(m, base, table);
+    if (m > -INFINITY) {  // sums of different chunks meet by the largest element of each: they are 1 or more, what is far below is nothing
+      high = wave_max(high);
+      sum /= exp_of(high, base, table);
+      m = high;
+    }
   } else {
     while (true) {
       float top = x[0];

@@ -1,0 +1,103 @@
+"""Verification of drafts at temperatures near zero, where a row's chunks have several pieces, and where logits run away along a row,
+against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import page_util as pu
+import share_util as su
+from share_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nnc():
+    from paper_2512_21571_amd import binding
+    binding.lib()
+    return binding
+
+
+def drawn(x, t, u):
+    """One token of softmax(x / t) for a random number."""
+    sums = np.cumsum(su.softmax(x, t))
+    return int(np.searchsorted(sums, u * sums[-1], side="right"))
+
+
+def inputs(n, k, v, rows, t, seed, size=2.5):
+    """Drafts drawn at the temperature itself; targets that equal the draft's logits, differ from them by about the temperature (so that
+    a draft may be kept or not), or by more."""
+    rng = np.random.default_rng(seed)
+    draft = torch.from_numpy(rng.standard_normal((n, k, v), dtype=np.float32) * np.float32(size)).to(pu.ROWS[rows])
+    target = torch.from_numpy(rng.standard_normal((n, k + 1, v), dtype=np.float32) * np.float32(size)).to(pu.ROWS[rows])
+    for i in range(n):
+        noise = torch.from_numpy(rng.standard_normal((k, v), dtype=np.float32))
+        target[i, :k] = (draft[i].float() + noise * (0.0, t, 0.5)[i % 3]).to(pu.ROWS[rows])
+    u = rng.random((n, k + 1)).astype(np.float32).clip(0, 1 - 2.0 ** -24)
+    drafts = np.array([[drawn(pu.f64(draft[i, j]), float(np.float32(t)), rng.random()) for j in range(k)] for i in range(n)], np.int32).reshape(n, k)
+    return target, drafts, u, draft
+
+
+def margin(logits, drafts, u, draft_logits, t):
+    """How far the decisions of a call are from their borders.  p and q are good to 2^-41 of themselves (exponentials 2^-42 each way), so u q < p is
+    certain beyond 2^-40 of the larger side, and a running sum of max(p - q, 0), whose terms are off by 2^-41 (p + q), beyond 2^-39."""
+    n, rows, _ = logits.shape
+    near = 1.0
+    for i in range(n):
+        for j in range(rows):
+            r = p = su.softmax(logits[i, j], t)
+            if j < rows - 1:
+                x = int(drafts[i, j])
+                q = su.softmax(draft_logits[i, j], t) if draft_logits is not None else (np.arange(len(p)) == x).astype(np.float64)
+                a, b = float(u[i, j]) * q[x], p[x]
+                if max(a, b) > 0:
+                    near = min(near, abs(a - b) / max(a, b))
+                if a < b:
+                    continue
+                r = np.maximum(p - q, 0)
+                r = r if r.sum() > 0 else p
+            sums = np.cumsum(r)
+            near = min(near, np.abs(sums[:-1][r[1:] > 0] - float(u[i, -1]) * sums[-1]).min(initial=1.0))
+            break
+    return near
+
+
+def check(nnc, target, drafts, u, draft, t):
+    t = float(np.float32(t))
+    dev = [torch.from_numpy(x).to(DEV) for x in (drafts, u)]
+    heat = [np.float32(t)] * len(u)
+    x, y = pu.f64(target), None if draft is None else pu.f64(draft)
+    assert margin(x, drafts, u, y, t) > 2.0 ** -39
+    want = su.verify(x, drafts, u.astype(np.float64), y, None, heat)
+    got = nnc.draft_verify(target.to(DEV), *dev, None if draft is None else draft.to(DEV), temperature=t)
+    assert np.array_equal(got[1].cpu().numpy(), want[1]) and np.array_equal(got[0].cpu().numpy(), want[0]), (t, draft is None)
+    return want
+
+
+# (pieces of 1024 a chunk: 1, 2, 3 and 4)
+LOW = [shape + (t,) for t in (0.001, 0.005, 0.01, 0.05)
+       for shape in ((2, 4, 151936, "f32"), (1, 4, 300001, "bf16"), (16, 5, 151936, "f32"), (64, 7, 35001, "f16"), (40, 3, 100003, "f32"))]
+
+
+@pytest.mark.parametrize("n,k,v,rows,t", LOW + [(64, 7, 151936, "bf16", 0.005)])
+def test_low_temperatures(nnc, n, k, v, rows, t):
+    target, drafts, u, draft = inputs(n, k, v, rows, t, seed=v + k)
+    check(nnc, target, drafts, u, draft, t)
+    best = pu.f64(target[:, :k]).argmax(-1).astype(np.int32)
+    check(nnc, target, best, u, None, t)
+
+
+@pytest.mark.parametrize("v", [5003, 300001])
+@pytest.mark.parametrize("t,step", [(1.0, 277.0), (1.0, 200.0), (1.0, 400.0), (1e-3, 0.3), (1e30, 2e32)])
+def test_logits_that_run_away(nnc, v, t, step):
+    """Logits that rise along the row by hundreds of temperatures, so that what was added up first is nothing beside what follows: 0, step,
+    2 step in places that are one chunk's or several's; p is on the last one, two equal ones share it."""
+    none = np.zeros((4, 0), np.int32)
+    u = np.array([[0.001], [0.4], [0.6], [0.999]], np.float32)
+    for places in ((3, 1030, 2900), (100, 1023, 1024), (10, 20, 2047), (v // 2, v // 2 + 1200, v - 1), (5, v - 2, v - 1)):
+        for last in (2.0, 1.0):
+            x = np.zeros((4, 1, v), np.float32)
+            x[..., places[1]] = step
+            x[..., places[2]] = step * last
+            want = check(nnc, torch.from_numpy(x), none, u, None, t)
+            assert (want[0][:, 0] == (places[2] if last == 2 else np.array([places[1]] * 2 + [places[2]] * 2))).all()
