@@ -68,18 +68,20 @@ __device__ constexpr ExpTable EXP_TABLE{};
 
 // What the logits of a row (or of a chunk) are measured by: a large one of them, m (finite), and the temperature.  Logits so far below it that
 // e^.. is below 2^-400 count as lying there; none is as far above it.  (Where the temperature is so low that the next smaller number than m does, it is taken to be as
-// high as that allows, which is the same.  m / T 256 log2 e is below 2^41 by that.)
+// high as that allows, which is the same.  m / T 256 log2 e is below 2^41 by that.)  Where no finite number is that far below m, `least` is -infinity: the sum has to
+// leave out what is -infinity by itself.
 __device__ __forceinline__ double steps_per(float T) { return EXP_STEPS * LOG2E / (double)T; }
 struct ExpBase {
   double c, bias;
   float least;
   __device__ __forceinline__ ExpBase(float top, float T, double steps) : c(steps) {
     constexpr double FAR = FAR_STEPS, MAGIC = 6755399441055744.;
-    least = fmaxf(top - T * (float)(FAR / (EXP_STEPS * LOG2E)), -3.4028234663852886e38f);
+    least = top - T * (float)(FAR / (EXP_STEPS * LOG2E));
     if (!(least < top)) {
       const uint32_t b = __float_as_uint(top);
       least = __uint_as_float(top > 0.f ? b - 1 : top < 0.f ? b + 1 : 0x80000001u);
-      c = fmin(c, FAR / ((double)top - (double)least));
+      // (-infinity behind the lowest number, from which the next one is 2^104 away)
+      c = fmin(c, FAR / (least > -INFINITY ? (double)top - (double)least : 0x1p104));
     }
     bias = MAGIC - rint((double)top * c);
   }
@@ -145,12 +147,16 @@ __device__ __forceinline__ const void* row_of(const VerifyArgs& a, bool draft, u
   return p;
 }
 template <int DT>
-__device__ __forceinline__ float logit_of(const VerifyArgs& a, bool draft, uint32_t i, uint32_t j, uint32_t x) {
-  bool wide;
-  const void* row = row_of<DT>(a, draft, i, j, wide);
+__device__ __forceinline__ float element(const void* row, uint32_t x) {
   if constexpr (DT == DT_F32) return static_cast<const float*>(row)[x];
   else if constexpr (DT == DT_BF16) return Bf16::widen(static_cast<const uint16_t*>(row)[x]);
   else return Fp16::widen(static_cast<const uint16_t*>(row)[x]);
+}
+template <int DT>
+__device__ __forceinline__ float logit_of(const VerifyArgs& a, bool draft, uint32_t i, uint32_t j, uint32_t x) {
+  bool wide;
+  const void* row = row_of<DT>(a, draft, i, j, wide);
+  return element<DT>(row, x);
 }
 
 __device__ __forceinline__ double wave_add(double v) {
@@ -173,7 +179,7 @@ __device__ __forceinline__ double wave_scan(double v, int lane) {
 template <int DT>
 __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   __shared__ double table[EXP_STEPS];
-  const uint32_t n_target = a.v.n * (a.v.k + 1), row = blockIdx.y, chunk = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t n_target = a.v.n * (a.v.k + 1), row = blockIdx.y, chunk = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const bool draft = row >= n_target;
   const uint32_t per = draft ? a.v.k : a.v.k + 1, of = draft ? row - n_target : row, i = of / per, j = of - i * per;
   const int count = count_of(a, i);
@@ -195,7 +201,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   float m = -INFINITY, high = -INFINITY;  // what exponentials are measured by; the largest so far, by lane, which may be up to `far` beyond it
   uint32_t best = 0;
   double sum = 0.;
-  bool nan = false;
+  bool nan = false, again = false;  // again: the sum has to leave out what is -infinity
   if (T > 0.f) {
     const double steps = steps_per(T);
     const float far = T * (float)(FAR_STEPS / (EXP_STEPS * LOG2E));
@@ -214,6 +220,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
           sum *= exp_of(h, base, table) / exp_of(h, before, table);
         }
         m = mn;
+        again |= base.least == -INFINITY;
       }
       high = fmaxf(high, top);
       if (m > -INFINITY) {
@@ -236,6 +243,12 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
       if (piece + 2 < pieces) load16<DT>(p, wide, (piece + 2) * CHUNK + lane * 16, a.v.vocab, x);
       add(y);
       if (piece + 2 >= pieces) break;
+    }
+    if (again) {  // (a loop of its own, behind the other: within it the case would cost registers, and of the six waves of a SIMD one or two)
+      base = ExpBase(wave_max(high), T);
+      sum = 0.;
+#pragma unroll 1
+      for (uint32_t at = chunk * a.mult * CHUNK + lane; at < min(pieces * CHUNK, a.v.vocab); at += 64) sum += probability(element<DT>(p, at), base, table, 1.);
     }
     sum = wave_add(sum);
     if (m > -INFINITY) {  // sums of different chunks meet by the largest element of each: they are 1 or more, what is far below is nothing

@@ -1,5 +1,7 @@
 """Verification of drafts at temperatures near zero, where a row's chunks have several pieces, and where logits run away along a row,
-against the definition in 64 bits."""
+and with logits at the end of their type, against the definition in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -9,6 +11,8 @@ import share_util as su
 from share_util import DEV
 
 pytestmark = pytest.mark.gpu
+
+LOWEST = float(torch.finfo(torch.float32).min)
 
 
 @pytest.fixture(scope="module")
@@ -101,3 +105,32 @@ def test_logits_that_run_away(nnc, v, t, step):
             x[..., places[2]] = step * last
             want = check(nnc, torch.from_numpy(x), none, u, None, t)
             assert (want[0][:, 0] == (places[2] if last == 2 else np.array([places[1]] * 2 + [places[2]] * 2))).all()
+
+
+@pytest.mark.parametrize("t", [0.0, 1e-45, 1e-3, 0.7, 1.0, 1.3, 1e30])
+@pytest.mark.parametrize("v,ids", [(5003, 900), (151936, 40000)])
+def test_chunks_of_nothing_but_the_lowest_number(nnc, v, ids, t):
+    """Everything from some id on masked by the type's lowest number, to the end of a row, alone and mixed with -infinity."""
+    target, drafts, u, draft = inputs(6, 2, v, "f32", t if t > 0.5 else 1.0, seed=v)
+    target[..., ids:], draft[..., ids:] = LOWEST, LOWEST
+    target[3:, :, v - 40:], draft[3:, :, ids + 1024:ids + 4000] = -math.inf, -math.inf
+    drafts = np.minimum(drafts, ids - 1)
+    if 0 < t < 0.5:                                                       # (what such a temperature leaves: the largest)
+        drafts = pu.f64(draft).argmax(-1).astype(np.int32)
+    check(nnc, target, drafts, u, draft, t)
+    check(nnc, target, drafts, u, None, t)
+    check(nnc, target[:, 2:], drafts[:, :0], u[:, 2:], None, t)
+
+
+@pytest.mark.parametrize("t", [0.0, 1e-45, 1.0])
+@pytest.mark.parametrize("v", [60, 1024, 5003])
+def test_rows_of_nothing_but_the_lowest_number(nnc, v, t):
+    """The lowest number is a logit like others: where there is no larger one it has all the probability, in equal parts."""
+    x = torch.full((5, 1, v), LOWEST)
+    x[1, :, ::2] = -math.inf
+    x[2, :, :v // 2] = -math.inf
+    x[3, :, 1:] = -math.inf
+    x[4, :, v // 3] = LOWEST * (1 - 2.0 ** -23)
+    u = np.array([[0.3], [0.51], [0.77], [0.9], [0.2]], np.float32)
+    want = check(nnc, x, np.zeros((5, 0), np.int32), u, None, t)
+    assert want[0][3, 0] == 0 and want[0][4, 0] == v // 3
