@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   bool nan = false, again = false;  // again: the sum has to leave out what is -infinity
   if (T > 0.f) {
     const double steps = steps_per(T);
-    const float far = T * (float)(FAR_STEPS / (EXP_STEPS * LOG2E));
+    const float far = fminf(T * (float)(FAR_STEPS / (EXP_STEPS * LOG2E)), 3.4028234663852886e38f);  // (-infinity and it are -infinity still)
     ExpBase base(0.f, T, steps);
     auto add = [&](const float (&x)[16]) __attribute__((always_inline)) {
       float top = x[0];

@@ -1,5 +1,5 @@
-"""Verification of drafts at temperatures near zero, where a row's chunks have several pieces, and where logits run away along a row,
-and with logits at the end of their type, against the definition in 64 bits."""
+"""Verification of drafts at temperatures near zero and near the largest number, where a row's chunks have several pieces, where logits run
+away along a row and where they lie at the end of their type, against the definition in 64 bits."""
 import math
 
 import numpy as np
@@ -107,7 +107,26 @@ def test_logits_that_run_away(nnc, v, t, step):
             assert (want[0][:, 0] == (places[2] if last == 2 else np.array([places[1]] * 2 + [places[2]] * 2))).all()
 
 
-@pytest.mark.parametrize("t", [0.0, 1e-45, 1e-3, 0.7, 1.0, 1.3, 1e30])
+@pytest.mark.parametrize("t", [1.2e36, 1.3e36, 1e37, 3.4028234e38])
+@pytest.mark.parametrize("n,k,v", [(3, 2, 777), (2, 3, 5003), (1, 2, 300001), (40, 3, 100003)])
+def test_high_temperatures(nnc, n, k, v, t):
+    """Every finite logit near the others, at most a few temperatures apart where logits are as large as the temperature; -infinity, and what lies
+    behind a row's end, has no probability however high the temperature is."""
+    target, drafts, u, draft = inputs(n, k, v, "f32", t, seed=v, size=1.0)
+    for scale in (1.0, 5e37):
+        x, y = (target * scale).clamp(-3e38, 3e38), (draft * scale).clamp(-3e38, 3e38)
+        check(nnc, x, drafts, u, y, t)
+        mask = torch.from_numpy(np.random.default_rng(v).random((n, k + 1, v)) < 0.5)
+        mask[:, :k] &= torch.from_numpy(np.arange(v) != drafts[..., None])
+        check(nnc, x.masked_fill(mask, -math.inf), drafts, u, None, t)
+        check(nnc, x.masked_fill(mask, -math.inf), drafts, u, y.masked_fill(mask[:, :k], -math.inf), t)
+        low = x.masked_fill(mask, LOWEST)
+        check(nnc, low, drafts, u, None, t)
+        low[:, :, v // 2:] = -math.inf
+        check(nnc, low, np.minimum(drafts, v // 2 - 1), u, None, t)
+
+
+@pytest.mark.parametrize("t", [0.0, 1e-45, 1e-3, 0.7, 1.0, 1.3, 1e30, 1e37])
 @pytest.mark.parametrize("v,ids", [(5003, 900), (151936, 40000)])
 def test_chunks_of_nothing_but_the_lowest_number(nnc, v, ids, t):
     """Everything from some id on masked by the type's lowest number, to the end of a row, alone and mixed with -infinity."""
@@ -122,7 +141,7 @@ def test_chunks_of_nothing_but_the_lowest_number(nnc, v, ids, t):
     check(nnc, target[:, 2:], drafts[:, :0], u[:, 2:], None, t)
 
 
-@pytest.mark.parametrize("t", [0.0, 1e-45, 1.0])
+@pytest.mark.parametrize("t", [0.0, 1e-45, 1.0, 1e37])
 @pytest.mark.parametrize("v", [60, 1024, 5003])
 def test_rows_of_nothing_but_the_lowest_number(nnc, v, t):
     """The lowest number is a logit like others: where there is no larger one it has all the probability, in equal parts."""
@@ -133,4 +152,4 @@ def test_rows_of_nothing_but_the_lowest_number(nnc, v, t):
     x[4, :, v // 3] = LOWEST * (1 - 2.0 ** -23)
     u = np.array([[0.3], [0.51], [0.77], [0.9], [0.2]], np.float32)
     want = check(nnc, x, np.zeros((5, 0), np.int32), u, None, t)
-    assert want[0][3, 0] == 0 and want[0][4, 0] == v // 3
+    assert want[0][3, 0] == 0 and (t > 1 or want[0][4, 0] == v // 3)
