@@ -622,6 +622,8 @@ typedef struct {
  *   was not kept (p_j itself if that is zero everywhere), and r = p_j of the row behind the last draft
  * tokens_out: the kept drafts, that token, and -1 behind it; accepted_out: how many were kept.  Sums, exponentials and comparisons are in
  * 64 bits (exponentials to 2^-42), and sums are taken in a fixed order: the same call gives the same tokens.  Rows behind a sequence's count are not looked at.
+ * A logit that lies 693 T (a factor of 2^-1000) or more below the largest of its row has the probability 0 in u_j q_j(x_j) < p_j(x_j) and in max(p_j - q_j, 0); in r = p_j it
+ * has next to none, which a u_k of exactly 0 does ask for: only -infinity forbids a token whatever the random numbers are.
  * A sequence whose count is none of 0 .. k or whose temperature is negative or not finite gives the token -1 and
  * keeps nothing; where a row that has to be looked at has no distribution (a NaN, a +infinity, only -infinities), a draft is
  * no token or a random number is NaN, the token there is -1, behind the drafts kept before.

@@ -639,7 +639,8 @@ def _rows_apart(x, rows, name):
 def draft_verify(logits, drafts, uniforms, draft_logits=None, counts=None, temperature=1.0, workspace=None):
     """Which drafted tokens are kept and the token behind them (nnc_draft_verify): logits [n, k + 1, vocab] of the target (float32,
     bfloat16, float16), drafts int32 [n, k], uniforms float32 [n, k + 1] of [0, 1), draft_logits [n, k, vocab] of the logits' type or None (drafts
-    that were not drawn), counts int32 [n] (0 .. k drafts each) or None, temperature: a number or float32 [n]; 0: greedy.
+    that were not drawn), counts int32 [n] (0 .. k drafts each) or None, temperature: a number or float32 [n]; 0: greedy.  A token is forbidden by -infinity
+    (a finite mask leaves it next to nothing, which a random number of exactly 0 may pick).
     Returns tokens int32 [n, k + 1] (the kept drafts, one token more, then -1) and how many were kept, int32 [n]."""
     L, torch = lib(), _torch
     if logits.dim() != 3 or logits.device.type != "cuda":

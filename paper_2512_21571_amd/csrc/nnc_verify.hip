@@ -50,7 +50,7 @@ constexpr double LOG2E = 1.4426950408889634;
 // lowest bits, r is exact: eight operations of 64 bits, which issue like others, and four others (960 rows of 151936 bf16 logits: with a
 // series up to r^11 and no table, twenty operations, 160 us; with x - m formed first and the exponent cut out of n 104 to 112; so 91).
 constexpr int EXP_STEPS = 256;
-constexpr double FAR_STEPS = 400. * EXP_STEPS;
+constexpr double FAR_STEPS = 1000. * EXP_STEPS, SCAN_FAR_STEPS = 400. * EXP_STEPS;
 struct ExpTable {
   double v[EXP_STEPS];  // 2^(i / 256), and i 2^12 off its upper half, where n 2^12 is added whose multiples of 256 are the exponent
   constexpr ExpTable() : v() {
@@ -67,25 +67,26 @@ struct ExpTable {
 __device__ constexpr ExpTable EXP_TABLE{};
 
 // What the logits of a row (or of a chunk) are measured by: a large one of them, m (finite), and the temperature.  Logits so far below it that
-// e^.. is below 2^-400 count as lying there; none is as far above it.  (Where the temperature is so low that the next smaller number than m does, it is taken to be as
-// high as that allows, which is the same.  m / T 256 log2 e is below 2^41 by that.)  Where no finite number is that far below m, `least` is -infinity: the sum has to
+// e^.. is below 2^-1000 count as lying there.  In the scan that is 2^-400: its m is not the largest, and none is that far above it.  (Where the temperature is
+// so low that the next smaller number than m does, it is taken to be as
+// high as that allows, which is the same.  m / T 256 log2 e is below 2^42 by that.)  Where no finite number is that far below m, `least` is -infinity: the sum has to
 // leave out what is -infinity by itself.
 __device__ __forceinline__ double steps_per(float T) { return EXP_STEPS * LOG2E / (double)T; }
 struct ExpBase {
   double c, bias;
   float least;
-  __device__ __forceinline__ ExpBase(float top, float T, double steps) : c(steps) {
-    constexpr double FAR = FAR_STEPS, MAGIC = 6755399441055744.;
-    least = top - T * (float)(FAR / (EXP_STEPS * LOG2E));
+  __device__ __forceinline__ ExpBase(float top, float T, double steps, double far) : c(steps) {
+    constexpr double MAGIC = 6755399441055744.;
+    least = top - T * (float)(far / (EXP_STEPS * LOG2E));
     if (!(least < top)) {
       const uint32_t b = __float_as_uint(top);
       least = __uint_as_float(top > 0.f ? b - 1 : top < 0.f ? b + 1 : 0x80000001u);
       // (-infinity behind the lowest number, from which the next one is 2^104 away)
-      c = fmin(c, FAR / (least > -INFINITY ? (double)top - (double)least : 0x1p104));
+      c = fmin(c, far / (least > -INFINITY ? (double)top - (double)least : 0x1p104));
     }
     bias = MAGIC - rint((double)top * c);
   }
-  __device__ __forceinline__ ExpBase(float top, float T) : ExpBase(top, T, steps_per(T)) {}
+  __device__ __forceinline__ ExpBase(float top, float T) : ExpBase(top, T, steps_per(T), FAR_STEPS) {}
 };
 __device__ __forceinline__ void exp_parts(float x, const ExpBase& b, const double* table, double& power, double& series) {
   constexpr double L = 0.69314718055994531 / EXP_STEPS;
@@ -104,6 +105,10 @@ __device__ __forceinline__ double exp_of(float x, const ExpBase& b, const double
 // (a forbidden token has no probability at all)
 __device__ __forceinline__ double probability(float x, const ExpBase& b, const double* table, double factor) {
   return x == -INFINITY ? 0. : exp_of(x, b, table) * factor;
+}
+// The same where two of them are compared: of what lies so far below the largest logit, for p as for q, nothing is known but that it is next to nothing.
+__device__ __forceinline__ double known_probability(float x, const ExpBase& b, const double* table, double factor) {
+  return x <= b.least ? 0. : exp_of(x, b, table) * factor;
 }
 __device__ __forceinline__ void load_table(double* table) {
   if (threadIdx.x < EXP_STEPS) table[threadIdx.x] = EXP_TABLE.v[threadIdx.x];
@@ -204,8 +209,8 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   bool nan = false, again = false;  // again: the sum has to leave out what is -infinity
   if (T > 0.f) {
     const double steps = steps_per(T);
-    const float far = fminf(T * (float)(FAR_STEPS / (EXP_STEPS * LOG2E)), 3.4028234663852886e38f);  // (-infinity and it are -infinity still)
-    ExpBase base(0.f, T, steps);
+    const float far = fminf(T * (float)(SCAN_FAR_STEPS / (EXP_STEPS * LOG2E)), 3.4028234663852886e38f);  // (-infinity and it are -infinity still)
+    ExpBase base(0.f, T, steps, SCAN_FAR_STEPS);
     auto add = [&](const float (&x)[16]) __attribute__((always_inline)) {
       float top = x[0];
 #pragma unroll
@@ -213,7 +218,7 @@ __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
       if (__any(top > m + far)) {  // (the first time, and where logits run away)
         const float mn = wave_max(top);
         const ExpBase before = base;
-        base = ExpBase(mn, T, steps);
+        base = ExpBase(mn, T, steps, SCAN_FAR_STEPS);
         // (by the largest so far, whose exponential is what the sum is about: by m, whose exponential ends at 2^-400, a sum of 2^400 would become 1)
         if (m > -INFINITY) {
           const float h = wave_max(high);
@@ -330,9 +335,12 @@ __device__ __forceinline__ void rest16(const VerifyArgs& a, const void* p, bool 
   const double pf = 1. / w.p_sum, qf = 1. / w.q_sum;
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    r[e] = probability(x[e], pb, table, pf);
-    if (residual == 1) r[e] = fmax(r[e] - probability(y[e], qb, table, qf), 0.);
-    else if (residual == 2 && at + e == w.drafted) r[e] = 0.;
+    if (residual == 1) {
+      r[e] = fmax(known_probability(x[e], pb, table, pf) - known_probability(y[e], qb, table, qf), 0.);
+    } else {
+      r[e] = probability(x[e], pb, table, pf);
+      if (residual == 2 && at + e == w.drafted) r[e] = 0.;
+    }
   }
 }
 
@@ -535,8 +543,8 @@ __global__ __launch_bounds__(64 * JUDGE_WAVES) void k_draft_judge(VerifyArgs a) 
           v = (double)u * (drafter ? x == drafted[lane].best ? 1. : 0. : 1.) < (x == p.best ? 1. : 0.);
         } else {
           double q = 1.;
-          if (drafter) q = probability(lq, ExpBase(drafted[lane].top, T), table, 1. / drafted[lane].sum);
-          v = (double)u * q < probability(lp, ExpBase(p.top, T), table, 1. / p.sum);
+          if (drafter) q = known_probability(lq, ExpBase(drafted[lane].top, T), table, 1. / drafted[lane].sum);
+          v = (double)u * q < known_probability(lp, ExpBase(p.top, T), table, 1. / p.sum);
         }
       }
       const uint64_t stop = __ballot(lane < n && v != 1);

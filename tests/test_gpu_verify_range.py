@@ -8,7 +8,7 @@ import torch
 
 import page_util as pu
 import share_util as su
-from share_util import DEV
+from share_util import DEV, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -153,3 +153,35 @@ def test_rows_of_nothing_but_the_lowest_number(nnc, v, t):
     u = np.array([[0.3], [0.51], [0.77], [0.9], [0.2]], np.float32)
     want = check(nnc, x, np.zeros((5, 0), np.int32), u, None, t)
     assert want[0][3, 0] == 0 and (t > 1 or want[0][4, 0] == v // 3)
+
+
+def test_probabilities_below_those_of_a_random_number(nnc):
+    """Drafts whose probabilities lie below 2^-400 of the best token's are compared like others, down to the end of 64 bits; what lies below
+    that, as tokens do that a finite mask forbids, is not kept, not even by a random number of zero."""
+    v = 3000
+    x = torch.zeros((8, 2, v))
+    y = torch.zeros((8, 1, v))
+    x[..., 7], y[..., 7] = 50.0, 50.0
+    far = [(-300.0, -600.0), (-600.0, -300.0), (-400.0, -400.5), (-400.5, -400.0), (-500.0, -499.0), (-1e9, -1e9), (LOWEST, LOWEST), (-2000.0, -3000.0)]
+    for i, (p, q) in enumerate(far):
+        x[i, :, 99], y[i, :, 99] = p, q
+    drafts = np.full((8, 1), 99, np.int32)
+    kept = {0.9: [1, 0, 1, 0, 0, 0, 0, 0], 0.5: [1, 0, 1, 1, 0, 0, 0, 0], 0.0: [1, 1, 1, 1, 1, 0, 0, 0]}
+    for u0, accepted in kept.items():
+        u = np.array([[u0, 0.5]] * 8, np.float32)
+        want = check(nnc, x, drafts, u, y, 1.0)
+        assert want[1].tolist() == accepted
+    # what is left of p behind q is next to nothing, or nothing, where they agree on all that counts
+    x[:, :, 5], y[:, :, 5] = -400.0, -700.0
+    u = np.array([[0.999, 0.5]] * 8, np.float32)
+    got = nnc.draft_verify(x.to(DEV), ints(drafts), torch.from_numpy(u).to(DEV), y.to(DEV))
+    want = su.verify(pu.f64(x), drafts, u.astype(np.float64), pu.f64(y), None, [1.0] * 8)
+    assert np.array_equal(got[0].cpu().numpy(), want[0])
+    u[:, 1] = 0.0                                                          # a mask is never what is picked behind a rejected draft
+    x[:, :, :4], y[:, :, :4] = -1e9, -1e9
+    got = nnc.draft_verify(x.to(DEV), ints(drafts), torch.from_numpy(u).to(DEV), y.to(DEV))
+    want = su.verify(pu.f64(x), drafts, u.astype(np.float64), pu.f64(y), None, [1.0] * 8)
+    lost = want[1] == 0
+    assert np.array_equal(got[0].cpu().numpy()[lost], want[0][lost]) and (want[0][lost, 0] >= 4).all() and np.array_equal(got[1].cpu().numpy(), want[1])
+    # ... but of p itself it is the first number of all, e^(-1e9 - 50) / sum > 0, where the random number is zero (in 64 bits that is a zero, as the definition here has it)
+    assert got[0][~torch.from_numpy(lost).to(DEV)].tolist() == [[99, 0]] * int((~lost).sum())
