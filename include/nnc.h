@@ -514,7 +514,7 @@ typedef struct {
  * Bring the bounds of a layer up to date: of every sequence i those of the pages that hold positions since[i] .. lens[i] - 1 (device
  * arrays of n_seqs; since NULL: since0 for all), each from all of the page's positions below lens[i].  max_new: no sequence has more such
  * positions (0: what the table holds); pages behind that many are left as they are.  A NaN among a page's keys makes the bounds of its dimension NaN.
- * Nothing is done for a negative length or since, nor for a page that does not exist.  A page that several of the sequences name gets
+ * Nothing is done for a negative length or since, for a since that is not below the length, nor for a page that does not exist.  A page that several of the sequences name gets
  * the bounds that one of them gives it: they are to see the same positions of it.
  */
 nnc_status nnc_page_bound(const nnc_pages *pages, uint32_t layer, const nnc_page_bounds *bounds, const nnc_page_table *table,

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void k_page_bound(PageBound b) {
   const uint32_t seq = blockIdx.y, id = blockIdx.x * 4 + (threadIdx.x >> 6), slot = fdiv(id, b.by_head), head = id - slot * b.p.n_kv_heads;
   const int lane = threadIdx.x & 63, row0 = lane / LPR, at = lane % LPR * EPL;
   const int32_t len = b.lens[seq], since = b.since ? b.since[seq] : b.since0;
-  if (slot >= b.slots || len < 0 || since < 0) return;
+  if (slot >= b.slots || since < 0 || len <= since) return;
   const uint32_t T = b.p.page_tokens, block = fdiv((uint32_t)since, b.p.by_page) + slot;
   if ((uint64_t)block * T >= (uint32_t)len || block >= b.t.max_pages) return;
   const int32_t page = b.t.entries[(size_t)seq * b.t.max_pages + block];
