@@ -139,10 +139,22 @@ __global__ __launch_bounds__(256) void k_page_bound(PageBound b) {
       }
       for (uint32_t r0 = 0; r0 < n; r0 += LOADS * ROWS) {
         load(r0, w, scale);
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) odd |= !(fabsf(scale[j]) < INFINITY);
+        if (odd) {  // a scale that is NaN makes a NaN of everything, an infinite one of a zero
+#pragma unroll 1
+          for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+              const uint32_t word = e < 8 ? (e < 4 ? w[j][0] : w[j][1]) : (e < 12 ? w[j][2] : w[j][3]);
+              const bool zero = ((word >> (e % 4 * 8)) & (STORE == PS_E4M3 ? 0x7fu : 0xffu)) == 0;
+              nan |= scale[j] != scale[j] || (zero && fabsf(scale[j]) == INFINITY) ? 1u << e : 0u;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
           const double s = (double)scale[j];
-          if (!(scale[j] == scale[j])) nan = 0xffffu;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float f[4];

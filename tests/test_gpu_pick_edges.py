@@ -1,8 +1,12 @@
-"""Bounds of pages without new positions."""
+"""Bounds of pages without new positions and of rows with infinite scales."""
+import math
+
+import numpy as np
 import pytest
+import torch
 
 import page_util as pu
-from share_util import ints
+from share_util import DEV, ints
 from test_gpu_pick import check_bounds, filled, nnc  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +33,23 @@ def test_sequences_without_new_positions_leave_bounds_alone(nnc, store):
         x.fill_(7.0)
     p.bound(1, bounds, shared, ints(lens), since=ints([40, 37, 33, 47]), max_new=1)
     check_bounds(p, bounds, old, shared, lens, [48, 48, 48, 47])
+
+
+@pytest.mark.parametrize("store", list(pu.TOP))
+@pytest.mark.parametrize("tokens", [1, 7, 40])
+def test_bounds_of_rows_with_infinite_scales(nnc, store, tokens):
+    """An infinite scale makes its row's zeros NaN and its other values infinite."""
+    p, tables = filled(nnc, store, [3 * tokens], tokens, 2, 128)
+    rng = np.random.default_rng(2)
+    page = int(tables[0, 1])
+    row = rng.integers(-1, 2, 128)                                            # (a third of them zeros)
+    p.k[1, page, 1, tokens // 2] = torch.from_numpy(row).float().to(p.k.dtype).to(DEV)
+    p.k_scale[1, page, 1, tokens // 2] = math.inf
+    bounds = p.empty_bounds()
+    p.bound(1, bounds, tables, ints([3 * tokens]))
+    with np.errstate(invalid="ignore"):
+        k = pu.pool_values(p, 1)[0][page, 1]
+    lo, hi = (pu.f64(x[1, page, 1]) for x in bounds)
+    assert np.array_equal(np.isnan(lo), row == 0) and np.array_equal(np.isnan(hi), row == 0)
+    assert (hi[row > 0] == math.inf).all() and (lo[row < 0] == -math.inf).all()
+    assert (lo[row > 0] <= k[:, row > 0].min(0)).all() and (hi[row < 0] >= k[:, row < 0].max(0)).all()
