@@ -1,4 +1,4 @@
-"""Bounds of pages without new positions and of rows with infinite scales."""
+"""Bounds of pages without new positions and with scales that are infinite, picks by infinite bounds."""
 import math
 
 import numpy as np
@@ -6,8 +6,8 @@ import pytest
 import torch
 
 import page_util as pu
-from share_util import DEV, ints
-from test_gpu_pick import check_bounds, filled, nnc  # noqa: F401
+from share_util import DEV, ints, make_pool, queries
+from test_gpu_pick import check_bounds, check_pick, filled, nnc, random_bounds  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,30 @@ def test_bounds_of_rows_with_infinite_scales(nnc, store, tokens):
     assert np.array_equal(np.isnan(lo), row == 0) and np.array_equal(np.isnan(hi), row == 0)
     assert (hi[row > 0] == math.inf).all() and (lo[row < 0] == -math.inf).all()
     assert (lo[row > 0] <= k[:, row > 0].min(0)).all() and (hi[row < 0] >= k[:, row < 0].max(0)).all()
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,group,dim", [(1, 1, 128), (2, 2, 64), (2, 5, 128), (1, 4, 64)])
+def test_scores_of_infinite_bounds(nnc, store, rows, heads, group, dim):
+    """max(q lo, q hi) of an infinite bound is the other one's product where q has the sign for it, infinite where it has not, NaN where q is zero."""
+    p = make_pool(nnc, store, 2, 60, 16, heads, dim)
+    tables = ints(np.random.default_rng(1).permutation(60)[None].repeat(3, 0))
+    bounds, q = random_bounds(p, 3), queries((3, heads * group, dim), rows)
+    lo, hi = bounds
+    q[0, :, 5], q[1, :, 5], q[2, :, 5] = 1.5, -1.5, 0.0
+    q[:, :, 9] = -q[:, :, 5]
+    lo[1, 10:20, :, 5] = -math.inf
+    hi[1, 20:30, :, 5] = math.inf
+    lo[1, 25:35, :, 9], hi[1, 25:35, :, 9] = -math.inf, math.inf
+    lo[1, 40, :, 5], hi[1, 41, :, 9] = math.inf, -math.inf
+    hi[1, 40, :, 5], lo[1, 41, :, 9] = math.inf, -math.inf
+    lens = [960, 955, 960]
+    for keep in (3, 12, 30, 50):
+        check_pick(p, p.pick(1, bounds, q, tables, ints(lens), keep), bounds, q, tables, lens, keep, 1, 1)
+    many = ints(np.random.default_rng(2).integers(0, 60, (3, 400)))          # the same pages beside infinite ones and beside others: ties everywhere
+    lens = [6400, 6391, 6400]
+    check_pick(p, p.pick(1, bounds, q, many, ints(lens), 150), bounds, q, many, lens, 150, 1, 1)
+    lens = [960, 955, 960]
+    lo[1, :, :, 5] = -math.inf                                               # on every page: only where q is positive does the score stay a number
+    check_pick(p, p.pick(1, bounds, q, tables, ints(lens), 20), bounds, q, tables, lens, 20, 1, 1)
