@@ -1,4 +1,4 @@
-"""Bounds of pages without new positions and with scales that are infinite, picks by infinite bounds."""
+"""Bounds of pages without new positions and with scales that are infinite, picks by infinite bounds and of thousands of pages."""
 import math
 
 import numpy as np
@@ -80,3 +80,17 @@ def test_scores_of_infinite_bounds(nnc, store, rows, heads, group, dim):
     lens = [960, 955, 960]
     lo[1, :, :, 5] = -math.inf                                               # on every page: only where q is positive does the score stay a number
     check_pick(p, p.pick(1, bounds, q, tables, ints(lens), 20), bounds, q, tables, lens, 20, 1, 1)
+
+
+@pytest.mark.parametrize("blocks,keep,first,last", [(8192, 256, 1, 2), (8193, 500, 2, 1), (12001, 64, 0, 1), (16384, 4096, 3, 9), (16385, 100, 1, 1)])
+def test_pick_of_thousands_of_pages(nnc, blocks, keep, first, last):
+    """Both sides of the number of pages that a thread keeps in registers, with ties and without."""
+    p = make_pool(nnc, "bf16", 2, 50, 4, 1, 64)
+    tables = ints(np.random.default_rng(blocks).integers(0, 50, (2, blocks)))
+    bounds, q = random_bounds(p, 4), queries((2, 2, 64), "bf16")
+    lens = [blocks * 4, blocks * 4 - 1021]
+    check_pick(p, p.pick(1, bounds, q, tables, ints(lens), keep, first=first, last=last), bounds, q, tables, lens, keep, first, last)
+    p = make_pool(nnc, "f16", 2, blocks, 1, 1, 64)
+    tables = ints(np.random.default_rng(1).permutation(blocks)[None])
+    bounds, q = random_bounds(p, 5), queries((1, 3, 64), "f32")
+    check_pick(p, p.pick(1, bounds, q, tables, ints([blocks]), keep, first=first, last=last), bounds, q, tables, [blocks], keep, first, last)
