@@ -482,8 +482,10 @@ nnc_status nnc_page_attention(const nnc_pages *pages, uint32_t layer, const nnc_
  *     more positions behind its prefix (0: none has any).
  *   prefix NULL: the table has a row for every group, whose query rows are new tokens of one sequence: row r sees its first lens[r]
  *     positions, all of them read once (max_own is not looked at).
- * The result of a row is that of nnc_page_attention for its length, but for the order of sums and, with NNC_BF16 queries over a pool of 16 or 8
- * bits, the products' weights, which have 17 bits (2^-18 of sum w |v| is left out; the output's own rounding is 2^-9 of it).  A length may end
+ * The result of a row is that of nnc_page_attention for its length, but for the order of sums and, with NNC_BF16 queries over an NNC_BF16 pool or one of 8
+ * bits, where a group has more than sixteen rows (width x query heads of a kv head) or none has positions of its own, the products' weights, which have 17 bits
+ * (2^-18 of sum w |v| is left out; the output's own rounding is 2^-9 of it).  Weights of up to 2^20 stand in those sums: values of V beyond 2^107 / positions may
+ * make them infinite.  A length may end
  * inside the prefix; it gives zeros where it is 0, and NaN where it is negative, above max_len or more than max_own behind the prefix, as
  * does a negative prefix.  A row is NaN as a whole where one of its positions has no page or a value of V that is not finite
  * and that other rows do not see.  What positions behind a row's own length hold does not reach it.  query->window must be 0.

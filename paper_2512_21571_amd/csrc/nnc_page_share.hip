@@ -126,9 +126,11 @@ __device__ __forceinline__ uint32_t rows_flagged(bool x) {
   return (uint32_t)(b | (b >> 16) | (b >> 32) | (b >> 48)) & 0xffffu;
 }
 
-// Weights in pieces of the matrix cores' type: three for an fp32 output, and two, where the queries and so the output have 16 bits: two
-// bf16 pieces leave out 2^-18 of a weight, which is 2^-9 of the output's own rounding, two binary16 pieces 2^-22.  (Two for three: the 256
-// rows of 16384 positions of launch_page_share's figures 50.9 -> 43.5 us.)  The remainder behind a bf16 value is one product of pairs, v - (0 a + 1 b),
+// Weights in pieces of the matrix cores' type: three for an fp32 output; where the queries and so the output have 16 bits, two of binary16, which leave out
+// 2^-22 of a weight.  Of bf16 two leave out 2^-18, 2^-9 of the output's own rounding: two in k_page_attn_block, where the third costs 10% of a wide group and 2% of
+// a few rows (no positions of their own, 16384 positions, 256 rows 45.1 us with two and 49.6 with three, 64 25.8 and 27.1, 20 20.5 and 21.1), three in
+// k_page_attn_rows, which waits for its loads (8 rows of 304 positions 14.3 us with two and 14.4 with three, of 16384 23.6 and 23.7).
+// The remainder behind a bf16 value is one product of pairs, v - (0 a + 1 b),
 // exact like the subtraction (a weight that is no number spoils its neighbour, which is of the same row).  The pairs (-1, 0) and (0, -1) are kept
 // from the compiler, which takes the first for the inline constant -1, to the instruction a pair (0, -1).
 template <class HF, int NP>
@@ -225,7 +227,7 @@ template <int STORE, int D, bool FULL, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
   constexpr bool B8 = page_scaled(STORE);
-  constexpr int NQ = FULL ? 3 : 1, NP = FULL ? 3 : 2, KT = D / 32, DT = D / 16;
+  constexpr int NQ = FULL ? 3 : 1, NP = FULL || !HF::kNarrowRange ? 3 : 2, KT = D / 32, DT = D / 16;
   constexpr int LD = B8 ? D / 64 : D / 32;   // 16-byte loads of a lane per row: bytes i * 64 + g * 16
   constexpr int PITCH = D * 2 + 32, OPITCH = D + 4;
   __shared__ __attribute__((aligned(16))) char vbuf[NW][32 * PITCH];

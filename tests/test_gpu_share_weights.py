@@ -1,5 +1,4 @@
-"""What the weights of shared and of picked attention carry, in every form of their kernels, where sums cancel and where
-values of V are as large as their type's."""
+"""What the weights of shared and of picked attention carry, in every form of their kernels, where sums cancel."""
 import numpy as np
 import pytest
 import torch
@@ -76,3 +75,26 @@ def test_picked_pages_have_the_weights_of_one_row(nnc, store, rows, dim):
     q[..., 0] = 1.0
     out = p.attention(0, q, ints([[[0]]] * 3), ints([[N]] * 3), scale=1.0)
     check(out, s, x, rows, 2.0 ** -22 if store == rows == "f16" else 0.0)
+
+
+@pytest.mark.parametrize("store", ["bf16", "i8", "e4m3"])
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("width,prefix", [(1, 3), (1, 0), (4, 3), (8, 5), (16, 0)])
+def test_up_to_sixteen_rows_with_their_own_positions_have_the_weights_of_one_row(nnc, store, dim, width, prefix):
+    """Forty groups of different scores: what a weight's pieces leave out differs from score to score."""
+    groups, rng = 40, np.random.default_rng(3)
+    p = nnc.Pages.empty(1, groups, 8, 1, dim, pu.STORES[store], DEV)
+    made = [cancelling(rng, store, dim, N) for _ in range(groups)]
+    k, v, ks, vs = np.zeros((groups, 8, dim)), np.zeros((groups, 8, dim)), np.zeros((groups, 8)), np.ones((groups, 8))
+    for i, (s, x, scale) in enumerate(made):
+        k[i, :N, 0], v[i, :N], ks[i, :N], vs[i, :N] = (s if store == "bf16" else -1), x, -s, scale
+    p.k.copy_(torch.from_numpy(k).float()[None, :, None].to(p.k.dtype))
+    p.v.copy_(torch.from_numpy(v).float()[None, :, None].to(p.v.dtype))
+    if p.k_scale is not None:
+        p.k_scale.copy_(torch.from_numpy(ks).float()[None, :, None])
+        p.v_scale.copy_(torch.from_numpy(vs).float()[None, :, None])
+    q = torch.zeros((groups, width, 1, dim), device=DEV, dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    out = p.attention_shared(0, q, ints(np.repeat(np.arange(groups), width)[:, None]), ints(np.full((groups, width), N)), ints(np.full(groups, prefix)), max_own=N - prefix, scale=1.0)
+    for i, (s, x, scale) in enumerate(made):
+        check(out[i], s, x * scale[:, None], "bf16", 0.0)
