@@ -349,8 +349,8 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
         for (int i = 0; i < 8; ++i) {
           const double q = element(a.q, a.q_dtype, (int64_t)seq * a.q_row + (int64_t)(kvh * G + h) * a.q_head + dim + i);
           const double lo = element(a.lo, DT, (int64_t)at + i), hi = element(a.hi, DT, (int64_t)at + i);
-          if (!(q < 0.)) sum[0] = __builtin_fma(q, hi, sum[0]);
-          if (!(q > 0.)) sum[0] = __builtin_fma(q, lo, sum[0]);
+          if (!(q < 0.) || hi != hi) sum[0] = __builtin_fma(q, hi, sum[0]);  // (a NaN counts whatever the sign is)
+          if (!(q > 0.) || lo != lo) sum[0] = __builtin_fma(q, lo, sum[0]);
         }
         lanes_sum<LPR / 2>(sum, lane);
         top = max(top, order_of(sum[0]));

@@ -82,6 +82,20 @@ def test_scores_of_infinite_bounds(nnc, store, rows, heads, group, dim):
     check_pick(p, p.pick(1, bounds, q, tables, ints(lens), 20), bounds, q, tables, lens, 20, 1, 1)
 
 
+@pytest.mark.parametrize("store", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("heads,group,dim", [(1, 1, 128), (2, 2, 64), (2, 5, 128)])
+def test_a_nan_in_one_bound_is_a_score_of_nan(nnc, store, heads, group, dim):
+    """... whatever sign the query has there."""
+    p = make_pool(nnc, store, 2, 60, 16, heads, dim)
+    tables = ints(np.random.default_rng(1).permutation(60)[None].repeat(2, 0))
+    bounds, q = random_bounds(p, 3), queries((2, heads * group, dim), "f32")
+    q[0, :, 7], q[1, :, 7] = 0.5, -0.5
+    bounds[0][1, 20, :, 7], bounds[1][1, 30, :, 7] = math.nan, math.nan
+    bounds[0][1, 40, :, 3], bounds[1][1, 40, :, 4] = -math.inf, math.nan
+    for keep in (3, 5, 20):
+        check_pick(p, p.pick(1, bounds, q, tables, ints([960, 960]), keep), bounds, q, tables, [960, 960], keep, 1, 1)
+
+
 @pytest.mark.parametrize("blocks,keep,first,last", [(8192, 256, 1, 2), (8193, 500, 2, 1), (12001, 64, 0, 1), (16384, 4096, 3, 9), (16385, 100, 1, 1)])
 def test_pick_of_thousands_of_pages(nnc, blocks, keep, first, last):
     """Both sides of the number of pages that a thread keeps in registers, with ties and without."""
