@@ -477,11 +477,12 @@ nnc_status nnc_page_attention(const nnc_pages *pages, uint32_t layer, const nnc_
 /*
  * Attention of rows that share the first positions of their contexts (a batch behind one prompt, the beams of a search, the new
  * tokens of one sequence).  Query row g * width + w is row w of group g; query->lens: device [rows].
- *   prefix not NULL: device [groups]; the table has a row for every query row.  Positions below prefix[g] are read once for
- *     the whole group, through the table row of its first query row, the others through the row's own.  max_own: no row has
+ *   prefix not NULL: device [groups]; the table has a row for every query row.  Positions below prefix[g] are read for the
+ *     whole group (once for up to 128 rows x query heads of a kv head, 64 where the queries are not of the type that the pool's products are
+ *     in, 16 of an fp32 pool) through the table row of its first query row, the others through the row's own.  max_own: no row has
  *     more positions behind its prefix (0: none has any).
  *   prefix NULL: the table has a row for every group, whose query rows are new tokens of one sequence: row r sees its first lens[r]
- *     positions, all of them read once (max_own is not looked at).
+ *     positions, all of them read in the same way (max_own is not looked at).
  * The result of a row is that of nnc_page_attention for its length, but for the order of sums and, with NNC_BF16 queries over an NNC_BF16 pool or one of 8
  * bits, where a group has more than sixteen rows (width x query heads of a kv head) or none has positions of its own, the products' weights, which have 17 bits
  * (2^-18 of sum w |v| is left out; the output's own rounding is 2^-9 of it).  Weights of up to 2^20 stand in those sums: values of V beyond 2^107 / positions may
@@ -506,7 +507,7 @@ nnc_status nnc_page_attention_shared(const nnc_pages *pages, uint32_t layer, con
  * Attention to a part of a long context: the pages whose keys promise the largest scores.
  * nnc_page_bounds: for every page and kv head the smallest and the largest key, dimension by dimension, memory of the caller:
  *   lo, hi  [n_layers][n_pages][n_kv_heads][head_dim], on a multiple of 16 bytes; in the pool's dtype, NNC_BF16 for pools of 8 bits
- *           (whose values, with their scales, are rounded outwards: downwards in lo, upwards in hi)
+ *           (whose values, with their scales, are rounded outwards: downwards in lo, upwards in hi).  lo <= hi, or a NaN in one of them
  */
 typedef struct {
   void *lo, *hi;

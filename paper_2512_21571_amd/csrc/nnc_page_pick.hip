@@ -46,7 +46,8 @@ __device__ __forceinline__ uint32_t word_of(i16x2 v) { return __builtin_bit_cast
 // A wave per page and kv head: 64 / LPR rows at a time, a lane 16 bytes of one (EPL values), four such loads on their way at once.
 // Sixteen-bit keys are compared as integers, two at a time.  A value of 8 bits times its scale is exact in 64 bits; rounding outwards
 // does not change an order, so lanes round their own before they compare.  A NaN shows in both bounds of its dimension.
-// Bound: the keys' bytes (16384 rows of 8 kv heads, bf16, 37.7 MB read and written: 7.6 us, 5.0 TB/s); a step's few pages: the loads that wait
+// Bound: the keys' bytes (16384 rows of 8 kv heads, bf16, 37.7 MB read and written: 7.2 us, 5.2 TB/s), of 8 bits the 64-bit products, minima and maxima
+// (int8 23 us, e4m3 26); a step's few pages: the loads that wait
 // for each other, length -> table -> row (48 sequences, int8, 8.6 us).
 template <int STORE, int D>
 __global__ __launch_bounds__(256) void k_page_bound(PageBound b) {
@@ -262,7 +263,7 @@ __device__ __forceinline__ double element(const void* p, int dtype, int64_t i) {
 // LPR lanes a page, eight dims each, LOADS pages of them on their way at once; max(q lo, q hi) is q hi for a positive and q lo for a
 // negative q, so that a product with both parts of q is all there is to do, HG query heads at a time.
 // Bound: loads that wait for each other (length, table, bounds) and then the 64-bit products, 1.7 us for each query head (8192 pages, 8 kv heads,
-// bf16, 33.5 MB: 7.1 us for one query head, 12.8 for four, 18.7 for eight; with every sum on its own through all lanes 7.6, 13.4, 20.3).  Two or
+// bf16, 33.5 MB: 7.2 us for one query head, 13.0 for four, 18.5 for eight; with every sum on its own through all lanes 7.6, 13.4, 20.3).  Two or
 // eight pages on their way 14.1 and 18.6 us for four heads, two heads at a time in place of four no less at two thirds of the registers.
 template <int DT, int D, int HG>
 __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* keys) {
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(256, 2) void k_page_score(PagePick a, uint64_t* key
 // highest bit in which two keys differ) until few keys are left, which are ranked; then the pages above it and, lowest
 // first, as many equal to it as fit, in order.  R: keys that a thread keeps in registers, key i of it page 1024 i + thread; 0: more
 // pages, which are read again for every digit.  Bound: latency, of the passes and of the barriers between them
-// (8192 pages 10.5 us, 512 pages 5.5).  With 16 keys a thread 12.6 and 9.2, read again for every digit 18.9 and 7.3; 16384 pages with 16 keys
+// (8192 pages 10.2 us, 512 pages 5.4).  With 16 keys a thread 12.6 and 9.2, read again for every digit 18.9 and 7.3; 16384 pages with 16 keys
 // 16.2 and 41.9, 31250, which no registers hold, 65.5.
 template <int R>
 __global__ __launch_bounds__(1024) void k_page_best(PagePick a, const uint64_t* all) {

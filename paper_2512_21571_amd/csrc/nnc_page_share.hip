@@ -222,7 +222,7 @@ __device__ __forceinline__ void load_queries(const AttnArgs& a, const Block<RT>&
 // Rows see different positions: scores of others are -infinity.  Weight zero does not hide an infinity or a NaN in V, so values that are not finite are
 // taken as zeros where not every row sees them, and rows that do become NaN; the same for pages that do not exist.
 // Bound: the loads that wait for each other (length, table, rows) and a tile's chain of a wave, not bytes: four rows of 304 + 1 .. 16 positions, 8 kv
-// heads, bf16, 1.4 MB, 14.8 us; of 16384, 67 MB, 19.7 (3.4 TB/s).
+// heads, bf16, 1.4 MB, 14.9 us; of 16384, 67 MB, 19.3 (3.5 TB/s).
 template <int STORE, int D, bool FULL, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
   using HF = std::conditional_t<STORE == PS_F16, Fp16, Bf16>;
@@ -467,8 +467,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_page_attn_rows(AttnArgs a) {
 // down, widened, in a second buffer.  Products, pieces, layouts and masks as above; what a position spoils (`spoilt`: the first one
 // without a page, or with a value in V that is no number and has been taken out) is looked at in the end.
 // Bound: the vector instructions of the softmax and of the weights' pieces between the matrix instructions, and for few rows one
-// wave's chain on each SIMD.  256 rows (64 sequences of 4 query heads) of 16384 positions, 8 kv heads, bf16, 67 MB, 42 us: 410 TFLOP/s of the
-// two products, 615 of those issued; 20 rows each of four sequences of 333 .. 4100 positions over int8 18.4 us.  At 65536 positions,
+// wave's chain on each SIMD.  256 rows (64 sequences of 4 query heads) of 16384 positions, 8 kv heads, bf16, 67 MB, 38 us: 450 TFLOP/s of the
+// two products, 680 of those issued; 20 rows each of four sequences of 333 .. 4100 positions over int8 17.9 us.  At 65536 positions,
 // 172 us with three pieces, it took 102 without the second product, 153 without exponentials and pieces, 148 without loads; a second tile of
 // loads on its way changed nothing (18.6 for 18.4 us, 87.7 for 81).
 template <int STORE, int D, bool FULL, int NW, int WR>

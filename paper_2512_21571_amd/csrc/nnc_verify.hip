@@ -48,7 +48,8 @@ constexpr double LOG2E = 1.4426950408889634;
 // log2 e = (N + n + r) / 256, |r| <= 1/2, N a whole number near m / T 256 log2 e, it is 2^(n / 256) out of a table of 256 and an exponent, times
 // the series of e^(r ln2 / 256) up to r^3 (the next term is below 2^-42.7).  n is what a product and a sum with 1.5 2^52 - N leave in the
 // lowest bits, r is exact: eight operations of 64 bits, which issue like others, and four others (960 rows of 151936 bf16 logits: with a
-// series up to r^11 and no table, twenty operations, 160 us; with x - m formed first and the exponent cut out of n 104 to 112; so 91).
+// series up to r^11 and no table, twenty operations, 160 us; with x - m formed first and the exponent cut out of n 104 to 112; so 91, and 81 in a run of
+// passes, which the clock has risen for).
 constexpr int EXP_STEPS = 256;
 constexpr double FAR_STEPS = 1000. * EXP_STEPS, SCAN_FAR_STEPS = 400. * EXP_STEPS;
 struct ExpTable {
@@ -180,7 +181,8 @@ __device__ __forceinline__ double wave_scan(double v, int lane) {
 }
 
 // A wave per chunk, the next sixteen elements of a lane on their way during the work on these.  Bound: the logits' bytes where they are fp32 (176 rows
-// of 151936 17 us, 6.2 TB/s), the instructions where they have sixteen bits (960 rows 91 us: 17 of them for each 64 exponentials, 80% of the issue slots).
+// of 151936 16.5 us, 6.4 TB/s), the instructions where they have sixteen bits (960 rows 81 us: 17 of them for each 64 exponentials, 80% of the issue
+// slots; at temperature 0, where nothing but a maximum is looked for and no load is on its way meanwhile, 47.5).
 template <int DT>
 __global__ __launch_bounds__(256) void k_draft_scan(VerifyArgs a) {
   __shared__ double table[EXP_STEPS];
@@ -487,8 +489,8 @@ __device__ __forceinline__ void answer(const VerifyArgs& a, uint32_t i, int32_t 
 
 // Every workgroup of a sequence decides for itself (a few dozen numbers a row), and each of its waves adds r up over a chunk where that
 // takes the draft's probabilities off the target's.  Otherwise the sequence has one workgroup, which picks its token too.
-// Bound: few sequences the loads that wait for each other (one of four drafts 8.5 us), many the 64-bit exponentials of p and q where
-// q is taken off (16 sequences of 151936 tokens 14.5 us, 64 27).
+// Bound: few sequences the loads that wait for each other (one of four drafts 8.1 us), many the 64-bit exponentials of p and q where
+// q is taken off (16 sequences of 151936 tokens 13.9 us, 64 23.6).
 template <int DT>
 __global__ __launch_bounds__(64 * JUDGE_WAVES) void k_draft_judge(VerifyArgs a) {
   constexpr int ROWS = 32;  // drafts that are judged at once
